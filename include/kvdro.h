@@ -51,8 +51,11 @@ typedef enum {
     KVDRO_ENOMEM = -2,   /* a device or pinned-host allocation failed */
     KVDRO_ECUDA = -3,    /* a CUDA call failed (message in kvdro_last_error) */
     KVDRO_ESTATE = -4,   /* call out of order, e.g. eval before samples are loaded */
-    KVDRO_ETIMEOUT = -5  /* a kernel gave up a bounded wait and reported it; the outputs are then
+    KVDRO_ETIMEOUT = -5, /* a kernel gave up a bounded wait and reported it; the outputs are then
                             incomplete (r_idx is -1 where no r was evaluated) */
+    KVDRO_ERANGE = -6    /* a page cache kernel met a value in device memory outside its range (a page
+                            number, a slot, a length); it left out what the value stood for.  Reported
+                            by kvdro_sync */
 } kvdro_status;
 
 typedef enum {
@@ -203,7 +206,107 @@ int kvdro_eval_grid_noalloc(int32_t K, const int64_t* offsets, const int32_t* le
                             float* cost, int32_t* lam_idx, int32_t* r_idx, float* min_cost, double* fhat,
                             void* stream, char* err, int32_t err_len);
 
-/* Wait for the context's device work and report any asynchronous CUDA error or kernel timeout. */
+/*
+ * The page cache -- what a serving engine does with the reservations.  Keys and values live in
+ * pages of `page_size` token slots; a request holds a row of page numbers (its block table), as many
+ * as its reservation r asks for.  One step of a server is
+ *     kvdro_kv_plan     pages for the requests' lengths and reservations, slots for their new tokens
+ *     kvdro_kv_append   the new tokens' keys and values into those slots     (once per layer)
+ *     kvdro_kv_attend   the new tokens' attention over their requests' pages (once per layer)
+ * The paper's data plane runs a paged cache of this kind unchanged beneath its decisions (Fig. 1, Sec. 2).
+ * All arrays are device memory and every call is asynchronous on `stream` and allocates nothing, so
+ * that calls can be captured into a CUDA graph (after one call of the same kind outside a capture,
+ * which loads its kernels).  A value in device memory that is out of range is never followed: the kernels leave
+ * out what it stands for and the next kvdro_sync() returns KVDRO_ERANGE.
+ * Calls on one context may use several streams: kvdro_kv_attend orders its scratch across
+ * them itself, outside of captures (the launches of captured graphs that share a context must be ordered by
+ * the caller); the caller orders everything else (his arrays) as for any kernel.
+ */
+typedef struct kvdro_kv kvdro_kv;
+
+typedef enum { KVDRO_BF16 = 0, KVDRO_FP16 = 1 } kvdro_kv_dtype;
+
+/*
+ * Describe a page cache that the caller owns: k and v hold element (page, slot, head, d) at
+ * page * stride[0] + slot * stride[1] + head * stride[2] + d, strides in elements (NULL: [n_pages][page_size]
+ * [n_kv_heads][head_dim], contiguous).
+ *   dtype       KVDRO_BF16 or KVDRO_FP16;  page_size: 16, 32, 64 or 128;  head_dim: 64 or 128.
+ *   n_pages     >= 1, n_pages * page_size < 2^31;  1 <= n_kv_heads <= 1024.
+ *   k, v        device memory, 16-byte aligned, strides positive multiples of 8 elements below 2^39.
+ * The arrays must outlive the handle; the handle must not be used after kvdro_destroy(ctx), which frees
+ * the handles left open.  Allocates scratch of the context's own, at the first call.
+ */
+int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
+                  int32_t head_dim, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride);
+
+/* Free the handle (the arrays stay the caller's).  NULL is accepted. */
+int kvdro_kv_close(kvdro_kv* kv);
+
+/*
+ * Pages for one step.  For request b with cached[b] tokens in the cache, new_len[b] tokens to come in this
+ * step, reserve[b] tokens to hold pages for (the reservation r, input included) and held[b] pages at table[b]:
+ *   new_len > 0   pages are handed out until ceil(max(cached + new_len, min(reserve, max_pages * page_size)) /
+ *                 page_size) are held.  In the order of b, until one does not fit the free pages: that request and every later one
+ *                 that needs pages is refused, as is one whose tokens pass max_pages * page_size.  A refused request keeps
+ *                 what it holds; its tokens have slot and pos -1 and its kv_len is 0.
+ *   new_len = 0   the request waits: it keeps its pages.
+ *   new_len < 0   the request is done: its pages go back, to be handed out from the next call on.
+ * Free pages are a ring of n_pages page numbers: pool = {head, count}; pages are taken at head and
+ * returned behind the last.  Every page number is in the ring or in one request's table.
+ *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size < 2^31.
+ *   cached, new_len, held  int32[B];  reserve: int32[B] or NULL (no reservations).
+ *   table      int32[B][max_pages], updated: entries held[b] <= j < held_out[b] are written.
+ *   ring       int32[n_pages], updated: returned pages are written behind the last.
+ *   pool       int32[2];  pool_out: int32[2];  held_out: int32[B] (held and pool are not changed, and
+ *              must not overlap their outputs: the same call again gives the same results).
+ *   q_off      int32[B+1]  prefix sums of max(new_len, 0): request b's tokens are q_off[b] .. q_off[b+1]-1.
+ *   kv_len     int32[B]    cached + new_len, the tokens that kvdro_kv_attend sees; 0 if refused or done.
+ *   slot, pos  int32[T] (pos may be NULL; T >= 0)  page * page_size + offset, and the position in the request, of every
+ *              new token; -1 behind the last token.  More new tokens than T is a range error (the rest is left out).
+ */
+int kvdro_kv_plan(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages, int32_t B, int32_t max_pages, int32_t T,
+                  const int32_t* cached, const int32_t* new_len, const int32_t* reserve, const int32_t* held,
+                  int32_t* table, int32_t* ring, const int32_t* pool, int32_t* held_out, int32_t* pool_out,
+                  int32_t* q_off, int32_t* kv_len, int32_t* slot, int32_t* pos, void* stream);
+
+/*
+ * Write T tokens' keys and values into their slots: cache[slot[t]] = k[t], v[t] for every head; a
+ * token whose slot is -1 is skipped.  Slots must differ from one another.
+ *   k, v       element (t, head, d) at t * stride[0] + head * stride[1] + d, strides in elements (NULL: contiguous
+ *              [T][n_kv_heads][head_dim]), of the cache's dtype; 16-byte aligned, strides multiples of 8.
+ *   slot       int32[T], T >= 0.
+ */
+int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_stride, const void* v,
+                    const int64_t* v_stride, const int32_t* slot, void* stream);
+
+/*
+ * Attention of the new tokens over their requests' cached ones, their own included (append first).  Token i
+ * of request b's n = q_off[b+1] - q_off[b] stands at position p = kv_len[b] - n + i; its query head h reads key/value
+ * head h / (n_heads / n_kv_heads):
+ *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q . k_j),   f(x) = x, or softcap tanh(x / softcap)
+ * over the positions j < kv_len[b] with j <= p (causal) and j > p - window (window > 0).  A token that sees
+ * no position gets out = 0 and lse = -infinity.  What is stored at unseen positions does not
+ * matter, NaN included.  Products are of the cache's dtype with FP32 sums; the softmax is FP32, its
+ * weights are rounded to the cache's dtype for the product with v.
+ *   B          requests, 1 <= B <= 16384;  T: tokens, T >= 0; tokens beyond T are left out, and T tokens of out and lse
+ *              are written (zeros and -infinity for tokens of no request).
+ *   n_heads    a multiple of n_kv_heads, at most 4096.
+ *   max_q      the most new tokens of one request, as far as the caller knows, 0 if unknown.  It chooses among
+ *              kernels; the results are right whatever it says.
+ *   q, out     element (t, h, d) at t * stride[0] + h * stride[1] + d (NULL: contiguous [T][n_heads][head_dim]), of the
+ *              cache's dtype; 16-byte aligned, strides multiples of 8.
+ *   q_off      int32[B+1], ascending from 0;  kv_len: int32[B];  table: int32[B][max_pages].
+ *   scale      finite;  causal: 0 or 1;  window >= 0 (0: none; needs causal);  softcap finite, >= 0 (0: none).
+ *   lse        float [T][n_heads], log sum_j exp(s_j); may be NULL.
+ */
+int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,
+                    const int64_t* q_stride, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                    int32_t max_pages, double scale, int causal, int32_t window, double softcap, void* out,
+                    const int64_t* out_stride, float* lse, void* stream);
+
+/* Wait for the context's last call's stream and report any asynchronous CUDA error, kernel timeout or value out
+ * of range.  (Page cache calls on several streams: what kernels on the others found is reported
+ * once they are done.) */
 int kvdro_sync(kvdro_ctx* ctx);
 
 /* Text of the last error on this context ("" if none).  Valid until the next call on ctx. */

@@ -5,17 +5,12 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
-#include <cstdarg>
-#include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <string>
 #include <vector>
 
-#include <nvtx3/nvToolsExt.h>
-
-#include "kvdro.h"
-#include "kvdro_internal.cuh"
+#include "context.cuh"
 
 namespace kvdro {
 int64_t hist_slice_samples();
@@ -24,7 +19,16 @@ int64_t scan_tile_bins();
 bool scan_direct(int64_t scan_tiles);
 }  // namespace kvdro
 
+using kvdro::align_up;
+using kvdro::Buf;
+using kvdro::cuda_fail;
+using kvdro::DeviceGuard;
+using kvdro::ensure;
+using kvdro::fail;
+using kvdro::is_device_ptr;
+using kvdro::NvtxRange;
 using kvdro::Prec;
+using kvdro::release;
 
 namespace {
 
@@ -41,119 +45,6 @@ constexpr int32_t kMaxNLf64 = 128;
 // Host outputs of a grid over several regimes return in up to this many regime blocks, each
 // copied while the next evaluates.
 constexpr int64_t kCopyBlocks = 16;
-
-struct Buf {
-    void* p = nullptr;
-    size_t bytes = 0;
-};
-
-}  // namespace
-
-struct kvdro_ctx {
-    int device = 0;
-    int sms = 0;  // of the device
-    std::string err;
-    int fail_after = -1;  // test hook: the fail_after-th allocation of this context fails
-    int skip_chunk = -1;  // test hook: grid kernels never copy this chunk, so their waits run out
-    int allocs = 0;
-    cudaStream_t last_stream = nullptr;
-
-    bool loaded = false;
-    bool quads = false;  // the staged form of the loaded samples
-    int32_t K = 0;
-    int64_t total = 0, pair_total = 0, hist_total = 0;
-    std::vector<int64_t> off, pair_off, hist_off, N;
-    std::vector<int32_t> L, Lin, hist_blocks, exp_blocks;
-    std::vector<double> inv_n;
-
-    Buf sorted, pairs, hist, cum, csum, sumx, meta, errs, in_stage, grid_in, keys, cost64, out_stage, ranks, scan_tot,
-        tile_lo;
-    void* pin = nullptr;  // pinned host staging
-    size_t pin_bytes = 0;
-    void* land = nullptr;  // pinned: small results and the status words land here on their way to the caller
-    cudaEvent_t pin_free = nullptr;  // completes when the last copy out of `pin` is done
-    cudaEvent_t grid_t0 = nullptr, grid_t1 = nullptr;  // around the last grid-kernel launches
-    // Copies of host outputs back to the caller, overlapped with later grid launches
-    cudaStream_t copy_stream = nullptr;
-    cudaEvent_t copy_ready = nullptr, copy_done = nullptr;
-    bool grid_timed = false;
-
-    // device views into `meta`
-    int64_t *d_off = nullptr, *d_pair_off = nullptr, *d_hist_off = nullptr, *d_N = nullptr;
-    double* d_inv_n = nullptr;
-    int32_t* d_cum = nullptr;  // cumulative counts
-    int32_t *d_L = nullptr, *d_Lin = nullptr, *d_hist_blocks = nullptr, *d_exp_blocks = nullptr;
-};
-
-namespace {
-
-int fail(kvdro_ctx* c, int code, const char* fmt, ...) {
-    if (c) {
-        char buf[512];
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(buf, sizeof(buf), fmt, ap);
-        va_end(ap);
-        c->err = buf;
-    }
-    return code;
-}
-
-int cuda_fail(kvdro_ctx* c, cudaError_t e, const char* what) {
-    return fail(c, KVDRO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
-#define KV_CUDA(call, what)                            \
-    do {                                               \
-        cudaError_t e_ = (call);                       \
-        if (e_ != cudaSuccess) return cuda_fail(ctx, e_, what); \
-    } while (0)
-
-// An NVTX range around one entry point (visible in Nsight timelines; a no-op without a tool).
-struct NvtxRange {
-    explicit NvtxRange(const char* name) { nvtxRangePushA(name); }
-    ~NvtxRange() { nvtxRangePop(); }
-};
-
-// Keeps the caller's current device and restores it on exit.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
-
-int ensure(kvdro_ctx* ctx, Buf& b, size_t bytes) {
-    if (bytes == 0) bytes = 16;
-    if (b.bytes >= bytes) return KVDRO_OK;
-    if (b.p) {
-        cudaFree(b.p);
-        b.p = nullptr;
-        b.bytes = 0;
-    }
-    ctx->allocs++;
-    if (ctx->fail_after > 0 && ctx->allocs == ctx->fail_after)
-        return fail(ctx, KVDRO_ENOMEM, "device allocation of %zu bytes failed (injected by KVDRO_TEST_FAIL_ALLOC)", bytes);
-    cudaError_t e = cudaMalloc(&b.p, bytes);
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        b.p = nullptr;
-        return fail(ctx, KVDRO_ENOMEM, "cudaMalloc(%zu): %s", bytes, cudaGetErrorString(e));
-    }
-    b.bytes = bytes;
-    return KVDRO_OK;
-}
-
-void release(Buf& b) {
-    if (b.p) cudaFree(b.p);
-    b.p = nullptr;
-    b.bytes = 0;
-}
 
 // Pinned staging for small host->device uploads; waits for the previous upload first.
 int pinned(kvdro_ctx* ctx, size_t bytes, void** out) {
@@ -204,19 +95,6 @@ struct Params {
         return KVDRO_OK;
     }
 };
-
-// Device-accessible (device or managed memory) versus host memory (pinned or pageable).
-bool is_device_ptr(const void* p) {
-    cudaPointerAttributes at;
-    cudaError_t e = cudaPointerGetAttributes(&at, p);
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged;
-}
-
-size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Device results read back to the host: up to kLandBytes at a time in one copy, with the kernels' status words
 // behind them, and one wait.  (A copy into pageable memory for each output, a wait and another copy and wait
@@ -332,8 +210,9 @@ int kvdro_destroy(kvdro_ctx* ctx) {
     if (ctx->last_stream) cudaStreamSynchronize(ctx->last_stream);
     cudaDeviceSynchronize();
     for (Buf* b : {&ctx->sorted, &ctx->scan_tot, &ctx->pairs, &ctx->hist, &ctx->cum, &ctx->csum, &ctx->sumx, &ctx->meta, &ctx->errs, &ctx->in_stage,
-                   &ctx->grid_in, &ctx->keys, &ctx->cost64, &ctx->out_stage, &ctx->ranks, &ctx->tile_lo})
+                   &ctx->grid_in, &ctx->keys, &ctx->cost64, &ctx->out_stage, &ctx->ranks, &ctx->tile_lo, &ctx->kv_err})
         release(*b);
+    while (ctx->caches) kvdro_kv_close(ctx->caches);
     if (ctx->pin) cudaFreeHost(ctx->pin);
     if (ctx->land) cudaFreeHost(ctx->land);
     if (ctx->pin_free) cudaEventDestroy(ctx->pin_free);
@@ -929,7 +808,8 @@ int kvdro_sync(kvdro_ctx* ctx) {
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
     KV_CUDA(cudaStreamSynchronize(ctx->last_stream), "synchronising");
     KV_CUDA(cudaGetLastError(), "asynchronous error");
-    return check_kernel_errors(ctx, ctx->last_stream);
+    if (int rc = check_kernel_errors(ctx, ctx->last_stream)) return rc;
+    return kvdro::check_kv_errors(ctx);
 }
 
 }  // extern "C"

@@ -1,0 +1,50 @@
+// Internal declarations of the page cache: the handle's description and the kernels' arguments.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace kvdro {
+
+// Error bits that page cache kernels report in ctx->kv_err.
+constexpr int kKvErrRange = 1;
+constexpr int kKvErrTimeout = 2;
+
+constexpr int kKvMaxRequests = 16384;
+
+struct PlanArgs {
+    int32_t page_shift, n_pages, B, max_pages, T;
+    const int32_t *cached, *new_len, *reserve, *held, *pool;
+    int32_t *table, *ring, *held_out, *pool_out, *q_off, *kv_len, *slot, *pos;
+    int32_t* err;
+};
+cudaError_t kv_plan_prepare();
+cudaError_t launch_kv_plan(const PlanArgs& a, int sms, cudaStream_t s);
+
+struct AppendArgs {
+    const uint4 *k, *v;                      // caller's rows, in 16-byte units like every stride below
+    uint4 *kc, *vc;                          // the cache
+    int64_t k_tok, k_head, v_tok, v_head;
+    int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+    const int32_t* slot;
+    int32_t T, n_slots, page_shift, heads, vec_shift;  // 16-byte vectors of a head: 1 << vec_shift
+    int32_t* err;
+};
+cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
+
+struct AttendArgs {
+    const uint16_t *q, *k, *v;
+    uint16_t* out;
+    float* lse;
+    int64_t q_tok, q_head, out_tok, out_head;  // in elements
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
+    const int32_t *q_off, *kv_len, *table;
+    int32_t B, T, heads, group, head_dim, n_pages, page_shift, max_pages, window;
+    bool half, causal;
+    float scale, cap;  // cap 0: none
+    int32_t* err;
+};
+cudaError_t launch_kv_attend(const AttendArgs& a, cudaStream_t s);
+
+}  // namespace kvdro

@@ -1,0 +1,291 @@
+// C ABI of the page cache (declared in include/kvdro.h): argument validation and launches.
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <initializer_list>
+#include <new>
+
+#include "context.cuh"
+#include "kv.cuh"
+
+using kvdro::cuda_fail;
+using kvdro::DeviceGuard;
+using kvdro::ensure;
+using kvdro::fail;
+using kvdro::is_device_ptr;
+using kvdro::NvtxRange;
+
+namespace {
+
+constexpr int64_t kMaxStride = (int64_t)1 << 39;  // elements: what a tensor map's 40 bits of bytes hold
+constexpr int32_t kMaxTokens = 1 << 30;
+constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
+
+int log2_of(int32_t v) {
+    int s = 0;
+    while ((1 << s) < v) s++;
+    return s;
+}
+
+int check_pages(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages) {
+    if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128)
+        return fail(ctx, KVDRO_EINVAL, "page_size = %d is not 16, 32, 64 or 128", page_size);
+    if (n_pages < 1 || (int64_t)n_pages * page_size > 0x7fffffffLL)
+        return fail(ctx, KVDRO_EINVAL, "n_pages = %d: n_pages * page_size outside [page_size, 2^31)", n_pages);
+    return KVDRO_OK;
+}
+
+int check_requests(kvdro_ctx* ctx, int32_t B, int32_t T, int32_t max_pages, int32_t page_size) {
+    if (B < 1 || B > kvdro::kKvMaxRequests) return fail(ctx, KVDRO_EINVAL, "B = %d outside [1, %d]", B, kvdro::kKvMaxRequests);
+    if (T < 0 || T > kMaxTokens) return fail(ctx, KVDRO_EINVAL, "T = %d outside [0, 2^30]", T);
+    if (max_pages < 1 || (int64_t)max_pages * page_size > 0x7fffffffLL)
+        return fail(ctx, KVDRO_EINVAL, "max_pages = %d: max_pages * page_size outside [page_size, 2^31)", max_pages);
+    return KVDRO_OK;
+}
+
+struct Arg {
+    const char* name;
+    const void* p;
+};
+
+int check_device(kvdro_ctx* ctx, std::initializer_list<Arg> args) {
+    for (const Arg& x : args) {
+        if (!x.p) return fail(ctx, KVDRO_EINVAL, "%s is required", x.name);
+        if (!is_device_ptr(x.p)) return fail(ctx, KVDRO_EINVAL, "%s must be device memory", x.name);
+    }
+    return KVDRO_OK;
+}
+
+// Strides of rows of 16-byte vectors: `n` of them into `out`, from the caller's or the contiguous ones.
+int rows(kvdro_ctx* ctx, const char* name, const void* p, const int64_t* stride, int n, const int64_t* dense, int64_t* out) {
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(ctx, KVDRO_EINVAL, "%s is not 16-byte aligned", name);
+    for (int i = 0; i < n; i++) {
+        out[i] = stride ? stride[i] : dense[i];
+        if (out[i] < 1 || out[i] >= kMaxStride || out[i] % 8)
+            return fail(ctx, KVDRO_EINVAL, "%s: stride %lld is not a positive multiple of 8 elements below 2^39", name,
+                        (long long)out[i]);
+    }
+    return KVDRO_OK;
+}
+
+// The word in which page cache kernels report what they met.
+int error_word(kvdro_ctx* ctx) {
+    if (ctx->kv_err.p) return KVDRO_OK;
+    if (int rc = ensure(ctx, ctx->kv_err, 16)) return rc;
+    KV_CUDA(cudaMemset(ctx->kv_err.p, 0, 16), "clearing status");
+    return KVDRO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
+                  int32_t head_dim, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride) {
+    NvtxRange nvtx_("kvdro_kv_open");
+    if (out) *out = nullptr;
+    if (!ctx) return KVDRO_EINVAL;
+    ctx->err.clear();
+    if (!out) return fail(ctx, KVDRO_EINVAL, "out is required");
+    if (dtype != KVDRO_BF16 && dtype != KVDRO_FP16) return fail(ctx, KVDRO_EINVAL, "dtype must be KVDRO_BF16 or KVDRO_FP16");
+    if (int rc = check_pages(ctx, page_size, n_pages)) return rc;
+    if (n_kv_heads < 1 || n_kv_heads > kMaxKvHeads)
+        return fail(ctx, KVDRO_EINVAL, "n_kv_heads = %d outside [1, %d]", n_kv_heads, kMaxKvHeads);
+    if (head_dim != 64 && head_dim != 128) return fail(ctx, KVDRO_EINVAL, "head_dim = %d is not 64 or 128", head_dim);
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    if (int rc = check_device(ctx, {{"k", k}, {"v", v}})) return rc;
+    const int64_t row = (int64_t)n_kv_heads * head_dim, dense[3] = {page_size * row, row, head_dim};
+    kvdro_kv c;
+    if (int rc = rows(ctx, "k", k, k_stride, 3, dense, c.k_stride)) return rc;
+    if (int rc = rows(ctx, "v", v, v_stride, 3, dense, c.v_stride)) return rc;
+    if (int rc = error_word(ctx)) return rc;
+    c.ctx = ctx;
+    c.half = dtype == KVDRO_FP16;
+    c.n_pages = n_pages;
+    c.page_size = page_size;
+    c.page_shift = log2_of(page_size);
+    c.heads = n_kv_heads;
+    c.head_dim = head_dim;
+    c.k = k;
+    c.v = v;
+    kvdro_kv* kv = new (std::nothrow) kvdro_kv(c);
+    if (!kv) return fail(ctx, KVDRO_ENOMEM, "no memory for the handle");
+    kv->next = ctx->caches;
+    if (kv->next) kv->next->prev = kv;
+    ctx->caches = kv;
+    *out = kv;
+    return KVDRO_OK;
+}
+
+int kvdro_kv_close(kvdro_kv* kv) {
+    if (!kv) return KVDRO_OK;
+    if (kv->prev) kv->prev->next = kv->next;
+    else kv->ctx->caches = kv->next;
+    if (kv->next) kv->next->prev = kv->prev;
+    delete kv;
+    return KVDRO_OK;
+}
+
+int kvdro_kv_plan(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages, int32_t B, int32_t max_pages, int32_t T,
+                  const int32_t* cached, const int32_t* new_len, const int32_t* reserve, const int32_t* held,
+                  int32_t* table, int32_t* ring, const int32_t* pool, int32_t* held_out, int32_t* pool_out,
+                  int32_t* q_off, int32_t* kv_len, int32_t* slot, int32_t* pos, void* stream) {
+    NvtxRange nvtx_("kvdro_kv_plan");
+    if (!ctx) return KVDRO_EINVAL;
+    ctx->err.clear();
+    if (int rc = check_pages(ctx, page_size, n_pages)) return rc;
+    if (int rc = check_requests(ctx, B, T, max_pages, page_size)) return rc;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    if (int rc = check_device(ctx, {{"cached", cached}, {"new_len", new_len}, {"held", held}, {"table", table}, {"ring", ring},
+                                    {"pool", pool}, {"held_out", held_out}, {"pool_out", pool_out}, {"q_off", q_off},
+                                    {"kv_len", kv_len}}))
+        return rc;
+    if (reserve)
+        if (int rc = check_device(ctx, {{"reserve", reserve}})) return rc;
+    if (T > 0)
+        if (int rc = check_device(ctx, {{"slot", slot}})) return rc;
+    if (T > 0 && pos)
+        if (int rc = check_device(ctx, {{"pos", pos}})) return rc;
+    if (held_out < held + B && held < held_out + B) return fail(ctx, KVDRO_EINVAL, "held_out overlaps held");
+    if (pool_out < pool + 2 && pool < pool_out + 2) return fail(ctx, KVDRO_EINVAL, "pool_out overlaps pool");
+    if (!ctx->kv_plan_ready) {
+        KV_CUDA(kvdro::kv_plan_prepare(), "preparing the plan kernel");
+        ctx->kv_plan_ready = true;
+    }
+    if (int rc = error_word(ctx)) return rc;
+    kvdro::PlanArgs a{log2_of(page_size), n_pages, B, max_pages, T, cached, new_len, reserve, held, pool, table, ring, held_out,
+                      pool_out, q_off, kv_len, slot, pos, static_cast<int32_t*>(ctx->kv_err.p)};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ctx->last_stream = s;
+    KV_CUDA(kvdro::launch_kv_plan(a, ctx->sms, s), "plan kernel");
+    return KVDRO_OK;
+}
+
+int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_stride, const void* v,
+                    const int64_t* v_stride, const int32_t* slot, void* stream) {
+    NvtxRange nvtx_("kvdro_kv_append");
+    if (!kv) return KVDRO_EINVAL;
+    kvdro_ctx* ctx = kv->ctx;
+    ctx->err.clear();
+    if (T < 0 || T > kMaxTokens) return fail(ctx, KVDRO_EINVAL, "T = %d outside [0, 2^30]", T);
+    if (T == 0) return KVDRO_OK;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    if (int rc = check_device(ctx, {{"k", k}, {"v", v}, {"slot", slot}})) return rc;
+    const int64_t dense[2] = {(int64_t)kv->heads * kv->head_dim, kv->head_dim};
+    int64_t ks[2], vs[2];
+    if (int rc = rows(ctx, "k", k, k_stride, 2, dense, ks)) return rc;
+    if (int rc = rows(ctx, "v", v, v_stride, 2, dense, vs)) return rc;
+    kvdro::AppendArgs a;
+    a.k = static_cast<const uint4*>(k);
+    a.v = static_cast<const uint4*>(v);
+    a.kc = static_cast<uint4*>(kv->k);
+    a.vc = static_cast<uint4*>(kv->v);
+    a.k_tok = ks[0] / 8;
+    a.k_head = ks[1] / 8;
+    a.v_tok = vs[0] / 8;
+    a.v_head = vs[1] / 8;
+    a.kc_page = kv->k_stride[0] / 8;
+    a.kc_slot = kv->k_stride[1] / 8;
+    a.kc_head = kv->k_stride[2] / 8;
+    a.vc_page = kv->v_stride[0] / 8;
+    a.vc_slot = kv->v_stride[1] / 8;
+    a.vc_head = kv->v_stride[2] / 8;
+    a.slot = slot;
+    a.T = T;
+    a.n_slots = kv->n_pages << kv->page_shift;
+    a.page_shift = kv->page_shift;
+    a.heads = kv->heads;
+    a.vec_shift = log2_of(kv->head_dim / 8);
+    a.err = static_cast<int32_t*>(ctx->kv_err.p);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ctx->last_stream = s;
+    KV_CUDA(kvdro::launch_kv_append(a, s), "append kernel");
+    return KVDRO_OK;
+}
+
+int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,
+                    const int64_t* q_stride, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                    int32_t max_pages, double scale, int causal, int32_t window, double softcap, void* out,
+                    const int64_t* out_stride, float* lse, void* stream) {
+    NvtxRange nvtx_("kvdro_kv_attend");
+    if (!kv) return KVDRO_EINVAL;
+    kvdro_ctx* ctx = kv->ctx;
+    ctx->err.clear();
+    if (int rc = check_requests(ctx, B, T, max_pages, kv->page_size)) return rc;
+    if (n_heads < 1 || n_heads > kMaxHeads || n_heads % kv->heads)
+        return fail(ctx, KVDRO_EINVAL, "n_heads = %d is not a multiple of n_kv_heads = %d up to %d", n_heads, kv->heads, kMaxHeads);
+    if (max_q < 0) return fail(ctx, KVDRO_EINVAL, "max_q = %d is negative", max_q);
+    if (!std::isfinite((float)scale)) return fail(ctx, KVDRO_EINVAL, "scale = %g is not finite", scale);
+    if (!std::isfinite((float)softcap) || softcap < 0.0 || (softcap > 0.0 && (float)softcap < 1e-30f))
+        return fail(ctx, KVDRO_EINVAL, "softcap = %g is neither 0 nor finite and at least 1e-30", softcap);
+    if (causal != 0 && causal != 1) return fail(ctx, KVDRO_EINVAL, "causal must be 0 or 1");
+    if (window < 0 || (window > 0 && !causal)) return fail(ctx, KVDRO_EINVAL, "window = %d: not negative, and with causal only", window);
+    if (T == 0) return KVDRO_OK;
+    if ((int64_t)T * n_heads > 0x7fffffffLL * 4) return fail(ctx, KVDRO_EINVAL, "T * n_heads is too large");
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    if (int rc = check_device(ctx, {{"q", q}, {"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"out", out}})) return rc;
+    if (lse)
+        if (int rc = check_device(ctx, {{"lse", lse}})) return rc;
+    const int64_t dense[2] = {(int64_t)n_heads * kv->head_dim, kv->head_dim};
+    int64_t qs[2], os[2];
+    if (int rc = rows(ctx, "q", q, q_stride, 2, dense, qs)) return rc;
+    if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
+    kvdro::AttendArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(kv->k);
+    a.v = static_cast<const uint16_t*>(kv->v);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    a.q_tok = qs[0];
+    a.q_head = qs[1];
+    a.out_tok = os[0];
+    a.out_head = os[1];
+    a.k_page = kv->k_stride[0];
+    a.k_slot = kv->k_stride[1];
+    a.k_head = kv->k_stride[2];
+    a.v_page = kv->v_stride[0];
+    a.v_slot = kv->v_stride[1];
+    a.v_head = kv->v_stride[2];
+    a.q_off = q_off;
+    a.kv_len = kv_len;
+    a.table = table;
+    a.B = B;
+    a.T = T;
+    a.heads = n_heads;
+    a.group = n_heads / kv->heads;
+    a.head_dim = kv->head_dim;
+    a.n_pages = kv->n_pages;
+    a.page_shift = kv->page_shift;
+    a.max_pages = max_pages;
+    a.window = window;
+    a.half = kv->half;
+    a.causal = causal != 0;
+    a.scale = (float)scale;
+    a.cap = (float)softcap;
+    a.err = static_cast<int32_t*>(ctx->kv_err.p);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ctx->last_stream = s;
+    KV_CUDA(kvdro::launch_kv_attend(a, s), "attention kernel");
+    return KVDRO_OK;
+}
+
+}  // extern "C"
+
+namespace kvdro {
+
+// What the page cache's kernels reported, cleared.  The stream has been waited for.
+int check_kv_errors(kvdro_ctx* ctx) {
+    if (!ctx->kv_err.p) return KVDRO_OK;
+    int32_t bits = 0;
+    KV_CUDA(cudaMemcpy(&bits, ctx->kv_err.p, sizeof(bits), cudaMemcpyDeviceToHost), "reading kernel status");
+    if (!bits) return KVDRO_OK;
+    KV_CUDA(cudaMemset(ctx->kv_err.p, 0, sizeof(bits)), "clearing status");
+    if (bits & kKvErrTimeout) return fail(ctx, KVDRO_ETIMEOUT, "an attention kernel gave up a bounded wait");
+    return fail(ctx, KVDRO_ERANGE, "a page cache kernel met a page number, slot or length outside its range");
+}
+
+}  // namespace kvdro

@@ -17,6 +17,7 @@ from __future__ import annotations
 import ctypes
 import os
 import threading
+import weakref
 from typing import Any
 
 import numpy as np
@@ -29,17 +30,21 @@ KVDRO_ENOMEM = -2
 KVDRO_ECUDA = -3
 KVDRO_ESTATE = -4
 KVDRO_ETIMEOUT = -5
+KVDRO_ERANGE = -6
 KVDRO_FP32 = 0
 KVDRO_FP64 = 1
 KVDRO_EXACT = 2
 KVDRO_ENVELOPE = 3
+KVDRO_BF16 = 0
+KVDRO_FP16 = 1
 
 _STATUS = {0: "KVDRO_OK", -1: "KVDRO_EINVAL", -2: "KVDRO_ENOMEM", -3: "KVDRO_ECUDA", -4: "KVDRO_ESTATE",
-           -5: "KVDRO_ETIMEOUT"}
+           -5: "KVDRO_ETIMEOUT", -6: "KVDRO_ERANGE"}
 
 # Every entry point declared in include/kvdro.h.
 SYMBOLS = ("kvdro_create", "kvdro_load_samples", "kvdro_quantiles", "kvdro_eval_grid", "kvdro_sorted_samples",
-           "kvdro_eval_dual", "kvdro_last_grid_ms", "kvdro_eval_grid_noalloc", "kvdro_sync", "kvdro_last_error", "kvdro_destroy")
+           "kvdro_eval_dual", "kvdro_last_grid_ms", "kvdro_eval_grid_noalloc", "kvdro_kv_open", "kvdro_kv_close",
+           "kvdro_kv_plan", "kvdro_kv_append", "kvdro_kv_attend", "kvdro_sync", "kvdro_last_error", "kvdro_destroy")
 
 _lock = threading.Lock()
 _lib = None
@@ -87,6 +92,17 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.kvdro_eval_grid_noalloc.restype = ctypes.c_int
         lib.kvdro_eval_grid_noalloc.argtypes = [i32, P, P, P, P, i32, P, i32, P, i32, P, i32, P, P, P, P, P, P, P, P,
                                                 ctypes.c_char_p, i32]
+        f64 = ctypes.c_double
+        lib.kvdro_kv_open.restype = ctypes.c_int
+        lib.kvdro_kv_open.argtypes = [P, ctypes.POINTER(P), ctypes.c_int, i32, i32, i32, i32, P, P, P, P]
+        lib.kvdro_kv_close.restype = ctypes.c_int
+        lib.kvdro_kv_close.argtypes = [P]
+        lib.kvdro_kv_plan.restype = ctypes.c_int
+        lib.kvdro_kv_plan.argtypes = [P, i32, i32, i32, i32, i32, P, P, P, P, P, P, P, P, P, P, P, P, P, P]
+        lib.kvdro_kv_append.restype = ctypes.c_int
+        lib.kvdro_kv_append.argtypes = [P, i32, P, P, P, P, P, P]
+        lib.kvdro_kv_attend.restype = ctypes.c_int
+        lib.kvdro_kv_attend.argtypes = [P, i32, i32, i32, i32, P, P, P, P, P, i32, f64, ctypes.c_int, i32, f64, P, P, P, P]
         lib.kvdro_sync.restype = ctypes.c_int
         lib.kvdro_sync.argtypes = [P]
         lib.kvdro_last_error.restype = ctypes.c_char_p
@@ -325,6 +341,144 @@ def kvdro_eval_grid_noalloc(K: int, offsets, lengths, L_max, L_in, R: int, r, NL
         raise KvdroError(st, buf.value.decode())
 
 
+# ------------------------------------------------------------------ page cache
+
+class KvdroKv:
+    """A handle of ``kvdro_kv_open`` and the tensors it describes, which it keeps alive."""
+
+    __slots__ = ("handle", "ctx", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
+
+
+def _dev(name: str, a: Any, dtype: str, n=None) -> int:
+    """Pointer of a contiguous CUDA tensor of this dtype (and of ``n`` elements)."""
+    if not getattr(a, "is_cuda", False):
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if not _kv_types:
+        _kv_setup()
+    if a.dtype is not _kv_types[dtype]:
+        raise TypeError(f"{name}: expected dtype {dtype}, got {a.dtype}")
+    if not a.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if n is not None and a.numel() != n:
+        raise ValueError(f"{name} has {a.numel()} elements; the call needs exactly {n}")
+    return a.data_ptr()
+
+
+_kv_types: dict = {}
+_caches: dict = {}  # handle of a context -> its open page caches, which kvdro_destroy closes
+_I2, _I3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
+def _kv_setup():
+    import torch
+    _kv_types.update({"int32": torch.int32, "float32": torch.float32, torch.bfloat16: KVDRO_BF16, torch.float16: KVDRO_FP16})
+
+
+def _heads(cache: KvdroKv, name: str, a: Any, T=None, heads=None):
+    """Pointer and strides (None if contiguous) of a CUDA tensor [T][heads][head_dim] of the cache's dtype."""
+    if not getattr(a, "is_cuda", False):
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if a.dtype is not cache.dtype:
+        raise TypeError(f"{name}: expected the cache's dtype {cache.dtype}, got {a.dtype}")
+    if a.dim() != 3 or a.shape[2] != cache.head_dim or (T is not None and a.shape[0] != T) or \
+            (heads is not None and a.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(a.shape)}; the call needs "
+                         f"({'T' if T is None else T}, {'heads' if heads is None else heads}, {cache.head_dim})")
+    if a.is_contiguous():
+        return a.data_ptr(), None
+    if a.stride(2) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    # a dimension of one element has no stride of its own: any that the library takes will do
+    tok, head = a.stride(0) if a.shape[0] > 1 else 8, a.stride(1) if a.shape[1] > 1 else 8
+    return a.data_ptr(), _I2(tok, head)
+
+
+def kvdro_kv_open(ctx, k, v) -> KvdroKv:
+    """Describe a page cache: ``k`` and ``v`` are CUDA tensors [n_pages][page_size][n_kv_heads][head_dim] of
+    bfloat16 or float16 whose last dimension is contiguous (other strides as they are)."""
+    if not _kv_types:
+        _kv_setup()
+    for name, a in (("k", k), ("v", v)):
+        _on_device(name, a)
+        if a.dtype not in _kv_types:
+            raise TypeError(f"{name}: expected bfloat16 or float16, got {a.dtype}")
+        if a.dim() != 4 or (a.shape[3] > 1 and a.stride(3) != 1):
+            raise ValueError(f"{name} must be [n_pages][page_size][n_kv_heads][head_dim] with a contiguous last dimension")
+    if k.shape != v.shape or k.dtype is not v.dtype:
+        raise ValueError("k and v differ in shape or dtype")
+    n, page, heads, d = k.shape
+    strides = [_I3(*(t.stride(i) if t.shape[i] > 1 else 8 for i in range(3))) for t in (k, v)]
+    h = ctypes.c_void_p()
+    _check(ctx, load_library().kvdro_kv_open(ctx, ctypes.byref(h), _kv_types[k.dtype], n, page, heads, d, k.data_ptr(),
+                                             strides[0], v.data_ptr(), strides[1]))
+    c = KvdroKv()
+    c.handle, c.ctx, c.k, c.v, c.dtype, c.heads, c.head_dim = h, ctx, k, v, k.dtype, heads, d
+    _caches.setdefault(getattr(ctx, "value", ctx), weakref.WeakSet()).add(c)
+    return c
+
+
+def kvdro_kv_close(cache: KvdroKv) -> None:
+    if cache.handle:
+        load_library().kvdro_kv_close(cache.handle)
+        cache.handle = None
+        cache.k = cache.v = None
+
+
+def kvdro_kv_plan(ctx, page_size: int, cached, new_len, held, table, ring, pool, held_out, pool_out, q_off, kv_len,
+                  slot, pos=None, reserve=None, stream=None) -> None:
+    """Pages and slots of one step (include/kvdro.h): int32 CUDA tensors; ``table`` is [B][max_pages], ``ring`` holds
+    one element per page and ``slot`` one per new token."""
+    if getattr(table, "ndim", 0) != 2:
+        raise ValueError("table must be [B][max_pages]")
+    B, max_pages = table.shape
+    T = _numel(slot)
+    p = [_dev("cached", cached, "int32", B), _dev("new_len", new_len, "int32", B),
+         None if reserve is None else _dev("reserve", reserve, "int32", B), _dev("held", held, "int32", B),
+         _dev("table", table, "int32"), _dev("ring", ring, "int32"), _dev("pool", pool, "int32", 2),
+         _dev("held_out", held_out, "int32", B), _dev("pool_out", pool_out, "int32", 2),
+         _dev("q_off", q_off, "int32", B + 1), _dev("kv_len", kv_len, "int32", B), _dev("slot", slot, "int32"),
+         None if pos is None else _dev("pos", pos, "int32", T)]
+    st = load_library().kvdro_kv_plan(ctx, page_size, ring.numel(), B, max_pages, T, *p, _stream(stream))
+    if st:
+        _check(ctx, st)
+
+
+def _open_handle(cache: KvdroKv):
+    if not cache.handle:
+        raise ValueError("the page cache is closed")
+    return cache.handle
+
+
+def kvdro_kv_append(cache: KvdroKv, k, v, slot, stream=None) -> None:
+    """Write the new tokens' keys and values, [T][n_kv_heads][head_dim] (last dimension contiguous), into their slots."""
+    kp, ks = _heads(cache, "k", k, None, cache.heads)
+    T = k.shape[0]
+    vp, vs = _heads(cache, "v", v, T, cache.heads)
+    st = load_library().kvdro_kv_append(_open_handle(cache), T, kp, ks, vp, vs, _dev("slot", slot, "int32", T),
+                                        _stream(stream))
+    if st:
+        _check(cache.ctx, st)
+
+
+def kvdro_kv_attend(cache: KvdroKv, q, q_off, kv_len, table, out, lse=None, scale=None, causal: bool = True,
+                    window: int = 0, softcap: float = 0.0, max_q: int = 0, stream=None) -> None:
+    """Attention of the new tokens ``q`` [T][n_heads][head_dim] over their requests' pages into ``out`` (and ``lse``
+    [T][n_heads] float32); ``scale`` defaults to head_dim ** -0.5."""
+    qp, qs = _heads(cache, "q", q)
+    T, heads, d = q.shape
+    op, os_ = _heads(cache, "out", out, T, heads)
+    if getattr(table, "ndim", 0) != 2:
+        raise ValueError("table must be [B][max_pages]")
+    B, max_pages = table.shape
+    st = load_library().kvdro_kv_attend(
+        _open_handle(cache), B, T, heads, max_q, qp, qs, _dev("q_off", q_off, "int32", B + 1),
+        _dev("kv_len", kv_len, "int32", B), _dev("table", table, "int32"), max_pages,
+        d ** -0.5 if scale is None else scale, 1 if causal else 0, window, softcap, op, os_,
+        None if lse is None else _dev("lse", lse, "float32", T * heads), _stream(stream))
+    if st:
+        _check(cache.ctx, st)
+
+
 def kvdro_sync(ctx) -> None:
     _check(ctx, load_library().kvdro_sync(ctx))
 
@@ -336,4 +490,6 @@ def kvdro_last_error(ctx) -> str:
 def kvdro_destroy(ctx) -> None:
     if ctx:
         _loaded.pop(getattr(ctx, "value", ctx), None)
+        for cache in list(_caches.pop(getattr(ctx, "value", ctx), ())):
+            kvdro_kv_close(cache)
         load_library().kvdro_destroy(ctx)
