@@ -210,7 +210,8 @@ int kvdro_destroy(kvdro_ctx* ctx) {
     if (ctx->last_stream) cudaStreamSynchronize(ctx->last_stream);
     cudaDeviceSynchronize();
     for (Buf* b : {&ctx->sorted, &ctx->scan_tot, &ctx->pairs, &ctx->hist, &ctx->cum, &ctx->csum, &ctx->sumx, &ctx->meta, &ctx->errs, &ctx->in_stage,
-                   &ctx->grid_in, &ctx->keys, &ctx->cost64, &ctx->out_stage, &ctx->ranks, &ctx->tile_lo, &ctx->kv_err})
+                   &ctx->grid_in, &ctx->keys, &ctx->cost64, &ctx->out_stage, &ctx->ranks, &ctx->tile_lo, &ctx->kv_err,
+                   &ctx->kv_pieces, &ctx->kv_tickets})
         release(*b);
     while (ctx->caches) kvdro_kv_close(ctx->caches);
     if (ctx->pin) cudaFreeHost(ctx->pin);
@@ -220,6 +221,7 @@ int kvdro_destroy(kvdro_ctx* ctx) {
     if (ctx->grid_t1) cudaEventDestroy(ctx->grid_t1);
     if (ctx->copy_ready) cudaEventDestroy(ctx->copy_ready);
     if (ctx->copy_done) cudaEventDestroy(ctx->copy_done);
+    if (ctx->kv_done) cudaEventDestroy(ctx->kv_done);
     if (ctx->copy_stream) cudaStreamDestroy(ctx->copy_stream);
     cudaGetLastError();
     delete ctx;

@@ -11,6 +11,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "kvdro.h"
+#include "kv.cuh"
 #include "kvdro_internal.cuh"
 
 namespace kvdro {
@@ -60,7 +61,11 @@ struct kvdro_ctx {
     // The page cache
     kvdro_kv* caches = nullptr;  // open handles
     kvdro::Buf kv_err;           // the word in which its kernels report what they met
-    bool kv_plan_ready = false;
+    kvdro::Buf kv_pieces, kv_tickets;  // scratch of the attention kernels
+    cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it
+    cudaStream_t kv_stream = nullptr;  // that call's stream
+    bool kv_used = false;
+    bool kv_plan_ready = false, kv_ready = false;
 };
 
 // A page cache that the caller owns.
@@ -71,6 +76,7 @@ struct kvdro_kv {
     int32_t n_pages = 0, page_size = 0, page_shift = 0, heads = 0, head_dim = 0;
     void *k = nullptr, *v = nullptr;
     int64_t k_stride[3] = {}, v_stride[3] = {};  // page, slot, head; in elements
+    kvdro::KvMaps maps;
 };
 
 namespace kvdro {

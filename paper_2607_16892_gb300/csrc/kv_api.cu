@@ -1,12 +1,12 @@
 // C ABI of the page cache (declared in include/kvdro.h): argument validation and launches.
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 
 #include <cmath>
 #include <initializer_list>
 #include <new>
 
 #include "context.cuh"
-#include "kv.cuh"
 
 using kvdro::cuda_fail;
 using kvdro::DeviceGuard;
@@ -68,6 +68,41 @@ int rows(kvdro_ctx* ctx, const char* name, const void* p, const int64_t* stride,
     return KVDRO_OK;
 }
 
+// A tensor map of k or v for boxes of 64 elements by `slots` slots of one head and page, rows of 128 bytes permuted
+// (128-byte swizzle) so that matrix loads meet no bank conflict.
+int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const int64_t* stride, int slots) {
+    static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+    }();
+    if (!fn) return fail(ctx, KVDRO_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages};
+    const cuuint64_t bytes[3] = {(cuuint64_t)stride[1] * 2, (cuuint64_t)stride[2] * 2, (cuuint64_t)stride[0] * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = fn(map, c.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, p, dims, bytes, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(ctx, KVDRO_EINVAL, "these sizes and strides make no tensor map (driver error %d)", (int)r);
+    return KVDRO_OK;
+}
+
+// What the attention kernels need once per context: attributes, scratch.
+int prepare_attend(kvdro_ctx* ctx) {
+    if (ctx->kv_ready) return KVDRO_OK;
+    KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
+    if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
+    if (int rc = ensure(ctx, ctx->kv_pieces, kvdro::kv_decode_piece_bytes(ctx->sms))) return rc;
+    const size_t tickets = 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);
+    if (int rc = ensure(ctx, ctx->kv_tickets, tickets)) return rc;
+    KV_CUDA(cudaMemset(ctx->kv_tickets.p, 0, tickets), "clearing scratch");
+    ctx->kv_ready = true;
+    return KVDRO_OK;
+}
+
 // The word in which page cache kernels report what they met.
 int error_word(kvdro_ctx* ctx) {
     if (ctx->kv_err.p) return KVDRO_OK;
@@ -100,6 +135,7 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     if (int rc = rows(ctx, "k", k, k_stride, 3, dense, c.k_stride)) return rc;
     if (int rc = rows(ctx, "v", v, v_stride, 3, dense, c.v_stride)) return rc;
     if (int rc = error_word(ctx)) return rc;
+    if (int rc = prepare_attend(ctx)) return rc;
     c.ctx = ctx;
     c.half = dtype == KVDRO_FP16;
     c.n_pages = n_pages;
@@ -109,6 +145,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     c.head_dim = head_dim;
     c.k = k;
     c.v = v;
+    if (int rc = encode(ctx, &c.maps.k16, c, k, c.k_stride, 16)) return rc;
+    if (int rc = encode(ctx, &c.maps.v16, c, v, c.v_stride, 16)) return rc;
     kvdro_kv* kv = new (std::nothrow) kvdro_kv(c);
     if (!kv) return fail(ctx, KVDRO_ENOMEM, "no memory for the handle");
     kv->next = ctx->caches;
@@ -224,7 +262,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     if (causal != 0 && causal != 1) return fail(ctx, KVDRO_EINVAL, "causal must be 0 or 1");
     if (window < 0 || (window > 0 && !causal)) return fail(ctx, KVDRO_EINVAL, "window = %d: not negative, and with causal only", window);
     if (T == 0) return KVDRO_OK;
-    if ((int64_t)T * n_heads > 0x7fffffffLL * 4) return fail(ctx, KVDRO_EINVAL, "T * n_heads is too large");
+    if ((int64_t)T * n_heads > 0x7fffffffLL) return fail(ctx, KVDRO_EINVAL, "T * n_heads = %lld passes 2^31 - 1", (long long)T * n_heads);
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
     if (int rc = check_device(ctx, {{"q", q}, {"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"out", out}})) return rc;
@@ -236,26 +274,19 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
     kvdro::AttendArgs a;
     a.q = static_cast<const uint16_t*>(q);
-    a.k = static_cast<const uint16_t*>(kv->k);
-    a.v = static_cast<const uint16_t*>(kv->v);
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     a.q_tok = qs[0];
     a.q_head = qs[1];
     a.out_tok = os[0];
     a.out_head = os[1];
-    a.k_page = kv->k_stride[0];
-    a.k_slot = kv->k_stride[1];
-    a.k_head = kv->k_stride[2];
-    a.v_page = kv->v_stride[0];
-    a.v_slot = kv->v_stride[1];
-    a.v_head = kv->v_stride[2];
     a.q_off = q_off;
     a.kv_len = kv_len;
     a.table = table;
     a.B = B;
     a.T = T;
     a.heads = n_heads;
+    a.kv_heads = kv->heads;
     a.group = n_heads / kv->heads;
     a.head_dim = kv->head_dim;
     a.n_pages = kv->n_pages;
@@ -266,10 +297,22 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.causal = causal != 0;
     a.scale = (float)scale;
     a.cap = (float)softcap;
+    a.pieces = static_cast<float*>(ctx->kv_pieces.p);
+    a.tickets = static_cast<unsigned*>(ctx->kv_tickets.p);
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->last_stream = s;
-    KV_CUDA(kvdro::launch_kv_attend(a, s), "attention kernel");
+    // Calls share the scratch: one on another stream than the last waits for that one.
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
+    const bool captured = capture != cudaStreamCaptureStatusNone;
+    if (!captured && ctx->kv_used && ctx->kv_stream != s) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
+    KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, ctx->sms, s), "attention kernel");
+    if (!captured) {
+        KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
+        ctx->kv_stream = s;
+        ctx->kv_used = true;
+    }
     return KVDRO_OK;
 }
 
@@ -284,7 +327,10 @@ int check_kv_errors(kvdro_ctx* ctx) {
     KV_CUDA(cudaMemcpy(&bits, ctx->kv_err.p, sizeof(bits), cudaMemcpyDeviceToHost), "reading kernel status");
     if (!bits) return KVDRO_OK;
     KV_CUDA(cudaMemset(ctx->kv_err.p, 0, sizeof(bits)), "clearing status");
-    if (bits & kKvErrTimeout) return fail(ctx, KVDRO_ETIMEOUT, "an attention kernel gave up a bounded wait");
+    if (bits & kKvErrTimeout) {  // arrivals may be missing
+        KV_CUDA(cudaMemset(ctx->kv_tickets.p, 0, ctx->kv_tickets.bytes), "clearing scratch");
+        return fail(ctx, KVDRO_ETIMEOUT, "an attention kernel gave up a bounded wait");
+    }
     return fail(ctx, KVDRO_ERANGE, "a page cache kernel met a page number, slot or length outside its range");
 }
 
