@@ -253,7 +253,7 @@ int kvdro_kv_close(kvdro_kv* kv);
  *   new_len < 0   the request is done: its pages go back, to be handed out from the next call on.
  * Free pages are a ring of n_pages page numbers: pool = {head, count}; pages are taken at head and
  * returned behind the last.  Every page number is in the ring or in one request's table.
- *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size < 2^31.
+ *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size <= 2^31 - 256.
  *   cached, new_len, held  int32[B];  reserve: int32[B] or NULL (no reservations).
  *   table      int32[B][max_pages], updated: entries held[b] <= j < held_out[b] are written.
  *   ring       int32[n_pages], updated: returned pages are written behind the last.

@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libkvdro.so")
 SOURCES = ["api.cu", "setup.cu", "sort.cu", "grid.cu", "dual.cu", "noalloc.cu",
-           "kv_api.cu", "kv_pages.cu", "kv_decode.cu"]
+           "kv_api.cu", "kv_pages.cu", "kv_decode.cu", "kv_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

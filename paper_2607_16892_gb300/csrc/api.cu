@@ -211,7 +211,7 @@ int kvdro_destroy(kvdro_ctx* ctx) {
     cudaDeviceSynchronize();
     for (Buf* b : {&ctx->sorted, &ctx->scan_tot, &ctx->pairs, &ctx->hist, &ctx->cum, &ctx->csum, &ctx->sumx, &ctx->meta, &ctx->errs, &ctx->in_stage,
                    &ctx->grid_in, &ctx->keys, &ctx->cost64, &ctx->out_stage, &ctx->ranks, &ctx->tile_lo, &ctx->kv_err,
-                   &ctx->kv_pieces, &ctx->kv_tickets})
+                   &ctx->kv_pieces, &ctx->kv_tickets, &ctx->kv_joins})
         release(*b);
     while (ctx->caches) kvdro_kv_close(ctx->caches);
     if (ctx->pin) cudaFreeHost(ctx->pin);

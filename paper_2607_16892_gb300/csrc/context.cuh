@@ -61,7 +61,7 @@ struct kvdro_ctx {
     // The page cache
     kvdro_kv* caches = nullptr;  // open handles
     kvdro::Buf kv_err;           // the word in which its kernels report what they met
-    kvdro::Buf kv_pieces, kv_tickets;  // scratch of the attention kernels
+    kvdro::Buf kv_pieces, kv_tickets, kv_joins;  // scratch of the attention kernels
     cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it
     cudaStream_t kv_stream = nullptr;  // that call's stream
     bool kv_used = false;

@@ -33,27 +33,37 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 
-// Tensor maps of a cache (d, slot, head, page) for boxes of 64 elements of d by 16 slots.
+// Tensor maps of a cache (d, slot, head, page) for boxes of 64 elements of d by 16 slots, and by a page's.
 struct KvMaps {
-    CUtensorMap k16, v16;
+    CUtensorMap k16, v16, k, v;
+};
+
+// A tile of the chunk kernel that several CTAs share, noted by the first of them.
+struct Join {
+    int32_t b, rt, h;
+    int32_t last;  // the last CTA with a piece; -1: no tile
 };
 
 struct AttendArgs {
-    const uint16_t* q;
+    const uint16_t *q, *v;
     uint16_t* out;
     float* lse;
-    int64_t q_tok, q_head, out_tok, out_head;  // in elements
+    int64_t q_tok, q_head, out_tok, out_head, v_page, v_slot, v_head;  // in elements
     const int32_t *q_off, *kv_len, *table;
     int32_t B, T, heads, kv_heads, group, head_dim, n_pages, page_shift, max_pages, window;
     bool half, causal;
     float scale, cap;    // cap 0: none
     float* pieces;       // sums of tiles that several CTAs share
     unsigned* tickets;   // by CTA: arrivals at the tile that its stretch ends in, zero between calls
+    Join* joins;         // by CTA
     int32_t* err;
 };
 size_t kv_decode_piece_bytes(int sms);
 int kv_decode_ctas(int sms);
 cudaError_t kv_decode_prepare();
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s);
+size_t kv_chunk_piece_bytes(int sms);
+cudaError_t kv_chunk_prepare();
+cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s);
 
 }  // namespace kvdro

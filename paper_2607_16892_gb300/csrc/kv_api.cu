@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <new>
@@ -20,6 +21,7 @@ namespace {
 constexpr int64_t kMaxStride = (int64_t)1 << 39;  // elements: what a tensor map's 40 bits of bytes hold
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
+constexpr int64_t kFewRows = 16;  // rows that share a key head, up to which the kernel for single tokens runs
 
 int log2_of(int32_t v) {
     int s = 0;
@@ -38,8 +40,8 @@ int check_pages(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages) {
 int check_requests(kvdro_ctx* ctx, int32_t B, int32_t T, int32_t max_pages, int32_t page_size) {
     if (B < 1 || B > kvdro::kKvMaxRequests) return fail(ctx, KVDRO_EINVAL, "B = %d outside [1, %d]", B, kvdro::kKvMaxRequests);
     if (T < 0 || T > kMaxTokens) return fail(ctx, KVDRO_EINVAL, "T = %d outside [0, 2^30]", T);
-    if (max_pages < 1 || (int64_t)max_pages * page_size > 0x7fffffffLL)
-        return fail(ctx, KVDRO_EINVAL, "max_pages = %d: max_pages * page_size outside [page_size, 2^31)", max_pages);
+    if (max_pages < 1 || (int64_t)max_pages * page_size > 0x7fffff00LL)
+        return fail(ctx, KVDRO_EINVAL, "max_pages = %d: max_pages * page_size outside [page_size, 2^31 - 256]", max_pages);
     return KVDRO_OK;
 }
 
@@ -94,8 +96,11 @@ int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const i
 int prepare_attend(kvdro_ctx* ctx) {
     if (ctx->kv_ready) return KVDRO_OK;
     KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
+    KV_CUDA(kvdro::kv_chunk_prepare(), "preparing the attention kernels");
     if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
-    if (int rc = ensure(ctx, ctx->kv_pieces, kvdro::kv_decode_piece_bytes(ctx->sms))) return rc;
+    const size_t pieces = std::max(kvdro::kv_decode_piece_bytes(ctx->sms), kvdro::kv_chunk_piece_bytes(ctx->sms));
+    if (int rc = ensure(ctx, ctx->kv_pieces, pieces)) return rc;
+    if (int rc = ensure(ctx, ctx->kv_joins, sizeof(kvdro::Join) * (size_t)ctx->sms)) return rc;
     const size_t tickets = 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);
     if (int rc = ensure(ctx, ctx->kv_tickets, tickets)) return rc;
     KV_CUDA(cudaMemset(ctx->kv_tickets.p, 0, tickets), "clearing scratch");
@@ -147,6 +152,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     c.v = v;
     if (int rc = encode(ctx, &c.maps.k16, c, k, c.k_stride, 16)) return rc;
     if (int rc = encode(ctx, &c.maps.v16, c, v, c.v_stride, 16)) return rc;
+    if (int rc = encode(ctx, &c.maps.k, c, k, c.k_stride, page_size)) return rc;
+    if (int rc = encode(ctx, &c.maps.v, c, v, c.v_stride, page_size)) return rc;
     kvdro_kv* kv = new (std::nothrow) kvdro_kv(c);
     if (!kv) return fail(ctx, KVDRO_ENOMEM, "no memory for the handle");
     kv->next = ctx->caches;
@@ -274,12 +281,16 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
     kvdro::AttendArgs a;
     a.q = static_cast<const uint16_t*>(q);
+    a.v = static_cast<const uint16_t*>(kv->v);
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     a.q_tok = qs[0];
     a.q_head = qs[1];
     a.out_tok = os[0];
     a.out_head = os[1];
+    a.v_page = kv->v_stride[0];
+    a.v_slot = kv->v_stride[1];
+    a.v_head = kv->v_stride[2];
     a.q_off = q_off;
     a.kv_len = kv_len;
     a.table = table;
@@ -299,6 +310,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.cap = (float)softcap;
     a.pieces = static_cast<float*>(ctx->kv_pieces.p);
     a.tickets = static_cast<unsigned*>(ctx->kv_tickets.p);
+    a.joins = static_cast<kvdro::Join*>(ctx->kv_joins.p);
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->last_stream = s;
@@ -307,7 +319,9 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
     const bool captured = capture != cudaStreamCaptureStatusNone;
     if (!captured && ctx->kv_used && ctx->kv_stream != s) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
-    KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, ctx->sms, s), "attention kernel");
+    const int64_t most = max_q > 0 ? max_q : T > B ? T : 1;  // new tokens of a request, as far as is known
+    if (most * a.group <= kFewRows) KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, ctx->sms, s), "attention kernel");
+    else KV_CUDA(kvdro::launch_kv_chunk(a, kv->maps, ctx->sms, s), "attention kernel");
     if (!captured) {
         KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
         ctx->kv_stream = s;

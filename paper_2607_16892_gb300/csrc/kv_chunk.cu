@@ -1,0 +1,790 @@
+// Attention of chunks of new tokens over pages, on the tcgen05 tensor cores.
+//
+// A tile is 256 rows (tokens times the heads that share a key head) in two halves of 128, a block 128 positions.  Per block and
+// half: S = Q K^T (128 x 128 into tensor memory), weights P = 2^(S - m) by four warps, a row per thread, back into
+// tensor memory over S, and O += P V.  Both halves use the same K and V out of a ring of shared-memory stages; while the
+// four warps of one half exponentiate, the tensor cores work for the other:
+//     S0(0) S1(0) | PV0(0) S0(1) PV1(0) S1(1) | PV0(1) S0(2) ...
+// Bound by the tensor cores (4 D operations per row and position) where contexts are long; a row's 128 exponentials per
+// block and half are the next limit.  The maximum m that weights refer to is raised only when a row's
+// true maximum passes it by 2^8, so that O is rescaled in a few blocks at most; sums are exact in any case, for l and O
+// refer to the same m.  The line of all blocks is dealt to one CTA per SM (kv_device.cuh); pieces of tiles that
+// cross CTAs go through global memory and a second small kernel joins them in a fixed order.
+//
+// Roles: warps 0-3 and 4-7 the halves' weights, Q and results; 8 issues the products; 9 the copies; 10 and 11 look
+// through V of blocks that some row does not see whole: a weight of 0 times infinity or NaN is not 0, so such elements are
+// replaced by 0 there, and the rows that do see them get them added at the end.
+#include "kv_device.cuh"
+
+namespace kvdro {
+
+namespace {
+
+using namespace kv;
+
+constexpr int kHalfRows = 128, kRows = 2 * kHalfRows, kKeys = 128;
+constexpr int kThreads = 384;
+constexpr int kNotes = 16;  // blocks that the copies are ahead of the weights, at most (a power of two)
+constexpr float kRaise = 8.f;
+
+template <int D>
+struct Shape {
+    static constexpr int kTile = kKeys * D * 2;  // bytes of K or V of a block, and of half a tile of Q
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kSmem = 2 * kTile + kStages * kTile + 1024;
+    static constexpr int kPieceFloats = kRows * (D + 2);
+};
+
+using ChunkLine = Line<kRows, kKeys, kKeys>;
+
+struct Shared {
+    uint64_t kv_full[10], kv_empty[10], v_clean[10];
+    uint64_t s_full[2], p_full[2], o_full[2], q_full[2], done;
+    int64_t base, warp_sum[kThreads / 32];  // where the requests of thread `found` begin in the line
+    int found, dead;
+    uint32_t tmem;
+    uint32_t skip[kNotes];  // by block: 16-slot slices whose page number is none
+    int2 odd[2][kNotes];    // by looking warp and piece: first and last block with elements replaced, first > last if none
+};
+
+// ------------------------------------------------------------------ tcgen05
+__device__ __forceinline__ void tc_alloc(uint32_t at) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tc_free(uint32_t tmem) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Loads are done; `r` is what one brought, so that nothing is computed from it before.
+template <int N, int M>
+__device__ __forceinline__ void tc_wait_ld(uint32_t (&r)[N][M]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int n = 0; n < N; n++)
+#pragma unroll
+        for (int i = 0; i < M; i++) asm volatile("" : "+r"(r[n][i]));
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// d (+)= a b: A in shared memory, or in tensor memory.
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void tc_mma_t(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+// 32 columns of this thread's lane.
+__device__ __forceinline__ void tc_load32(uint32_t (&r)[32], uint32_t at) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tc_load16(uint32_t (&r)[16], uint32_t at) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
+__device__ __forceinline__ void tc_store16(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
+// Matrix descriptors of tiles of rows of 128 bytes in the 128-byte swizzle, in units of 16 bytes.  Contiguous along the
+// summed dimension (Q, K): groups of 8 rows 1024 bytes apart.  Contiguous along the other (V: rows are positions, summed
+// over): groups of 8 positions 1024 bytes apart, chunks of 64 columns one half of the tile apart.
+__device__ __forceinline__ uint64_t descriptor(uint32_t addr, uint32_t lead, uint32_t stride) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+template <bool H, int N, bool T>
+__device__ __forceinline__ constexpr uint32_t instruction() {  // 128 x N, FP32 sums; T: B contiguous along N
+    return 1u << 4 | (H ? 0u : 1u) << 7 | (H ? 0u : 1u) << 10 | (T ? 1u : 0u) << 16 | (uint32_t)(N / 8) << 17 | (128u / 16) << 24;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r, x = *reinterpret_cast<uint64_t*>(&a), y = *reinterpret_cast<uint64_t*>(&b), z = *reinterpret_cast<uint64_t*>(&c);
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r, x = *reinterpret_cast<uint64_t*>(&a), y = *reinterpret_cast<uint64_t*>(&b);
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return *reinterpret_cast<float2*>(&r);
+}
+
+// A bounded wait that also ends once another one of the CTA ran out.
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* dead) {
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (unsigned polls = 0; polls < (1u << 28); polls++) {
+        if (mbar_try(bar, parity)) return true;
+        if (*dead) return false;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (polls > (1u << 14) && t - t0 > 2000000000ull) break;
+    }
+    *dead = 1;
+    return false;
+}
+__device__ __forceinline__ bool wait(uint64_t& bar, uint32_t parity, int& dead) {
+    return mbar_try(smem_u32(&bar), parity) || wait_slow(smem_u32(&bar), parity, &dead);
+}
+
+// The pieces of this CTA's stretch, in order: each role walks them for itself.
+struct Walk {
+    ChunkLine& line;
+    Cursor<ChunkLine> at;
+    int left;      // blocks of the stretch from this piece on
+    int p0, p1;    // the piece: blocks of the tile
+    int piece = 0;
+
+    __device__ __forceinline__ Walk(ChunkLine& l, const Shared& s, int per, int64_t u0, int64_t u1) : line(l) {
+        at.seek(line, s.found * per, s.base, u0);
+        left = (int)(u1 - u0);
+        p0 = (int)(u0 - at.start);
+        p1 = min(at.t.blocks, p0 + left);
+    }
+    __device__ __forceinline__ bool next() {
+        left -= p1 - p0;
+        if (left == 0) return false;
+        at.next(line);
+        p0 = 0;
+        p1 = min(at.t.blocks, left);
+        piece++;
+        return true;
+    }
+    // Rows of a half, and its blocks in the piece: [x, y), empty if no row sees any.
+    __device__ __forceinline__ int half_rows(int i) const {
+        return min(kHalfRows, at.r.rows - at.rt * kRows - i * kHalfRows);
+    }
+    __device__ __forceinline__ int2 half_blocks(int i) const {
+        const int rows = half_rows(i);
+        if (rows <= 0) return make_int2(0, 0);
+        const int first = at.rt * kRows + i * kHalfRows, g = line.a.group;
+        const int hi = line.seen(at.r, (first + rows - 1) / g).y, lo = min(line.seen(at.r, first / g).x, hi);
+        const int b0 = max(p0, (lo - at.t.lo) / kKeys), b1 = min(p1, (hi - at.t.lo + kKeys - 1) / kKeys);
+        return make_int2(b0, max(b0, b1));
+    }
+    // Positions that every row of the tile sees.
+    __device__ __forceinline__ int2 all_see() const {
+        const int first = at.rt * kRows, last = min(first + kRows, at.r.rows) - 1;
+        return make_int2(line.seen(at.r, last / line.a.group).x, line.seen(at.r, first / line.a.group).y);
+    }
+    __device__ __forceinline__ bool edge(int blk, int2 all) const {
+        const int j0 = at.t.lo + blk * kKeys;
+        return j0 < all.x || j0 + kKeys > all.y;
+    }
+};
+
+// Q of a half into shared memory: rows of 16-byte chunks, sixteen (or eight) lanes to a row.
+template <int D>
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int half, char* to, int tid) {
+    constexpr int C = D / 8, kRowsAtOnce = kHalfRows / C, N = kHalfRows / kRowsAtOnce;
+    const int rows = w.half_rows(half), c = tid % C;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    uint4 x[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int r = tid / C + i * kRowsAtOnce;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+            const int row = w.at.rt * kRows + half * kHalfRows + r, tok = row / a.group, g = row - tok * a.group;
+            x[i] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.at.r.q0 + tok) * a.q_tok +
+                                                   (int64_t)(w.at.h * a.group + g) * a.q_head + c * 8);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int r = tid / C + i * kRowsAtOnce;
+        *reinterpret_cast<uint4*>(to + (c >> 3) * (kHalfRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+            make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
+    }
+}
+
+template <bool H, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_kv_chunk(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+    extern __shared__ char s_raw[];
+    __shared__ Shared sh;
+    using Sh = Shape<D>;
+    constexpr int kTile = Sh::kTile, kStages = Sh::kStages;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t raw = smem_u32(s_raw), smem = (raw + 1023) & ~1023u;
+    char* const smem_ptr = s_raw + (smem - raw);
+    const uint32_t q_at = smem, kv_at = smem + 2 * kTile;
+    ChunkLine line(a);
+
+    if (tid == 0) {
+        for (int i = 0; i < kStages; i++) {
+            mbar_init(smem_u32(&sh.kv_full[i]), 1);
+            mbar_init(smem_u32(&sh.kv_empty[i]), 3);
+            mbar_init(smem_u32(&sh.v_clean[i]), 64);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(smem_u32(&sh.s_full[i]), 1);
+            mbar_init(smem_u32(&sh.p_full[i]), 128);
+            mbar_init(smem_u32(&sh.o_full[i]), 1);
+            mbar_init(smem_u32(&sh.q_full[i]), 128);
+        }
+        mbar_init(smem_u32(&sh.done), 1);
+        sh.dead = 0;
+        fence_mbar_init();
+    }
+    if (warp == 8) tc_alloc(smem_u32(&sh.tmem));
+
+    // The line's length, and where each thread's requests begin in it.
+    const int per = (a.B + kThreads - 1) / kThreads;
+    int64_t mine = 0;
+    for (int b = min(tid * per, a.B), b1 = min(b + per, a.B); b < b1; b++) mine += line.cost(line.request(b));
+    int64_t incl = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) sh.warp_sum[warp] = incl;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < kThreads / 32; w++) {
+        if (w == warp) before = total;
+        total += sh.warp_sum[w];
+    }
+    before += incl - mine;
+    const int64_t share = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
+    const int64_t u0 = blockIdx.x * share, u1 = min(u0 + share, total);
+    if (u0 >= before && u0 < before + mine) {
+        sh.found = tid;
+        sh.base = before;
+    }
+    if (tid == 0) a.joins[blockIdx.x].last = -1;
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+
+    {  // tokens of no request: out = 0
+        const int end = max(0, min(a.q_off[a.B], a.T));
+        const int64_t vecs = (int64_t)(a.T - end) * a.heads * (D / 8);
+        for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < vecs; i += (int64_t)gridDim.x * kThreads) {
+            const int64_t row = i / (D / 8);
+            const int t = end + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
+            *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
+            if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
+        }
+    }
+
+    bool range = false;
+    if (u0 < u1) {
+        if (warp < 8) {
+            // ---------------------------------------------------------- weights and results of a half
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+            const int half = warp >> 2, row_in = tid & 127;
+            const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+            const uint32_t s_at = tmem + half * 128 + lanes, o_at = tmem + 256 + half * D + lanes;
+            const float cap2 = a.cap * kLog2e, scale = fmaxf(fabsf(a.scale), 0x1p-100f);
+            const float mul_in = a.cap > 0.f ? 2.f * kLog2e * scale / a.cap : kLog2e * scale;
+            const float mul = a.cap > 0.f ? 1.f : mul_in;
+            char* const q_to = smem_ptr + half * kTile;
+            uint32_t n_s = 0, n_o = 0;  // products awaited so far
+            int note = 0;               // blocks of the stretch before this piece
+            bool ok = true;
+            Walk w(line, sh, per, u0, u1);
+            bool loaded = false, more = true;
+            while (more) {
+                const int rows = w.half_rows(half);
+                const int2 blocks = w.half_blocks(half);
+                if (!loaded && blocks.x < blocks.y) {
+                    load_q<D>(a, w, half, q_to, row_in);
+                    fence_proxy_async();
+                    mbar_arrive(smem_u32(&sh.q_full[half]));
+                }
+                loaded = false;
+                const int row = w.at.rt * kRows + half * kHalfRows + row_in, tok = row / a.group;
+                const bool valid = row_in < rows;
+                const int2 see = valid ? line.seen(w.at.r, tok) : make_int2(0, 0x7fffffff);
+                float m = -INFINITY, l = 0.f;  // m in units of log2
+                for (int blk = blocks.x; blk < blocks.y && ok; blk++) {
+                    ok = __all_sync(~0u, wait(sh.s_full[half], n_s & 1, sh.dead));
+                    if (!ok) break;
+                    n_s++;
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) tc_load32(s[i], s_at + 32 * i);
+                    const int j0 = w.at.t.lo + blk * kKeys;
+                    const uint32_t skip = sh.skip[(note + blk - w.p0) & (kNotes - 1)];
+                    const bool masked = __any_sync(~0u, j0 < see.x || j0 + kKeys > see.y) || skip;
+                    tc_wait_ld(s);
+                    if (a.cap > 0.f) {
+#pragma unroll
+                        for (int i = 0; i < 128; i++)
+                            s[i >> 5][i & 31] = __float_as_uint(score(__uint_as_float(s[i >> 5][i & 31]), mul_in, cap2));
+                    }
+                    if (masked) {
+                        const int x = min(max(see.x - j0, 0), kKeys), y = min(max(see.y - j0, 0), kKeys);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const int x0 = min(max(x - 32 * i, 0), 32), y0 = min(max(y - 32 * i, 0), 32);
+                            uint32_t keep = (y0 == 32 ? ~0u : (1u << y0) - 1u) & (x0 == 32 ? 0u : ~0u << x0);
+                            keep &= (skip >> (2 * i) & 1 ? 0xffff0000u : ~0u) & (skip >> (2 * i + 1) & 1 ? 0xffffu : ~0u);
+#pragma unroll
+                            for (int c = 0; c < 32; c++)
+                                if (!(keep >> c & 1)) s[i][c] = 0xff800000u;
+                        }
+                    }
+                    float top = __uint_as_float(s[0][0]);
+#pragma unroll
+                    for (int i = 1; i < 127; i += 2)
+                        top = max3(top, __uint_as_float(s[i >> 5][i & 31]), __uint_as_float(s[(i + 1) >> 5][(i + 1) & 31]));
+                    top = fmaxf(top, __uint_as_float(s[3][31])) * mul;
+                    // Raise the maximum that the weights refer to, and rescale what is summed: rarely.
+                    const bool raise = top > m + kRaise || (m == -INFINITY && top > m);
+                    if (__any_sync(~0u, raise)) {
+                        const float to = raise ? top : m, keep = raise ? exp2_fast(m - to) : 1.f;
+                        m = to;
+                        l *= keep;
+                        if (blk > blocks.x) {
+                            ok = __all_sync(~0u, wait(sh.o_full[half], (n_o - 1) & 1, sh.dead));
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[1][16];
+                                tc_load16(o[0], o_at + c);
+                                tc_wait_ld(o);
+#pragma unroll
+                                for (int i = 0; i < 16; i++) o[0][i] = __float_as_uint(__uint_as_float(o[0][i]) * keep);
+                                tc_store16(o_at + c, o[0]);
+                            }
+                        }
+                    }
+                    const float shift = m == -INFINITY ? 0.f : m;
+                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2) {
+                            float2 y = fma2(make_float2(__uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1])), make_float2(mul, mul),
+                                            make_float2(-shift, -shift));
+                            y.x = exp2_fast(y.x);
+                            y.y = exp2_fast(y.y);
+                            sum[c >> 1 & 1] = add2(sum[c >> 1 & 1], y);
+                            p[c / 2] = pack2<H>(y.x, y.y);
+                        }
+                        tc_store16(s_at + 16 * i, p);
+                    }
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    tc_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&sh.p_full[half]));
+                    n_o++;
+                }
+                // The next piece's Q while the last product runs.
+                const Walk cur = w;
+                note += cur.p1 - cur.p0;
+                more = w.next();
+                if (more && ok && blocks.x < blocks.y) {
+                    const int2 nb = w.half_blocks(half);
+                    if (nb.x < nb.y) {
+                        load_q<D>(a, w, half, q_to, row_in);
+                        fence_proxy_async();
+                        mbar_arrive(smem_u32(&sh.q_full[half]));
+                        loaded = true;
+                    }
+                }
+                const bool some = blocks.x < blocks.y;
+                if (some && ok) {
+                    ok = __all_sync(~0u, wait(sh.o_full[half], (n_o - 1) & 1, sh.dead));
+                    tc_fence_after();
+                }
+                if (!ok) break;
+                if (rows <= 0) continue;
+                const int64_t c0 = cur.at.start / share, c1 = (cur.at.start + cur.at.t.blocks - 1) / share;
+                const int cta = blockIdx.x, g = row - tok * a.group, h = cur.at.h * a.group + g;
+                const int64_t t = cur.at.r.q0 + tok;
+                const bool whole = c0 == c1;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                float* const piece = a.pieces + (int64_t)(2 * cta + (c0 == cta)) * Sh::kPieceFloats;
+                const int prow = half * kHalfRows + row_in;
+                int2 odd = make_int2(1, 0);
+                const int2 all = cur.all_see();
+                if (some && (cur.edge(cur.p0, all) || cur.edge(cur.p1 - 1, all))) {  // else nobody looked
+                    const int2 x = sh.odd[0][cur.piece & (kNotes - 1)], y = sh.odd[1][cur.piece & (kNotes - 1)];
+                    odd = make_int2(min(x.x, y.x), max(x.y, y.y));
+                }
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t got[1][32];
+                    uint32_t(&o)[32] = got[0];
+                    if (some) {
+                        tc_load32(o, o_at + c);
+                        tc_wait_ld(got);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i++) o[i] = 0u;
+                    }
+                    if (valid && odd.x <= odd.y) {  // what was replaced by 0, for the rows that see it
+                        const int j1 = min(see.y, cur.at.t.lo + (odd.y + 1) * kKeys);
+                        for (int j = max(see.x, cur.at.t.lo + odd.x * kKeys); j < j1; j++) {
+                            const int page = a.table[(int64_t)cur.at.b * a.max_pages + (j >> a.page_shift)];
+                            if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+                            const uint16_t* v = a.v + page * a.v_page + (j & ((1 << a.page_shift) - 1)) * a.v_slot + cur.at.h * a.v_head + c;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const uint32_t x = *reinterpret_cast<const uint32_t*>(v + i);
+                                if (!any_nonfinite<H>(x)) continue;
+                                const float2 f = unpack2<H>(x);
+                                if (!isfinite(f.x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f.x);
+                                if (!isfinite(f.y)) o[i + 1] = __float_as_uint(__uint_as_float(o[i + 1]) + f.y);
+                            }
+                        }
+                    }
+                    if (!valid) continue;
+                    if (whole) {
+                        uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 x;
+                            x.x = pack2<H>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                            x.y = pack2<H>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                            x.z = pack2<H>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                            x.w = pack2<H>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                            out[i / 8] = x;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            reinterpret_cast<uint4*>(piece)[(c + i) / 4 * kRows + prow] = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    }
+                }
+                if (valid) {
+                    if (whole) {
+                        if (a.lse) a.lse[t * a.heads + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+                    } else {
+                        reinterpret_cast<float2*>(piece + kRows * D)[prow] = make_float2(m, l);
+                    }
+                }
+                if (!whole && c0 == cta && row_in == 0 && half == 0) {
+                    Join& j = a.joins[cta];
+                    j.b = cur.at.b;
+                    j.rt = cur.at.rt;
+                    j.h = cur.at.h;
+                    j.last = (int)c1;
+                }
+                tc_fence_before();
+            }
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+            Walk w(line, sh, per, u0, u1);
+            int stage = 0;
+            uint32_t round = 0;  // of the ring
+            auto advance = [&] {
+                if (++stage == kStages) {
+                    stage = 0;
+                    round ^= 1;
+                }
+            };
+            if (warp == 8) {
+                // ------------------------------------------------------ products
+                if (lane == 0) {
+                    constexpr uint32_t kIdS = instruction<H, 128, false>(), kIdO = instruction<H, D, true>();
+                    uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, clean = 0;
+                    bool act_prev[2] = {false, false}, first_prev[2] = {false, false}, edge_prev = false, any_prev = false;
+                    int v_prev = 0;
+                    uint32_t v_round = 0;
+                    bool ok = true;
+                    auto issue_s = [&](int i, uint32_t k_at) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; k++) {
+                            const uint32_t off = (k >> 2) * (kKeys * 128) + (k & 3) * 32;
+                            tc_mma(tmem + i * 128, descriptor(q_at + i * kTile + off, 16, 1024), descriptor(k_at + off, 16, 1024), kIdS, k > 0);
+                        }
+                        tc_commit(smem_u32(&sh.s_full[i]));
+                    };
+                    // O += P V of the block before, half i.
+                    auto issue_o = [&](int i) {
+                        ok = ok && wait(sh.p_full[i], n_p[i]++ & 1, sh.dead);
+                        if (!ok) return;
+                        tc_fence_after();
+                        const uint32_t v_at = kv_at + v_prev * kTile;
+#pragma unroll
+                        for (int k = 0; k < kKeys / 16; k++)
+                            tc_mma_t(tmem + 256 + i * D, tmem + i * 128 + k * 8, descriptor(v_at + k * 2048, kKeys * 128, 1024), kIdO,
+                                     k > 0 || !first_prev[i]);
+                        tc_commit(smem_u32(&sh.o_full[i]));
+                    };
+                    auto await_v = [&] {
+                        ok = ok && wait(sh.kv_full[v_prev], v_round, sh.dead);
+                        if (edge_prev) {
+                            ok = ok && wait(sh.v_clean[v_prev], clean >> v_prev & 1, sh.dead);
+                            clean ^= 1u << v_prev;
+                        }
+                        tc_fence_after();
+                    };
+                    bool more = true;
+                    while (more && ok) {
+                        int2 hb[2] = {w.half_blocks(0), w.half_blocks(1)};
+                        const int2 all = w.all_see();
+                        for (int blk = w.p0; blk < w.p1 && ok; blk++) {
+                            const int k_stage = stage;
+                            const uint32_t k_round = round;
+                            advance();
+                            if (any_prev) await_v();
+                            bool have_k = false;
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                if (act_prev[i]) issue_o(i);
+                                if (i == 1 && any_prev && ok) tc_commit(smem_u32(&sh.kv_empty[v_prev]));
+                                const bool act = blk >= hb[i].x && blk < hb[i].y;
+                                if (act && ok) {
+                                    if (!have_k) ok = wait(sh.kv_full[k_stage], k_round, sh.dead);
+                                    have_k = true;
+                                    if (blk == hb[i].x) ok = ok && wait(sh.q_full[i], n_q[i]++ & 1, sh.dead);
+                                    if (ok) {
+                                        tc_fence_after();
+                                        issue_s(i, kv_at + k_stage * kTile);
+                                    }
+                                }
+                                act_prev[i] = act;
+                                first_prev[i] = blk == hb[i].x;
+                            }
+                            if (!have_k) ok = ok && wait(sh.kv_full[k_stage], k_round, sh.dead);
+                            if (ok) tc_commit(smem_u32(&sh.kv_empty[k_stage]));
+                            v_prev = stage;
+                            v_round = round;
+                            edge_prev = w.edge(blk, all);
+                            any_prev = true;
+                            advance();
+                        }
+                        more = w.next();
+                    }
+                    if (any_prev && ok) {
+                        await_v();
+                        for (int i = 0; i < 2; i++)
+                            if (act_prev[i]) issue_o(i);
+                    }
+                    // Everything issued is done before tensor memory is given back.
+                    tc_commit(smem_u32(&sh.done));
+                    if (!mbar_wait(smem_u32(&sh.done), 0)) sh.dead = 1;
+                }
+                __syncwarp();
+            } else if (warp == 9) {
+                // ------------------------------------------------------ copies
+                bool ok = true, more = true;
+                uint32_t turns = 0;
+                int note = 0;
+                const int n = kKeys >> a.page_shift;
+                while (more && ok) {
+                    for (int blk = w.p0; blk < w.p1 && ok; blk++, note++) {
+                        const int j = w.at.t.lo + blk * kKeys + (lane << a.page_shift);
+                        int page = a.n_pages;  // past the last page: zeros
+                        bool none = false;
+                        if (lane < n && j < w.at.t.hi) {
+                            page = a.table[(int64_t)w.at.b * a.max_pages + (j >> a.page_shift)];
+                            if ((uint32_t)page >= (uint32_t)a.n_pages) {
+                                page = a.n_pages;
+                                none = true;
+                                range = true;
+                            }
+                        }
+                        const uint32_t nones = __ballot_sync(~0u, none);
+                        uint32_t skip = 0;
+                        if (nones) {
+                            for (int i = 0; i < kKeys / 16; i++)
+                                if (nones >> (16 * i >> a.page_shift) & 1) skip |= 1u << i;
+                        }
+                        if (lane == 0) sh.skip[note & (kNotes - 1)] = skip;
+                        __syncwarp();
+                        for (int v = 0; v < 2; v++) {
+                            if (turns >= (uint32_t)kStages) ok = __all_sync(~0u, wait(sh.kv_empty[stage], round ^ 1, sh.dead));
+                            if (!ok) break;
+                            const uint32_t bar = smem_u32(&sh.kv_full[stage]), to = kv_at + stage * kTile + (lane << a.page_shift) * 128;
+                            if (lane == 0) mbar_expect(bar, kTile);
+                            __syncwarp();
+                            if (lane < n) {
+#pragma unroll
+                                for (int d = 0; d < D / 64; d++)
+                                    load_box(to + d * (kKeys * 128), v ? &vmap : &kmap, d * 64, 0, w.at.h, page, bar);
+                            }
+                            turns++;
+                            advance();
+                        }
+                    }
+                    more = w.next();
+                }
+                if (!ok) {  // what is in flight must land before the CTA's memory is given away
+                    const uint32_t left = turns < (uint32_t)kStages ? turns : kStages;
+                    for (uint32_t i = 0; i < left; i++) {
+                        stage = stage == 0 ? kStages - 1 : stage - 1;
+                        if (stage == kStages - 1) round ^= 1;
+                        mbar_wait(smem_u32(&sh.kv_full[stage]), round);
+                    }
+                }
+            } else {
+                // ------------------------------------------------------ V that not every row sees
+                bool ok = true, more = true;
+                const int part = warp - 10;
+                while (more && ok) {
+                    const int2 all = w.all_see();
+                    const int seen_lo = line.seen(w.at.r, w.at.rt * kRows / a.group).x;
+                    int2 odd = make_int2(0x7fffffff, -1);
+                    if (lane == 0) sh.odd[part][w.piece & (kNotes - 1)] = odd;
+                    for (int blk = w.p0; blk < w.p1 && ok; blk++) {
+                        for (int v = 0; v < 2 && ok; v++) {
+                            ok = __all_sync(~0u, wait(sh.kv_full[stage], round, sh.dead));
+                            if (!ok) break;
+                            if (v && w.edge(blk, all)) {
+                                uint4* const at = reinterpret_cast<uint4*>(smem_ptr + 2 * kTile + stage * kTile + part * (kTile / 2));
+                                const int j0 = w.at.t.lo + blk * kKeys + (D == 64 ? part * (kKeys / 2) : 0);
+                                bool found = false;
+#pragma unroll 4
+                                for (int i = lane; i < kTile / 32; i += 32) {
+                                    uint4 x = at[i];
+                                    uint32_t* const e = reinterpret_cast<uint32_t*>(&x);
+                                    if (any_nonfinite<H>(x.x) || any_nonfinite<H>(x.y) || any_nonfinite<H>(x.z) || any_nonfinite<H>(x.w)) {
+                                        const int j = j0 + (i >> 3);
+                                        found |= j >= seen_lo && j < w.at.t.hi;
+                                        for (int k = 0; k < 4; k++) {
+                                            const float2 f = unpack2<H>(e[k]);
+                                            e[k] &= (isfinite(f.x) ? 0xffffu : 0u) | (isfinite(f.y) ? 0xffff0000u : 0u);
+                                        }
+                                        at[i] = x;
+                                    }
+                                }
+                                if (__any_sync(~0u, found)) {
+                                    odd = make_int2(min(odd.x, blk), blk);
+                                    if (lane == 0) sh.odd[part][w.piece & (kNotes - 1)] = odd;
+                                }
+                                fence_proxy_async();
+                                __syncwarp();
+                                mbar_arrive(smem_u32(&sh.v_clean[stage]));
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(&sh.kv_empty[stage]));
+                            advance();
+                        }
+                    }
+                    more = w.next();
+                }
+            }
+        }
+    }
+    if (__any_sync(~0u, range || line.bad) && lane == 0) atomicOr(a.err, kKvErrRange);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (tid == 0 && sh.dead) atomicOr(a.err, kKvErrTimeout);
+    if (warp == 8) tc_free(tmem);
+}
+
+// Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
+// last of CTA c; four threads a row's sums, lanes along the rows as the pieces are laid out.
+constexpr int kJoinThreads = 128, kJoinRows = 32;
+
+template <bool H, int D>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Join j = a.joins[blockIdx.x];
+    if (j.last < 0) return;
+    ChunkLine line(a);
+    const Request r = line.request(j.b);
+    const int row_in = blockIdx.y * kJoinRows + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const int row = j.rt * kRows + row_in;
+    if (row >= r.rows) return;
+    constexpr int kFloats = Shape<D>::kPieceFloats, N = D / 16;  // 16-byte vectors of a part
+    auto piece = [&](int c) { return a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats; };
+    float m = -INFINITY, l = 0.f;
+    for (int c = blockIdx.x; c <= j.last; c++) m = fmaxf(m, reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in].x);
+    const float shift = m == -INFINITY ? 0.f : m;
+    float4 o[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = blockIdx.x; c <= j.last; c++) {
+        const float2 ml = reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in];
+        const float f = exp2_fast(ml.x - shift);
+        l += ml.y * f;
+        const float4* p = reinterpret_cast<const float4*>(piece(c)) + part * N * kRows + row_in;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float4 x = p[i * kRows];
+            o[i] = make_float4(fmaf(x.x, f, o[i].x), fmaf(x.y, f, o[i].y), fmaf(x.z, f, o[i].z), fmaf(x.w, f, o[i].w));
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int tok = row / a.group, h = j.h * a.group + row - tok * a.group;
+    const int64_t t = r.q0 + tok;
+    uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + part * (D / 4));
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+        out[i / 2] = make_uint4(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv),
+                                pack2<H>(o[i + 1].x * inv, o[i + 1].y * inv), pack2<H>(o[i + 1].z * inv, o[i + 1].w * inv));
+    if (a.lse && part == 0) a.lse[t * a.heads + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+}
+
+template <bool H, int D>
+cudaError_t prepare() {
+    return cudaFuncSetAttribute(k_kv_chunk<H, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+}
+
+template <bool H, int D>
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
+    k_kv_chunk<H, D><<<sms, kThreads, Shape<D>::kSmem, s>>>(a, maps.k, maps.v);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute early[1];  // set up while the first kernel ends
+    early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(sms, kRows / kJoinRows);
+    c.blockDim = dim3(kJoinThreads);
+    c.stream = s;
+    c.attrs = early;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a);
+}
+
+}  // namespace
+
+size_t kv_chunk_piece_bytes(int sms) { return (size_t)sms * 2 * Shape<128>::kPieceFloats * sizeof(float); }
+
+cudaError_t kv_chunk_prepare() {
+    cudaError_t e;
+    if ((e = prepare<false, 64>()) != cudaSuccess || (e = prepare<true, 64>()) != cudaSuccess ||
+        (e = prepare<false, 128>()) != cudaSuccess)
+        return e;
+    return prepare<true, 128>();
+}
+
+cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
+    if (a.half) return a.head_dim == 128 ? launch<true, 128>(a, maps, sms, s) : launch<true, 64>(a, maps, sms, s);
+    return a.head_dim == 128 ? launch<false, 128>(a, maps, sms, s) : launch<false, 64>(a, maps, sms, s);
+}
+
+}  // namespace kvdro

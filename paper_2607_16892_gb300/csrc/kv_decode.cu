@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ char s_raw[];
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
-    __shared__ int64_t s_base[kThreads], s_warp_sum[kWarps];
+    __shared__ int64_t s_base, s_warp_sum[kWarps];  // where the requests of thread `s_found` begin in the line
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ int s_found, s_last;
     constexpr int kStage = kStageBytes<D>, kHalf = kStage / 2, KS = D / 16, NT = D / 8;
@@ -95,8 +95,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     before += incl - mine;
     const int64_t share = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
     const int64_t u0 = blockIdx.x * share, u1 = min(u0 + share, total);
-    s_base[tid] = before;
-    if (u0 >= before && u0 < before + mine) s_found = tid;
+    if (u0 >= before && u0 < before + mine) {
+        s_found = tid;
+        s_base = before;
+    }
     __syncthreads();
 
     // Tokens of no request: out = 0.
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     }
 
     Cursor<DecodeLine> in, at;  // of the copies, and of the sums
-    in.seek(line, s_found * per, s_base[s_found], u0);
+    in.seek(line, s_found * per, s_base, u0);
     at = in;
     int in_blk = (int)(u0 - in.start), in_left = (int)(u1 - u0);
 
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         }
         const uint32_t st = ring + stage * kStage;
         if ((filled >> stage & 1) && !dead) {
-            if (mbar_wait(smem_u32(&s_bar[warp][stage]), phase >> stage & 1)) phase ^= 1u << stage;
+            if (__all_sync(~0u, mbar_wait(smem_u32(&s_bar[warp][stage]), phase >> stage & 1))) phase ^= 1u << stage;
             else dead = true;
         }
         if ((filled >> stage & 1) && !dead) {

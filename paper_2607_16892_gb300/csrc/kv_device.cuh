@@ -27,11 +27,11 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
     if constexpr (H) return __half22float2(*reinterpret_cast<__half2*>(&w));
     else return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&w));
 }
-// Whether either half is an infinity or NaN: all exponent bits set.
+// Whether either half is an infinity or NaN: all exponent bits set, so that one more carries into the sign's place.
 template <bool H>
 __device__ __forceinline__ bool any_nonfinite(uint32_t w) {
-    constexpr uint32_t lo = H ? 0x7c00u : 0x7f80u, hi = lo << 16;
-    return (w & lo) == lo || (w & hi) == hi;
+    constexpr uint32_t exponent = H ? 0x7c007c00u : 0x7f807f80u, one = H ? 0x04000400u : 0x00800080u;
+    return ((w & exponent) + one) & 0x80008000u;
 }
 
 // 2^x.  Relative error 2^-22; 0 at -infinity.
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Waits for a phase, for about 2 s at most: 2 s of the GPU's timer and 2^14 polls made while running.
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+static __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     for (unsigned polls = 0; polls < (1u << 28); polls++) {
