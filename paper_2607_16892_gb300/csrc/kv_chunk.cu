@@ -39,7 +39,7 @@ using ChunkLine = Line<kRows, kKeys, kKeys>;
 
 struct Shared {
     uint64_t kv_full[10], kv_empty[10], v_clean[10];
-    uint64_t s_full[2], p_full[2], o_full[2], q_full[2], done;
+    uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2], done;
     int64_t base, warp_sum[kThreads / 32];  // where the requests of thread `found` begin in the line
     int found, dead;
     uint32_t tmem;
@@ -54,6 +54,11 @@ __device__ __forceinline__ void tc_alloc(uint32_t at) {
 }
 __device__ __forceinline__ void tc_free(uint32_t tmem) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -249,7 +254,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < 2; i++) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
-            mbar_init(smem_u32(&sh.p_full[i]), 128);
+            mbar_init(smem_u32(&sh.p_full[i][0]), 4);
+            mbar_init(smem_u32(&sh.p_full[i][1]), 4);
             mbar_init(smem_u32(&sh.o_full[i]), 1);
             mbar_init(smem_u32(&sh.q_full[i]), 128);
         }
@@ -328,6 +334,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int row = w.at.rt * kRows + half * kHalfRows + row_in, tok = row / a.group;
                 const bool valid = row_in < rows;
                 const int2 see = valid ? line.seen(w.at.r, tok) : make_int2(0, 0x7fffffff);
+                // Blocks inside [whole_lo, whole_hi) are seen whole by every row of the warp.
+                const int whole_lo = __reduce_max_sync(~0u, see.x), whole_hi = __reduce_min_sync(~0u, see.y);
                 float m = -INFINITY, l = 0.f;  // m in units of log2
                 for (int blk = blocks.x; blk < blocks.y && ok; blk++) {
                     ok = __all_sync(~0u, wait(sh.s_full[half], n_s & 1, sh.dead));
@@ -339,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 4; i++) tc_load32(s[i], s_at + 32 * i);
                     const int j0 = w.at.t.lo + blk * kKeys;
                     const uint32_t skip = sh.skip[(note + blk - w.p0) & (kNotes - 1)];
-                    const bool masked = __any_sync(~0u, j0 < see.x || j0 + kKeys > see.y) || skip;
+                    const bool masked = j0 < whole_lo || j0 + kKeys > whole_hi || skip;
                     tc_wait_ld(s);
                     if (a.cap > 0.f) {
 #pragma unroll
@@ -358,11 +366,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 if (!(keep >> c & 1)) s[i][c] = 0xff800000u;
                         }
                     }
-                    float top = __uint_as_float(s[0][0]);
+                    float tops[4];
 #pragma unroll
-                    for (int i = 1; i < 127; i += 2)
-                        top = max3(top, __uint_as_float(s[i >> 5][i & 31]), __uint_as_float(s[(i + 1) >> 5][(i + 1) & 31]));
-                    top = fmaxf(top, __uint_as_float(s[3][31])) * mul;
+                    for (int i = 0; i < 4; i++) tops[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
+#pragma unroll
+                    for (int c = 2; c < 32; c += 2)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) tops[i] = max3(tops[i], __uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1]));
+                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * mul;
                     // Raise the maximum that the weights refer to, and rescale what is summed: rarely.
                     const bool raise = top > m + kRaise || (m == -INFINITY && top > m);
                     if (__any_sync(~0u, raise)) {
@@ -385,25 +396,32 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     const float shift = m == -INFINITY ? 0.f : m;
-                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    float2 sum[4] = {};
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
+                        float2 y[16];
                         uint32_t p[16];
 #pragma unroll
-                        for (int c = 0; c < 32; c += 2) {
-                            float2 y = fma2(make_float2(__uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1])), make_float2(mul, mul),
-                                            make_float2(-shift, -shift));
-                            y.x = exp2_fast(y.x);
-                            y.y = exp2_fast(y.y);
-                            sum[c >> 1 & 1] = add2(sum[c >> 1 & 1], y);
-                            p[c / 2] = pack2<H>(y.x, y.y);
+                        for (int c = 0; c < 16; c++) {
+                            y[c] = fma2(make_float2(__uint_as_float(s[i][2 * c]), __uint_as_float(s[i][2 * c + 1])), make_float2(mul, mul),
+                                        make_float2(-shift, -shift));
+                            y[c] = make_float2(exp2_fast(y[c].x), exp2_fast(y[c].y));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 16; c++) {
+                            sum[c & 3] = add2(sum[c & 3], y[c]);
+                            p[c] = pack2<H>(y[c].x, y[c].y);
                         }
                         tc_store16(s_at + 16 * i, p);
+                        if (i & 1) {  // half of the positions: their product can start
+                            tc_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[half][i >> 1]));
+                        }
                     }
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    tc_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&sh.p_full[half]));
+                    sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                    l += sum[0].x + sum[0].y;
                     n_o++;
                 }
                 // The next piece's Q while the last product runs.
@@ -513,87 +531,106 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (warp == 8) {
                 // ------------------------------------------------------ products
-                if (lane == 0) {
-                    constexpr uint32_t kIdS = instruction<H, 128, false>(), kIdO = instruction<H, D, true>();
-                    uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, clean = 0;
-                    bool act_prev[2] = {false, false}, first_prev[2] = {false, false}, edge_prev = false, any_prev = false;
-                    int v_prev = 0;
-                    uint32_t v_round = 0;
-                    bool ok = true;
-                    auto issue_s = [&](int i, uint32_t k_at) {
+                // The whole warp takes part and one elected lane issues: descriptors and addresses stay in uniform registers
+                // (issued by a lane in a branch of its own, a product of 64 cycles took 90 to issue).
+                constexpr uint32_t kIdS = instruction<H, 128, false>(), kIdO = instruction<H, D, true>();
+                const uint32_t tm = __shfl_sync(~0u, tmem, 0);
+                uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, clean = 0;
+                bool act_prev[2] = {false, false}, first_prev[2] = {false, false}, edge_prev = false, any_prev = false;
+                int v_prev = 0;
+                uint32_t v_round = 0;
+                bool ok = true;
+                auto await = [&](uint64_t& bar, uint32_t parity) { return __all_sync(~0u, wait(bar, parity, sh.dead)); };
+                auto issue_s = [&](int i, int k_stage) {
+                    const uint64_t qd = descriptor(__shfl_sync(~0u, q_at + i * kTile, 0), 16, 1024);
+                    const uint64_t kd = descriptor(__shfl_sync(~0u, kv_at + k_stage * kTile, 0), 16, 1024);
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < D / 16; k++) {
-                            const uint32_t off = (k >> 2) * (kKeys * 128) + (k & 3) * 32;
-                            tc_mma(tmem + i * 128, descriptor(q_at + i * kTile + off, 16, 1024), descriptor(k_at + off, 16, 1024), kIdS, k > 0);
+                            const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
+                            tc_mma(tm + i * 128, qd + off, kd + off, kIdS, k > 0);
                         }
                         tc_commit(smem_u32(&sh.s_full[i]));
-                    };
-                    // O += P V of the block before, half i.
-                    auto issue_o = [&](int i) {
-                        ok = ok && wait(sh.p_full[i], n_p[i]++ & 1, sh.dead);
+                    }
+                    __syncwarp();
+                };
+                // O += P V of the block before, half i.
+                auto issue_o = [&](int i) {
+                    const uint64_t vd = descriptor(__shfl_sync(~0u, kv_at + v_prev * kTile, 0), kKeys * 128, 1024);
+                    const bool add = __shfl_sync(~0u, !first_prev[i], 0);
+#pragma unroll
+                    for (int part = 0; part < 2; part++) {
+                        ok = ok && await(sh.p_full[i][part], n_p[i] & 1);
                         if (!ok) return;
                         tc_fence_after();
-                        const uint32_t v_at = kv_at + v_prev * kTile;
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kKeys / 16; k++)
-                            tc_mma_t(tmem + 256 + i * D, tmem + i * 128 + k * 8, descriptor(v_at + k * 2048, kKeys * 128, 1024), kIdO,
-                                     k > 0 || !first_prev[i]);
-                        tc_commit(smem_u32(&sh.o_full[i]));
-                    };
-                    auto await_v = [&] {
-                        ok = ok && wait(sh.kv_full[v_prev], v_round, sh.dead);
-                        if (edge_prev) {
-                            ok = ok && wait(sh.v_clean[v_prev], clean >> v_prev & 1, sh.dead);
-                            clean ^= 1u << v_prev;
+                            for (int k = 4 * part; k < 4 * part + 4; k++)
+                                tc_mma_t(tm + 256 + i * D, tm + i * 128 + k * 8, vd + k * 128, kIdO, k > 0 || add);
+                            if (part == 1) tc_commit(smem_u32(&sh.o_full[i]));
                         }
-                        tc_fence_after();
-                    };
-                    bool more = true;
-                    while (more && ok) {
-                        int2 hb[2] = {w.half_blocks(0), w.half_blocks(1)};
-                        const int2 all = w.all_see();
-                        for (int blk = w.p0; blk < w.p1 && ok; blk++) {
-                            const int k_stage = stage;
-                            const uint32_t k_round = round;
-                            advance();
-                            if (any_prev) await_v();
-                            bool have_k = false;
-#pragma unroll
-                            for (int i = 0; i < 2; i++) {
-                                if (act_prev[i]) issue_o(i);
-                                if (i == 1 && any_prev && ok) tc_commit(smem_u32(&sh.kv_empty[v_prev]));
-                                const bool act = blk >= hb[i].x && blk < hb[i].y;
-                                if (act && ok) {
-                                    if (!have_k) ok = wait(sh.kv_full[k_stage], k_round, sh.dead);
-                                    have_k = true;
-                                    if (blk == hb[i].x) ok = ok && wait(sh.q_full[i], n_q[i]++ & 1, sh.dead);
-                                    if (ok) {
-                                        tc_fence_after();
-                                        issue_s(i, kv_at + k_stage * kTile);
-                                    }
-                                }
-                                act_prev[i] = act;
-                                first_prev[i] = blk == hb[i].x;
-                            }
-                            if (!have_k) ok = ok && wait(sh.kv_full[k_stage], k_round, sh.dead);
-                            if (ok) tc_commit(smem_u32(&sh.kv_empty[k_stage]));
-                            v_prev = stage;
-                            v_round = round;
-                            edge_prev = w.edge(blk, all);
-                            any_prev = true;
-                            advance();
-                        }
-                        more = w.next();
+                        __syncwarp();
                     }
-                    if (any_prev && ok) {
-                        await_v();
-                        for (int i = 0; i < 2; i++)
+                    n_p[i]++;
+                };
+                auto release = [&](int st) {
+                    if (elect_one()) tc_commit(smem_u32(&sh.kv_empty[st]));
+                    __syncwarp();
+                };
+                auto await_v = [&] {
+                    ok = ok && await(sh.kv_full[v_prev], v_round);
+                    if (edge_prev) {
+                        ok = ok && await(sh.v_clean[v_prev], clean >> v_prev & 1);
+                        clean ^= 1u << v_prev;
+                    }
+                    tc_fence_after();
+                };
+                bool more = true;
+                while (more && ok) {
+                    int2 hb[2] = {w.half_blocks(0), w.half_blocks(1)};
+                    const int2 all = w.all_see();
+                    for (int blk = w.p0; blk < w.p1 && ok; blk++) {
+                        const int k_stage = stage;
+                        const uint32_t k_round = round;
+                        advance();
+                        if (any_prev) await_v();
+                        bool have_k = false;
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
                             if (act_prev[i]) issue_o(i);
+                            if (i == 1 && any_prev && ok) release(v_prev);
+                            const bool act = blk >= hb[i].x && blk < hb[i].y;
+                            if (act && ok) {
+                                if (!have_k) ok = await(sh.kv_full[k_stage], k_round);
+                                have_k = true;
+                                if (blk == hb[i].x) ok = ok && await(sh.q_full[i], n_q[i]++ & 1);
+                                if (ok) {
+                                    tc_fence_after();
+                                    issue_s(i, k_stage);
+                                }
+                            }
+                            act_prev[i] = act;
+                            first_prev[i] = blk == hb[i].x;
+                        }
+                        if (!have_k) ok = ok && await(sh.kv_full[k_stage], k_round);
+                        if (ok) release(k_stage);
+                        v_prev = stage;
+                        v_round = round;
+                        edge_prev = w.edge(blk, all);
+                        any_prev = true;
+                        advance();
                     }
-                    // Everything issued is done before tensor memory is given back.
-                    tc_commit(smem_u32(&sh.done));
-                    if (!mbar_wait(smem_u32(&sh.done), 0)) sh.dead = 1;
+                    more = w.next();
                 }
+                if (any_prev && ok) {
+                    await_v();
+                    for (int i = 0; i < 2; i++)
+                        if (act_prev[i] && ok) issue_o(i);
+                }
+                // Everything issued is done before tensor memory is given back.
+                if (elect_one()) tc_commit(smem_u32(&sh.done));
+                __syncwarp();
+                if (!mbar_wait(smem_u32(&sh.done), 0)) sh.dead = 1;
                 __syncwarp();
             } else if (warp == 9) {
                 // ------------------------------------------------------ copies
