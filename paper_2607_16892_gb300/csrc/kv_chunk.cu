@@ -145,21 +145,20 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return *reinterpret_cast<float2*>(&r);
 }
 
-// A bounded wait that also ends once another one of the CTA ran out.
-__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* dead) {
+// A bounded wait.  Once one ran out in the CTA (`dead`), every wait ends at once and the roles run on to their ends without
+// waiting, over values that mean nothing: no role branches on it, so that warps stay whole; the copies stop.
+__device__ __forceinline__ void wait_slow(uint32_t bar, uint32_t parity, volatile int* dead) {
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     for (unsigned polls = 0; polls < (1u << 28); polls++) {
-        if (mbar_try(bar, parity)) return true;
-        if (*dead) return false;
+        if (mbar_try(bar, parity) || *dead) return;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
         if (polls > (1u << 14) && t - t0 > 2000000000ull) break;
     }
     *dead = 1;
-    return false;
 }
-__device__ __forceinline__ bool wait(uint64_t& bar, uint32_t parity, int& dead) {
-    return mbar_try(smem_u32(&bar), parity) || wait_slow(smem_u32(&bar), parity, &dead);
+__device__ __forceinline__ void wait(uint64_t& bar, uint32_t parity, int& dead) {
+    if (!mbar_try(smem_u32(&bar), parity)) wait_slow(smem_u32(&bar), parity, &dead);
 }
 
 // The pieces of this CTA's stretch, in order: each role walks them for itself.
@@ -319,7 +318,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             char* const q_to = smem_ptr + half * kTile;
             uint32_t n_s = 0, n_o = 0;  // products awaited so far
             int note = 0;               // blocks of the stretch before this piece
-            bool ok = true;
             Walk w(line, sh, per, u0, u1);
             bool loaded = false, more = true;
             while (more) {
@@ -337,9 +335,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // Blocks inside [whole_lo, whole_hi) are seen whole by every row of the warp.
                 const int whole_lo = __reduce_max_sync(~0u, see.x), whole_hi = __reduce_min_sync(~0u, see.y);
                 float m = -INFINITY, l = 0.f;  // m in units of log2
-                for (int blk = blocks.x; blk < blocks.y && ok; blk++) {
-                    ok = __all_sync(~0u, wait(sh.s_full[half], n_s & 1, sh.dead));
-                    if (!ok) break;
+                for (int blk = blocks.x; blk < blocks.y; blk++) {
+                    wait(sh.s_full[half], n_s & 1, sh.dead);
+                    __syncwarp();
                     n_s++;
                     tc_fence_after();
                     uint32_t s[4][32];
@@ -381,8 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         m = to;
                         l *= keep;
                         if (blk > blocks.x) {
-                            ok = __all_sync(~0u, wait(sh.o_full[half], (n_o - 1) & 1, sh.dead));
-                            if (!ok) break;
+                            wait(sh.o_full[half], (n_o - 1) & 1, sh.dead);
+                            __syncwarp();
                             tc_fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
@@ -428,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Walk cur = w;
                 note += cur.p1 - cur.p0;
                 more = w.next();
-                if (more && ok && blocks.x < blocks.y) {
+                if (more && blocks.x < blocks.y) {
                     const int2 nb = w.half_blocks(half);
                     if (nb.x < nb.y) {
                         load_q<D>(a, w, half, q_to, row_in);
@@ -438,11 +436,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 const bool some = blocks.x < blocks.y;
-                if (some && ok) {
-                    ok = __all_sync(~0u, wait(sh.o_full[half], (n_o - 1) & 1, sh.dead));
+                if (some) {
+                    wait(sh.o_full[half], (n_o - 1) & 1, sh.dead);
+                    __syncwarp();
                     tc_fence_after();
                 }
-                if (!ok) break;
                 if (rows <= 0) continue;
                 const int64_t c0 = cur.at.start / share, c1 = (cur.at.start + cur.at.t.blocks - 1) / share;
                 const int cta = blockIdx.x, g = row - tok * a.group, h = cur.at.h * a.group + g;
@@ -536,101 +534,85 @@ __global__ void __launch_bounds__(kThreads, 1)
                 constexpr uint32_t kIdS = instruction<H, 128, false>(), kIdO = instruction<H, D, true>();
                 const uint32_t tm = __shfl_sync(~0u, tmem, 0);
                 uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0}, clean = 0;
-                bool act_prev[2] = {false, false}, first_prev[2] = {false, false}, edge_prev = false, any_prev = false;
+                bool act_prev[2] = {false, false}, first_prev[2] = {false, false}, any_prev = false;
                 int v_prev = 0;
-                uint32_t v_round = 0;
-                bool ok = true;
-                auto await = [&](uint64_t& bar, uint32_t parity) { return __all_sync(~0u, wait(bar, parity, sh.dead)); };
-                auto issue_s = [&](int i, int k_stage) {
-                    const uint64_t qd = descriptor(__shfl_sync(~0u, q_at + i * kTile, 0), 16, 1024);
-                    const uint64_t kd = descriptor(__shfl_sync(~0u, kv_at + k_stage * kTile, 0), 16, 1024);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < D / 16; k++) {
-                            const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
-                            tc_mma(tm + i * 128, qd + off, kd + off, kIdS, k > 0);
-                        }
-                        tc_commit(smem_u32(&sh.s_full[i]));
-                    }
-                    __syncwarp();
-                };
-                // O += P V of the block before, half i.
-                auto issue_o = [&](int i) {
+                // O += P V of the block before, half i, as its weights come in two parts; `last`: V's stage is free after it.
+                auto issue_o = [&](int i, bool last) {
                     const uint64_t vd = descriptor(__shfl_sync(~0u, kv_at + v_prev * kTile, 0), kKeys * 128, 1024);
                     const bool add = __shfl_sync(~0u, !first_prev[i], 0);
+                    const uint32_t free = smem_u32(&sh.kv_empty[v_prev]);
 #pragma unroll
                     for (int part = 0; part < 2; part++) {
-                        ok = ok && await(sh.p_full[i][part], n_p[i] & 1);
-                        if (!ok) return;
-                        tc_fence_after();
+                        if (act_prev[i]) {
+                            wait(sh.p_full[i][part], n_p[i] & 1, sh.dead);
+                            tc_fence_after();
+                        }
+                        __syncwarp();
                         if (elect_one()) {
+                            if (act_prev[i]) {
 #pragma unroll
-                            for (int k = 4 * part; k < 4 * part + 4; k++)
-                                tc_mma_t(tm + 256 + i * D, tm + i * 128 + k * 8, vd + k * 128, kIdO, k > 0 || add);
-                            if (part == 1) tc_commit(smem_u32(&sh.o_full[i]));
+                                for (int k = 4 * part; k < 4 * part + 4; k++)
+                                    tc_mma_t(tm + 256 + i * D, tm + i * 128 + k * 8, vd + k * 128, kIdO, k > 0 || add);
+                                if (part == 1) tc_commit(smem_u32(&sh.o_full[i]));
+                            }
+                            if (part == 1 && last) tc_commit(free);
                         }
                         __syncwarp();
                     }
-                    n_p[i]++;
-                };
-                auto release = [&](int st) {
-                    if (elect_one()) tc_commit(smem_u32(&sh.kv_empty[st]));
-                    __syncwarp();
-                };
-                auto await_v = [&] {
-                    ok = ok && await(sh.kv_full[v_prev], v_round);
-                    if (edge_prev) {
-                        ok = ok && await(sh.v_clean[v_prev], clean >> v_prev & 1);
-                        clean ^= 1u << v_prev;
-                    }
-                    tc_fence_after();
+                    n_p[i] += act_prev[i];
                 };
                 bool more = true;
-                while (more && ok) {
+                while (more) {
                     int2 hb[2] = {w.half_blocks(0), w.half_blocks(1)};
                     const int2 all = w.all_see();
-                    for (int blk = w.p0; blk < w.p1 && ok; blk++) {
-                        const int k_stage = stage;
+                    for (int blk = w.p0; blk < w.p1; blk++) {
+                        const uint32_t k_at = kv_at + stage * kTile, k_free = smem_u32(&sh.kv_empty[stage]);
+                        uint64_t& k_full = sh.kv_full[stage];
                         const uint32_t k_round = round;
                         advance();
-                        if (any_prev) await_v();
-                        bool have_k = false;
 #pragma unroll
                         for (int i = 0; i < 2; i++) {
-                            if (act_prev[i]) issue_o(i);
-                            if (i == 1 && any_prev && ok) release(v_prev);
+                            if (any_prev) issue_o(i, i == 1);
                             const bool act = blk >= hb[i].x && blk < hb[i].y;
-                            if (act && ok) {
-                                if (!have_k) ok = await(sh.kv_full[k_stage], k_round);
-                                have_k = true;
-                                if (blk == hb[i].x) ok = ok && await(sh.q_full[i], n_q[i]++ & 1);
-                                if (ok) {
-                                    tc_fence_after();
-                                    issue_s(i, k_stage);
+                            if (i == 0) wait(k_full, k_round, sh.dead);
+                            if (act && blk == hb[i].x) wait(sh.q_full[i], n_q[i]++ & 1, sh.dead);
+                            tc_fence_after();
+                            const uint64_t qd = descriptor(__shfl_sync(~0u, q_at + i * kTile, 0), 16, 1024);
+                            const uint64_t kd = descriptor(__shfl_sync(~0u, k_at, 0), 16, 1024);
+                            if (elect_one()) {
+                                if (act) {
+#pragma unroll
+                                    for (int k = 0; k < D / 16; k++) {
+                                        const uint32_t off = ((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4;
+                                        tc_mma(tm + i * 128, qd + off, kd + off, kIdS, k > 0);
+                                    }
+                                    tc_commit(smem_u32(&sh.s_full[i]));
                                 }
+                                if (i == 1) tc_commit(k_free);
                             }
+                            __syncwarp();
                             act_prev[i] = act;
                             first_prev[i] = blk == hb[i].x;
                         }
-                        if (!have_k) ok = ok && await(sh.kv_full[k_stage], k_round);
-                        if (ok) release(k_stage);
+                        // V of this block, while S is computed.
                         v_prev = stage;
-                        v_round = round;
-                        edge_prev = w.edge(blk, all);
                         any_prev = true;
+                        wait(sh.kv_full[stage], round, sh.dead);
+                        if (w.edge(blk, all)) {
+                            wait(sh.v_clean[stage], clean >> stage & 1, sh.dead);
+                            clean ^= 1u << stage;
+                        }
                         advance();
                     }
                     more = w.next();
                 }
-                if (any_prev && ok) {
-                    await_v();
-                    for (int i = 0; i < 2; i++)
-                        if (act_prev[i] && ok) issue_o(i);
-                }
+                issue_o(0, false);
+                issue_o(1, true);
                 // Everything issued is done before tensor memory is given back.
+                __syncwarp();
                 if (elect_one()) tc_commit(smem_u32(&sh.done));
                 __syncwarp();
-                if (!mbar_wait(smem_u32(&sh.done), 0)) sh.dead = 1;
+                wait(sh.done, 0, sh.dead);
                 __syncwarp();
             } else if (warp == 9) {
                 // ------------------------------------------------------ copies
@@ -660,7 +642,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (lane == 0) sh.skip[note & (kNotes - 1)] = skip;
                         __syncwarp();
                         for (int v = 0; v < 2; v++) {
-                            if (turns >= (uint32_t)kStages) ok = __all_sync(~0u, wait(sh.kv_empty[stage], round ^ 1, sh.dead));
+                            if (turns >= (uint32_t)kStages) wait(sh.kv_empty[stage], round ^ 1, sh.dead);
+                            ok = __all_sync(~0u, *(volatile int*)&sh.dead == 0);
                             if (!ok) break;
                             const uint32_t bar = smem_u32(&sh.kv_full[stage]), to = kv_at + stage * kTile + (lane << a.page_shift) * 128;
                             if (lane == 0) mbar_expect(bar, kTile);
@@ -686,17 +669,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             } else {
                 // ------------------------------------------------------ V that not every row sees
-                bool ok = true, more = true;
+                bool more = true;
                 const int part = warp - 10;
-                while (more && ok) {
+                while (more) {
                     const int2 all = w.all_see();
                     const int seen_lo = line.seen(w.at.r, w.at.rt * kRows / a.group).x;
                     int2 odd = make_int2(0x7fffffff, -1);
                     if (lane == 0) sh.odd[part][w.piece & (kNotes - 1)] = odd;
-                    for (int blk = w.p0; blk < w.p1 && ok; blk++) {
-                        for (int v = 0; v < 2 && ok; v++) {
-                            ok = __all_sync(~0u, wait(sh.kv_full[stage], round, sh.dead));
-                            if (!ok) break;
+                    for (int blk = w.p0; blk < w.p1; blk++) {
+                        for (int v = 0; v < 2; v++) {
+                            wait(sh.kv_full[stage], round, sh.dead);
+                            __syncwarp();
                             if (v && w.edge(blk, all)) {
                                 uint4* const at = reinterpret_cast<uint4*>(smem_ptr + 2 * kTile + stage * kTile + part * (kTile / 2));
                                 const int j0 = w.at.t.lo + blk * kKeys + (D == 64 ? part * (kKeys / 2) : 0);
