@@ -33,9 +33,9 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 
-// Tensor maps of a cache (d, slot, head, page) for boxes of 64 elements of d by 16 slots, and by a page's.
+// Tensor maps of a cache (d, slot, head, page) for boxes of 64 elements of d by a page's slots, and by 32 at most.
 struct KvMaps {
-    CUtensorMap k16, v16, k, v;
+    CUtensorMap k, v, k_slice, v_slice;
 };
 
 // A tile of the chunk kernel that several CTAs share, noted by the first of them.
@@ -61,7 +61,8 @@ struct AttendArgs {
 size_t kv_decode_piece_bytes(int sms);
 int kv_decode_ctas(int sms);
 cudaError_t kv_decode_prepare();
-cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s);
+// `eight`: at most eight rows share a key head (else sixteen; more are right, but slow).
+cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 cudaError_t kv_chunk_prepare();
 cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s);

@@ -150,8 +150,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     c.head_dim = head_dim;
     c.k = k;
     c.v = v;
-    if (int rc = encode(ctx, &c.maps.k16, c, k, c.k_stride, 16)) return rc;
-    if (int rc = encode(ctx, &c.maps.v16, c, v, c.v_stride, 16)) return rc;
+    if (int rc = encode(ctx, &c.maps.k_slice, c, k, c.k_stride, std::min(page_size, 32))) return rc;
+    if (int rc = encode(ctx, &c.maps.v_slice, c, v, c.v_stride, std::min(page_size, 32))) return rc;
     if (int rc = encode(ctx, &c.maps.k, c, k, c.k_stride, page_size)) return rc;
     if (int rc = encode(ctx, &c.maps.v, c, v, c.v_stride, page_size)) return rc;
     kvdro_kv* kv = new (std::nothrow) kvdro_kv(c);
@@ -320,7 +320,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     const bool captured = capture != cudaStreamCaptureStatusNone;
     if (!captured && ctx->kv_used && ctx->kv_stream != s) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
     const int64_t most = max_q > 0 ? max_q : T > B ? T : 1;  // new tokens of a request, as far as is known
-    if (most * a.group <= kFewRows) KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, ctx->sms, s), "attention kernel");
+    if (most * a.group <= kFewRows) KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, most * a.group <= 8, ctx->sms, s), "attention kernel");
     else KV_CUDA(kvdro::launch_kv_chunk(a, kv->maps, ctx->sms, s), "attention kernel");
     if (!captured) {
         KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");

@@ -1,13 +1,17 @@
 // Attention of few rows over pages: single tokens, drafted tokens.
 //
 // Bound by the bytes of the keys and values, each read once for the (at most 16) rows that share a key head.  The line of
-// all blocks of 64 positions is dealt to two CTAs per SM (kv_device.cuh); in a block each of a CTA's four warps has 16
-// positions of its own, with its own ring of tensor copies, running maxima, sums and weighted sums: nothing
-// in the loop waits for another warp.  The warps are joined through shared memory at the end of a tile, pieces of a tile
-// through global memory by the CTA that arrives last, both in a fixed order.
+// all blocks of 128 positions is dealt to two CTAs per SM (kv_device.cuh); in a block each of a CTA's four warps has 32
+// positions of its own, with its own ring of tensor copies, maxima, sums and weighted sums: nothing in the loop waits
+// for another warp.  The warps are joined through shared memory at the end of a tile, pieces of a tile through
+// global memory by the CTA that arrives last, both in a fixed order.
 //
-// Products run on mma.m16n8k16: a tcgen05 tile has 128 rows, and a slice's 32 mma take far less than its copy.  The weights are
-// rounded to the cache's type for the second product, which adds about as much error as the result's own rounding.
+// Products run on mma.m16n8k16 with the positions (then the columns of V) as the 16 and the rows as the 8, so that up to
+// eight rows fill what they are given: S^T = K Q^T, O^T += V^T P^T.  A tcgen05 tile would have 128 rows.  With eight warps on
+// an SM a warp's latency per slice counts, hence 32 positions at a time and a maximum that is raised only when a
+// row's own passes it by 2^8 (O and the sum refer to the same one), which saves the shuffles in most slices.
+// The weights are rounded to the cache's type for the second product, which adds about as much error as the result's own
+// rounding.
 #include "kv_device.cuh"
 
 namespace kvdro {
@@ -16,16 +20,18 @@ namespace {
 
 using namespace kv;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kRows = 16, kSlice = 16, kKeys = kSlice * kWarps, kStages = 3;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16, kSlice = 32, kKeys = kSlice * kWarps;
 constexpr int kCtasPerSm = 2;
+constexpr float kRaise = 8.f;
 
 template <int D>
-constexpr int kStageBytes = 2 * kSlice * D * 2;
+struct Ring {  // a stage: K or V of a slice
+    static constexpr int kBytes = kSlice * D * 2, kStages = D == 128 ? 3 : 6;
+    static constexpr int kSmem = kWarps * kStages * kBytes + 1024;
+};
+// A piece in global memory: rows of D sums, then their maxima and sums of weights.
 template <int D>
-constexpr int kSmemBytes = kWarps * kStages * kStageBytes<D> + 1024;
-// A piece in global memory: kRows rows of D sums, then their maxima and sums of weights.
-template <int D>
-constexpr int kPieceFloats = kRows * (D + 2);
+constexpr int kPieceFloats = kMostRows * (D + 2);
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -38,6 +44,11 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                  : "r"(at)
                  : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {  // an 8 x 8 matrix of 16-bit elements across the warp
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 template <bool H>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -57,17 +68,19 @@ __device__ __forceinline__ uint32_t chunk_at(int key, int c) {
     return (uint32_t)((c >> 3) * (kSlice * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4));
 }
 
-using DecodeLine = Line<kRows, kKeys, kSlice>;
-
-template <bool H, int D>
+// NR: groups of eight rows of a tile.
+template <bool H, int D, int NR>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ char s_raw[];
+    constexpr int kStages = Ring<D>::kStages, kStage = Ring<D>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
+    constexpr int kRows = 8 * NR;
+    using DecodeLine = Line<kRows, kKeys, kSlice>;
+    constexpr int kRowFloats = D + 4;  // of a row of sums in shared memory: no bank conflicts
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
     __shared__ int64_t s_base, s_warp_sum[kWarps];  // where the requests of thread `s_found` begin in the line
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ int s_found, s_last;
-    constexpr int kStage = kStageBytes<D>, kHalf = kStage / 2, KS = D / 16, NT = D / 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(s_raw), ring = ((raw + 1023) & ~1023u) + warp * kStages * kStage;
     char* const ring_ptr = s_raw + (ring - raw);
@@ -117,50 +130,55 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         return;
     }
 
+    // Units in the order K, V of a slice, K, V of the next.
     Cursor<DecodeLine> in, at;  // of the copies, and of the sums
     in.seek(line, s_found * per, s_base, u0);
     at = in;
     int in_blk = (int)(u0 - in.start), in_left = (int)(u1 - u0);
+    bool in_v = false;
 
-    // Page numbers of this warp's slices of 32 blocks, one per lane.
-    int pg = -1, pg_b = -1, pg_rt = -1, pg_blk = -1;
+    // Page numbers of this warp's slices of 32 blocks, one per lane; a slice has two pages if they have 16 slots.
+    const int slots = min(kSlice, 1 << a.page_shift);
+    int pg[2] = {-1, -1}, pg_b = -1, pg_rt = -1, pg_blk = -1;
     bool range = false;
     uint32_t filled = 0, phase = 0;  // by stage: holds a slice; the parity to wait for
+    uint32_t gaps = 0;               // by stage, two bits: 16 positions whose page number is none
     auto fetch = [&](int stage) {
-        if (in_left == 0) {
-            filled &= ~(1u << stage);
-            return;
-        }
+        filled &= ~(1u << stage);
+        if (in_left == 0) return;
         if (in.b != pg_b || in.rt != pg_rt || (in_blk >> 5) != pg_blk) {
             pg_b = in.b;
             pg_rt = in.rt;
             pg_blk = in_blk >> 5;
             const int j = in.t.lo + ((in_blk & ~31) + lane) * kKeys + warp * kSlice;
-            pg = -1;
-            if (j < in.t.hi) {
-                pg = a.table[(int64_t)in.b * a.max_pages + (j >> a.page_shift)];
-                if ((uint32_t)pg >= (uint32_t)a.n_pages) {
-                    pg = -1;
-                    range = true;
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                pg[i] = -1;
+                if (j + 16 * i < in.t.hi) {
+                    const int page = a.table[(int64_t)in.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
+                    if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
+                    else range = true;
                 }
             }
         }
-        const int page = __shfl_sync(~0u, pg, in_blk & 31);
-        if (page >= 0) {
+        const int p0 = __shfl_sync(~0u, pg[0], in_blk & 31), p1 = __shfl_sync(~0u, pg[1], in_blk & 31);
+        gaps = (gaps & ~(3u << 2 * stage)) | ((p0 < 0 ? 1u : 0u) | (p1 < 0 ? 2u : 0u)) << 2 * stage;
+        if (p0 >= 0 || p1 >= 0) {
             if (lane == 0) {
                 const int slot = (in.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1);
                 const uint32_t bar = smem_u32(&s_bar[warp][stage]), to = ring + stage * kStage;
+                const CUtensorMap* const map = in_v ? &vmap : &kmap;
                 mbar_expect(bar, kStage);
 #pragma unroll
-                for (int d = 0; d < D / 64; d++) {
-                    load_box(to + d * (kSlice * 128), &kmap, d * 64, slot, in.h, page, bar);
-                    load_box(to + kHalf + d * (kSlice * 128), &vmap, d * 64, slot, in.h, page, bar);
+                for (int d = 0; d < D / 64; d++) {  // a page that is none reads as zeros
+                    load_box(to + d * (kSlice * 128), map, d * 64, slot, in.h, p0 >= 0 ? p0 : a.n_pages, bar);
+                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, in.h, p1 >= 0 ? p1 : a.n_pages, bar);
                 }
             }
             filled |= 1u << stage;
-        } else {
-            filled &= ~(1u << stage);
         }
+        in_v = !in_v;
+        if (in_v) return;
         in_left--;
         if (++in_blk == in.t.blocks && in_left) {
             in.next(line);
@@ -171,169 +189,206 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     for (int s = 0; s < kStages; s++) fetch(s);
 
     const float mul = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : kLog2e * a.scale, cap2 = a.cap * kLog2e;
-    const int r_lo = lane >> 2, r_hi = r_lo + 8;  // this thread's rows
-    uint32_t qf[KS][4];
-    float o[NT][4];
-    float m[2], l[2];
-    int2 see[2];
-    int2 all_see;  // positions that every row sees
-    bool alike = true;  // every row sees the same
+    uint32_t qf[NR][KS][2];
+    float o[NR][DT][4];
+    float m[NR][2], l[NR][2];  // of rows 8 n + 2 (lane & 3) + i
+    int2 see[NR][2];
+    int2 all_see, any_see;  // positions that every row of the tile sees, and that some row does
     bool dead = false;
     int stage = 0, blk = (int)(u0 - at.start);
     bool fresh = true;
+
+    // The slice in `stage`, once it is there; false if there is none.
+    auto ready = [&] {
+        if (!(filled >> stage & 1) || dead) return false;
+        if (__all_sync(~0u, mbar_wait(smem_u32(&s_bar[warp][stage]), phase >> stage & 1))) phase ^= 1u << stage;
+        else dead = true;
+        return !dead;
+    };
+    auto advance = [&] {
+        if (!dead) fetch(stage);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    };
 
     for (int64_t u = u0; u < u1; u++) {
         if (fresh) {  // a tile begins here, or this CTA's piece of it
             fresh = false;
             const int first = at.rt * kRows, rows = min(kRows, at.r.rows - first);
-            const uint16_t* qp[2];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int r = first + min(i ? r_hi : r_lo, rows - 1), tok = r / a.group, g = r - tok * a.group;
-                qp[i] = a.q + (int64_t)(at.r.q0 + tok) * a.q_tok + (int64_t)(at.h * a.group + g) * a.q_head;
-                see[i] = line.seen(at.r, tok);
-                m[i] = -INFINITY;
-                l[i] = 0.f;
+            for (int n = 0; n < NR; n++) {
+                {
+                    const int r = first + min(8 * n + (lane >> 2), rows - 1), tok = r / a.group, g = r - tok * a.group;
+                    const uint16_t* const q = a.q + (int64_t)(at.r.q0 + tok) * a.q_tok + (int64_t)(at.h * a.group + g) * a.q_head + 2 * (lane & 3);
+#pragma unroll
+                    for (int k = 0; k < KS; k++) {
+                        qf[n][k][0] = *reinterpret_cast<const uint32_t*>(q + k * 16);
+                        qf[n][k][1] = *reinterpret_cast<const uint32_t*>(q + k * 16 + 8);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    see[n][i] = line.seen(at.r, (first + min(8 * n + 2 * (lane & 3) + i, rows - 1)) / a.group);
+                    m[n][i] = -INFINITY;
+                    l[n][i] = 0.f;
+                }
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[n][d][i] = 0.f;
             }
             const int2 s0 = line.seen(at.r, first / a.group), s1 = line.seen(at.r, (first + rows - 1) / a.group);
             all_see = make_int2(s1.x, s0.y);
-            alike = s0.x == s1.x && s0.y == s1.y;
-#pragma unroll
-            for (int k = 0; k < KS; k++) {
-                const int c = k * 16 + 2 * (lane & 3);
-                qf[k][0] = *reinterpret_cast<const uint32_t*>(qp[0] + c);
-                qf[k][1] = *reinterpret_cast<const uint32_t*>(qp[1] + c);
-                qf[k][2] = *reinterpret_cast<const uint32_t*>(qp[0] + c + 8);
-                qf[k][3] = *reinterpret_cast<const uint32_t*>(qp[1] + c + 8);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; n++)
-#pragma unroll
-                for (int i = 0; i < 4; i++) o[n][i] = 0.f;
+            any_see = make_int2(s0.x, s1.y);
         }
+        const int j0 = at.t.lo + blk * kKeys + warp * kSlice;
+        const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || (gaps >> 2 * stage & 3);
+        const uint32_t gap = gaps >> 2 * stage & 3;
+        float s[NR][MT][4];  // scores, then weights: position 16 t + (lane >> 2) + 8 (i >> 1), row 8 n + 2 (lane & 3) + (i & 1)
+        const bool some = ready();
+        if (some) {
+            const uint32_t st = ring + stage * kStage;
+#pragma unroll
+            for (int n = 0; n < NR; n++)
+#pragma unroll
+                for (int t = 0; t < MT; t++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) s[n][t][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    uint32_t kf[4];
+                    ldsm4(kf, st + chunk_at(16 * t + (lane & 15), 2 * k + (lane >> 4)));
+#pragma unroll
+                    for (int n = 0; n < NR; n++) mma<H>(s[n][t], kf, qf[n][k][0], qf[n][k][1]);
+                }
+        }
+        __syncwarp();
+        advance();
+        const bool have = ready();
         const uint32_t st = ring + stage * kStage;
-        if ((filled >> stage & 1) && !dead) {
-            if (__all_sync(~0u, mbar_wait(smem_u32(&s_bar[warp][stage]), phase >> stage & 1))) phase ^= 1u << stage;
-            else dead = true;
-        }
-        if ((filled >> stage & 1) && !dead) {
-            const int j0 = at.t.lo + blk * kKeys + warp * kSlice;
-            const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y;
-            float s[2][4] = {};
+        if (some && have) {
+            float top[NR][2];
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                uint32_t kf[4];
-                ldsm4(kf, st + chunk_at((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-                mma<H>(s[0], qf[k], kf[0], kf[1]);
-                mma<H>(s[1], qf[k], kf[2], kf[3]);
-            }
+            for (int n = 0; n < NR; n++) {
+                top[n][0] = top[n][1] = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < 2; n++)
+                for (int t = 0; t < MT; t++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    s[n][i] = score(s[n][i], mul, cap2);
-                    if (edge) {
-                        const int j = j0 + 8 * n + 2 * (lane & 3) + (i & 1);
-                        if (j < see[i >> 1].x || j >= see[i >> 1].y) s[n][i] = -INFINITY;
+                    for (int i = 0; i < 4; i++) {
+                        float& x = s[n][t][i];
+                        x = score(x, mul, cap2);
+                        if (edge) {
+                            const int j = j0 + 16 * t + (lane >> 2) + 8 * (i >> 1);
+                            if (j < see[n][i & 1].x || j >= see[n][i & 1].y || (gap >> t & 1)) x = -INFINITY;
+                        }
+                        top[n][i & 1] = fmaxf(top[n][i & 1], x);
                     }
+            }
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NR; n++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) raise |= top[n][i] > m[n][i] + kRaise || (m[n][i] == -INFINITY && top[n][i] > m[n][i]);
+            if (__any_sync(~0u, raise)) {
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        float to = top[n][i];
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
+                        to = fmaxf(to, m[n][i]);
+                        const float keep = m[n][i] == -INFINITY ? 0.f : exp2_fast(m[n][i] - to);
+                        m[n][i] = to;
+                        l[n][i] *= keep;
+#pragma unroll
+                        for (int d = 0; d < DT; d++) {
+                            o[n][d][i] *= keep;
+                            o[n][d][i + 2] *= keep;
+                        }
+                    }
+            }
+            uint32_t pf[NR][MT][2];
+#pragma unroll
+            for (int n = 0; n < NR; n++)
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float to = m[n][i & 1];
+                        s[n][t][i] = exp2_fast(s[n][t][i] - (to == -INFINITY ? 0.f : to));
+                        l[n][i & 1] += s[n][t][i];
+                    }
+                    pf[n][t][0] = transpose8(pack2<H>(s[n][t][0], s[n][t][1]));
+                    pf[n][t][1] = transpose8(pack2<H>(s[n][t][2], s[n][t][3]));
                 }
-            float top[2];
-            bool grows = false;
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
-                top[i] = fmaxf(top[i], m[i]);
-                grows |= top[i] > m[i];
-            }
-            if (__any_sync(~0u, grows)) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const float keep = m[i] == -INFINITY ? 0.f : exp2_fast(m[i] - top[i]);
-                    m[i] = top[i];
-                    l[i] *= keep;
-#pragma unroll
-                    for (int n = 0; n < NT; n++) {
-                        o[n][2 * i] *= keep;
-                        o[n][2 * i + 1] *= keep;
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const float shift = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-                for (int n = 0; n < 2; n++)
-#pragma unroll
-                    for (int c = 0; c < 2; c++) {
-                        s[n][2 * i + c] = exp2_fast(s[n][2 * i + c] - shift);
-                        l[i] += s[n][2 * i + c];
-                    }
-            }
-            uint32_t pf[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) pf[i] = pack2<H>(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
             // Values of positions that no row sees are taken as zero, whatever is stored there.
-            uint32_t keep0 = ~0u, keep1 = ~0u;
+            uint32_t keep[MT][2];
             bool odd = false;
             if (edge) {
-                const int j = j0 + 2 * (lane & 3);
-                auto in_tile = [&](int x) {
-                    const int lo = alike ? all_see.x : at.t.lo, hi = alike ? all_see.y : at.t.hi;
-                    return x >= lo && x < hi;
-                };
-                keep0 = (in_tile(j) ? 0xffffu : 0u) | (in_tile(j + 1) ? 0xffff0000u : 0u);
-                keep1 = (in_tile(j + 8) ? 0xffffu : 0u) | (in_tile(j + 9) ? 0xffff0000u : 0u);
-                if (!alike) {  // a value that some rows see must be finite for the others
+                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y; };
+#pragma unroll
+                for (int t = 0; t < MT; t++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const int j = j0 + 16 * t + 8 * i + 2 * (lane & 3);
+                        keep[t][i] = (seen(j) ? 0xffffu : 0u) | (seen(j + 1) ? 0xffff0000u : 0u);
+                    }
+                if (any_see.x != all_see.x || any_see.y != all_see.y) {  // a value that some rows see must be finite for the others
 #pragma unroll 1
                     for (int c = lane; c < kSlice * D / 8; c += 32) {
                         uint32_t w[4];
                         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                                      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                     : "r"(st + kHalf + c * 16));
-                        for (int i = 0; i < 4; i++) odd |= any_nonfinite<H>(w[i]);
+                                     : "r"(st + c * 16));
+                        bool x = false;
+                        for (int i = 0; i < 4; i++) x |= any_nonfinite<H>(w[i]);
+                        odd |= x && seen(j0 + (c >> 3) % kSlice);
                     }
                     odd = __any_sync(~0u, odd);
                 }
             }
             if (!odd) {
 #pragma unroll
-                for (int n = 0; n < NT; n += 2) {
-                    uint32_t vf[4];
-                    ldsm4t(vf, st + kHalf + chunk_at((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
-                    if (edge) {
-                        vf[0] &= keep0;
-                        vf[1] &= keep1;
-                        vf[2] &= keep0;
-                        vf[3] &= keep1;
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int t = 0; t < MT; t++) {
+                        uint32_t vf[4];
+                        ldsm4t(vf, st + chunk_at(16 * t + ((lane >> 4) << 3) + (lane & 7), 2 * d + ((lane >> 3) & 1)));
+                        if (edge) {
+                            vf[0] &= keep[t][0];
+                            vf[1] &= keep[t][0];
+                            vf[2] &= keep[t][1];
+                            vf[3] &= keep[t][1];
+                        }
+#pragma unroll
+                        for (int n = 0; n < NR; n++) mma<H>(o[n][d], vf, pf[n][t][0], pf[n][t][1]);
                     }
-                    mma<H>(o[n], pf, vf[0], vf[1]);
-                    mma<H>(o[n + 1], pf, vf[2], vf[3]);
-                }
             } else {  // row by row, over what each sees
 #pragma unroll 1
                 for (int k = 0; k < kSlice; k++) {
-                    const int from = (lane & ~3) + ((k & 7) >> 1);
-                    float w[2];
+                    const int from = (k & 7) * 4 + (lane & 3);
 #pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const float x = k & 8 ? (k & 1 ? s[1][2 * i + 1] : s[1][2 * i]) : (k & 1 ? s[0][2 * i + 1] : s[0][2 * i]);
-                        w[i] = __shfl_sync(~0u, x, from);
-                    }
-                    const bool v0 = j0 + k >= see[0].x && j0 + k < see[0].y, v1 = j0 + k >= see[1].x && j0 + k < see[1].y;
+                    for (int n = 0; n < NR; n++) {
+                        float w[2];
+                        bool see_k[2];
 #pragma unroll
-                    for (int n = 0; n < NT; n++) {
-                        uint32_t x;
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(st + kHalf + chunk_at(k, n) + 4 * (lane & 3)));
-                        const float2 v = unpack2<H>(x);
-                        if (v0) {
-                            o[n][0] = fmaf(w[0], v.x, o[n][0]);
-                            o[n][1] = fmaf(w[0], v.y, o[n][1]);
+                        for (int i = 0; i < 2; i++) {
+                            const float x = k & 16 ? (k & 8 ? s[n][1][2 + i] : s[n][1][i]) : (k & 8 ? s[n][0][2 + i] : s[n][0][i]);
+                            w[i] = __shfl_sync(~0u, x, from);
+                            see_k[i] = j0 + k >= see[n][i].x && j0 + k < see[n][i].y && !(gap >> (k >> 4) & 1);
                         }
-                        if (v1) {
-                            o[n][2] = fmaf(w[1], v.x, o[n][2]);
-                            o[n][3] = fmaf(w[1], v.y, o[n][3]);
+#pragma unroll
+                        for (int d = 0; d < 2 * DT; d++) {
+                            uint16_t x;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(st + chunk_at(k, d) + 2 * (lane >> 2)));
+                            const float v = unpack2<H>(x).x;
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                float& y = o[n][d >> 1][2 * (d & 1) + i];
+                                if (see_k[i]) y = fmaf(w[i], v, y);
+                            }
                         }
                     }
                 }
@@ -344,29 +399,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         if (blk == at.t.blocks || u + 1 == u1) {  // the end of a tile, or of this CTA's piece of it
             const int first = at.rt * kRows, rows = min(kRows, at.r.rows - first);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                l[i] += __shfl_xor_sync(~0u, l[i], 1);
-                l[i] += __shfl_xor_sync(~0u, l[i], 2);
-                if ((lane & 3) == 0) {
-                    s_m[warp][i ? r_hi : r_lo] = m[i];
-                    s_l[warp][i ? r_hi : r_lo] = l[i];
-                }
-            }
-            __syncthreads();
-            // Each warp's sums go over its own last stage, whose next copy waits for that.
-            float* const mine_o = reinterpret_cast<float*>(ring_ptr + stage * kStage);
+            for (int n = 0; n < NR; n++)
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int r = i ? r_hi : r_lo;
-                float to = s_m[0][r];
-                for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][r]);
-                const float f = exp2_fast(m[i] - (to == -INFINITY ? 0.f : to));
+                for (int i = 0; i < 2; i++) {
 #pragma unroll
-                for (int n = 0; n < NT; n++) {
-                    const int c = (8 * n + 2 * (lane & 3)) ^ ((r & 3) << 3);
-                    *reinterpret_cast<float2*>(mine_o + r * D + c) = make_float2(o[n][2 * i] * f, o[n][2 * i + 1] * f);
+                    for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(~0u, l[n][i], x);
+                    if (lane < 4) {
+                        s_m[warp][8 * n + 2 * lane + i] = m[n][i];
+                        s_l[warp][8 * n + 2 * lane + i] = l[n][i];
+                    }
                 }
-            }
             __syncthreads();
             const int64_t c0 = at.start / share, c1 = (at.start + at.t.blocks - 1) / share;  // CTAs with a piece
             const int cta = blockIdx.x;
@@ -381,22 +423,41 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
                 if (a.lse && c == 0) a.lse[t * a.heads + h] = sum == 0.f ? -INFINITY : kLn2 * (to + log2f(sum));
             };
             constexpr int kQuads = D / 4;
-            for (int i = tid; i < rows * kQuads; i += kThreads) {
-                const int r = i / kQuads, c = 4 * (i % kQuads);
-                float to = s_m[0][r], sum = 0.f;
-                for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][r]);
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int w = 0; w < kWarps; w++) {
-                    const float4 y = *reinterpret_cast<const float4*>(ring_ptr + (w - warp) * kStages * kStage + stage * kStage +
-                                                                      4 * (r * D + (c ^ ((r & 3) << 3))));
-                    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-                    sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
+            // Each warp's sums go over its own last stage, whose next copy waits for that; eight rows at a time.
+            float* const mine_o = reinterpret_cast<float*>(ring_ptr + stage * kStage);
+#pragma unroll
+            for (int n = 0; n < NR; n++) {
+                if (n > 0) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const int r = 2 * (lane & 3) + i;
+                    float to = s_m[0][8 * n + r];
+                    for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][8 * n + r]);
+                    const float f = exp2_fast(m[n][i] - (to == -INFINITY ? 0.f : to));
+#pragma unroll
+                    for (int d = 0; d < DT; d++) {
+                        mine_o[r * kRowFloats + 16 * d + (lane >> 2)] = o[n][d][i] * f;
+                        mine_o[r * kRowFloats + 16 * d + 8 + (lane >> 2)] = o[n][d][i + 2] * f;
+                    }
                 }
-                if (c0 == c1) {
-                    row_out(r, c, x, to, sum);
-                } else {
-                    *reinterpret_cast<float4*>(piece + r * D + c) = x;
-                    if (c == 0) *reinterpret_cast<float2*>(piece + kRows * D + 2 * r) = make_float2(to, sum);
+                __syncthreads();
+                for (int i = tid; i < min(8, rows - 8 * n) * kQuads; i += kThreads) {
+                    const int r8 = i / kQuads, c = 4 * (i % kQuads), r = 8 * n + r8;
+                    float to = s_m[0][r], sum = 0.f;
+                    for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][r]);
+                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int w = 0; w < kWarps; w++) {
+                        const float4 y = *reinterpret_cast<const float4*>(ring_ptr + (w - warp) * kStages * kStage + stage * kStage +
+                                                                          4 * (r8 * kRowFloats + c));
+                        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+                        sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
+                    }
+                    if (c0 == c1) {
+                        row_out(r, c, x, to, sum);
+                    } else {
+                        *reinterpret_cast<float4*>(piece + r * D + c) = x;
+                        if (c == 0) *reinterpret_cast<float2*>(piece + kRows * D + 2 * r) = make_float2(to, sum);
+                    }
                 }
             }
             __syncthreads();
@@ -440,8 +501,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
                 fresh = true;
             }
         }
-        if (!dead) fetch(stage);
-        stage = stage + 1 == kStages ? 0 : stage + 1;
+        __syncwarp();
+        advance();
     }
     if (dead) {  // what is still in flight must land before the CTA's memory is given away
         for (int s = 0; s < kStages; s++)
@@ -451,14 +512,20 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     if (__any_sync(~0u, range || line.bad) && lane == 0) atomicOr(a.err, kKvErrRange);
 }
 
+template <bool H, int D, int NR>
+cudaError_t prepare() {
+    return cudaFuncSetAttribute(k_kv_decode<H, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D>::kSmem);
+}
 template <bool H, int D>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(k_kv_decode<H, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<D>);
+    const cudaError_t e = prepare<H, D, 1>();
+    return e == cudaSuccess ? prepare<H, D, 2>() : e;
 }
 
 template <bool H, int D>
-cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
-    k_kv_decode<H, D><<<sms * kCtasPerSm, kThreads, kSmemBytes<D>, s>>>(a, maps.k16, maps.v16);
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
+    if (eight) k_kv_decode<H, D, 1><<<sms * kCtasPerSm, kThreads, Ring<D>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
+    else k_kv_decode<H, D, 2><<<sms * kCtasPerSm, kThreads, Ring<D>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
     return cudaGetLastError();
 }
 
@@ -475,9 +542,9 @@ cudaError_t kv_decode_prepare() {
     return prepare<true, 128>();
 }
 
-cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
-    if (a.half) return a.head_dim == 128 ? launch<true, 128>(a, maps, sms, s) : launch<true, 64>(a, maps, sms, s);
-    return a.head_dim == 128 ? launch<false, 128>(a, maps, sms, s) : launch<false, 64>(a, maps, sms, s);
+cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
+    if (a.half) return a.head_dim == 128 ? launch<true, 128>(a, maps, eight, sms, s) : launch<true, 64>(a, maps, eight, sms, s);
+    return a.head_dim == 128 ? launch<false, 128>(a, maps, eight, sms, s) : launch<false, 64>(a, maps, eight, sms, s);
 }
 
 }  // namespace kvdro
