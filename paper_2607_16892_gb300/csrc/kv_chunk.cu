@@ -741,11 +741,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
     constexpr int kFloats = Shape<D>::kPieceFloats, N = D / 16;  // 16-byte vectors of a part
     auto piece = [&](int c) { return a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats; };
     float m = -INFINITY, l = 0.f;
+#pragma unroll 8
     for (int c = blockIdx.x; c <= j.last; c++) m = fmaxf(m, reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in].x);
     const float shift = m == -INFINITY ? 0.f : m;
     float4 o[N];
 #pragma unroll
     for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int c = blockIdx.x; c <= j.last; c++) {
         const float2 ml = reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in];
         const float f = exp2_fast(ml.x - shift);

@@ -21,12 +21,13 @@ namespace {
 using namespace kv;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16, kSlice = 32, kKeys = kSlice * kWarps;
-constexpr int kCtasPerSm = 2;
+constexpr int kMostCtas = 4;  // per SM
 constexpr float kRaise = 8.f;
 
-template <int D>
+template <int D, int NR>
 struct Ring {  // a stage: K or V of a slice
-    static constexpr int kBytes = kSlice * D * 2, kStages = D == 128 ? 3 : 6;
+    static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? 4 : 2);  // per SM
+    static constexpr int kBytes = kSlice * D * 2, kStages = D == 128 ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6);
     static constexpr int kSmem = kWarps * kStages * kBytes + 1024;
 };
 // A piece in global memory: rows of D sums, then their maxima and sums of weights.
@@ -70,10 +71,10 @@ __device__ __forceinline__ uint32_t chunk_at(int key, int c) {
 
 // NR: groups of eight rows of a tile.
 template <bool H, int D, int NR>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+__global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ char s_raw[];
-    constexpr int kStages = Ring<D>::kStages, kStage = Ring<D>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
+    constexpr int kStages = Ring<D, NR>::kStages, kStage = Ring<D, NR>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
     using DecodeLine = Line<kRows, kKeys, kSlice>;
     constexpr int kRowFloats = D + 4;  // of a row of sums in shared memory: no bank conflicts
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 
 template <bool H, int D, int NR>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(k_kv_decode<H, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D>::kSmem);
+    return cudaFuncSetAttribute(k_kv_decode<H, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NR>::kSmem);
 }
 template <bool H, int D>
 cudaError_t prepare() {
@@ -524,15 +525,15 @@ cudaError_t prepare() {
 
 template <bool H, int D>
 cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
-    if (eight) k_kv_decode<H, D, 1><<<sms * kCtasPerSm, kThreads, Ring<D>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
-    else k_kv_decode<H, D, 2><<<sms * kCtasPerSm, kThreads, Ring<D>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
+    if (eight) k_kv_decode<H, D, 1><<<sms * Ring<D, 1>::kCtas, kThreads, Ring<D, 1>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
+    else k_kv_decode<H, D, 2><<<sms * Ring<D, 2>::kCtas, kThreads, Ring<D, 2>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t kv_decode_piece_bytes(int sms) { return (size_t)sms * kCtasPerSm * 2 * kPieceFloats<128> * sizeof(float); }
-int kv_decode_ctas(int sms) { return sms * kCtasPerSm; }
+size_t kv_decode_piece_bytes(int sms) { return (size_t)sms * kMostCtas * 2 * kPieceFloats<128> * sizeof(float); }
+int kv_decode_ctas(int sms) { return sms * kMostCtas; }
 
 cudaError_t kv_decode_prepare() {
     cudaError_t e;

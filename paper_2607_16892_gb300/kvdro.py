@@ -349,19 +349,22 @@ class KvdroKv:
     __slots__ = ("handle", "ctx", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
 
 
-def _dev(name: str, a: Any, dtype: str, n=None) -> int:
-    """Pointer of a contiguous CUDA tensor of this dtype (and of ``n`` elements)."""
+# A serving step makes these calls once per layer, so their host time counts: the checks of a good argument take few
+# attribute reads, and what is wrong with a bad one is found out afterwards.
+def _dev(name: str, a: Any, dtype, n=None) -> int:
+    """Pointer of a contiguous CUDA tensor of this torch dtype (and of ``n`` elements)."""
+    try:
+        if a.is_cuda and a.dtype is dtype and a.is_contiguous() and (n is None or a.numel() == n):
+            return a.data_ptr()
+    except AttributeError:
+        pass
     if not getattr(a, "is_cuda", False):
         raise ValueError(f"{name} must be a CUDA tensor")
-    if not _kv_types:
-        _kv_setup()
-    if a.dtype is not _kv_types[dtype]:
+    if a.dtype is not dtype:
         raise TypeError(f"{name}: expected dtype {dtype}, got {a.dtype}")
     if not a.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if n is not None and a.numel() != n:
-        raise ValueError(f"{name} has {a.numel()} elements; the call needs exactly {n}")
-    return a.data_ptr()
+    raise ValueError(f"{name} has {a.numel()} elements; the call needs exactly {n}")
 
 
 _kv_types: dict = {}
@@ -369,35 +372,48 @@ _caches: dict = {}  # handle of a context -> its open page caches, which kvdro_d
 _I2, _I3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
+_lib_kv = _i32 = _f32 = None  # the loaded library and torch's dtypes
+
+
 def _kv_setup():
-    import torch
-    _kv_types.update({"int32": torch.int32, "float32": torch.float32, torch.bfloat16: KVDRO_BF16, torch.float16: KVDRO_FP16})
+    """The library, once loaded."""
+    global _lib_kv, _i32, _f32
+    if _i32 is None:
+        import torch
+        _i32, _f32 = torch.int32, torch.float32
+        _kv_types.update({torch.bfloat16: KVDRO_BF16, torch.float16: KVDRO_FP16})
+    _lib_kv = load_library()
+    return _lib_kv
 
 
 def _heads(cache: KvdroKv, name: str, a: Any, T=None, heads=None):
-    """Pointer and strides (None if contiguous) of a CUDA tensor [T][heads][head_dim] of the cache's dtype."""
+    """Pointer and strides (None if contiguous) of a CUDA tensor [T][heads][head_dim] of the cache's dtype, T and heads."""
+    try:
+        if a.is_cuda and a.dtype is cache.dtype:
+            t, h, d = a.shape
+            if d == cache.head_dim and (T is None or t == T) and (heads is None or h == heads):
+                if a.is_contiguous():
+                    return a.data_ptr(), None, t, h
+                s0, s1, s2 = a.stride()
+                if s2 == 1:
+                    # a dimension of one element has no stride of its own: any that the library takes will do
+                    return a.data_ptr(), _I2(s0 if t > 1 else 8, s1 if h > 1 else 8), t, h
+    except (AttributeError, ValueError):
+        pass
     if not getattr(a, "is_cuda", False):
         raise ValueError(f"{name} must be a CUDA tensor")
     if a.dtype is not cache.dtype:
         raise TypeError(f"{name}: expected the cache's dtype {cache.dtype}, got {a.dtype}")
-    if a.dim() != 3 or a.shape[2] != cache.head_dim or (T is not None and a.shape[0] != T) or \
-            (heads is not None and a.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(a.shape)}; the call needs "
-                         f"({'T' if T is None else T}, {'heads' if heads is None else heads}, {cache.head_dim})")
-    if a.is_contiguous():
-        return a.data_ptr(), None
-    if a.stride(2) != 1:
+    if a.dim() == 3 and a.stride(2) != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    # a dimension of one element has no stride of its own: any that the library takes will do
-    tok, head = a.stride(0) if a.shape[0] > 1 else 8, a.stride(1) if a.shape[1] > 1 else 8
-    return a.data_ptr(), _I2(tok, head)
+    raise ValueError(f"{name} has shape {tuple(a.shape)}; the call needs "
+                     f"({'T' if T is None else T}, {'heads' if heads is None else heads}, {cache.head_dim})")
 
 
 def kvdro_kv_open(ctx, k, v) -> KvdroKv:
     """Describe a page cache: ``k`` and ``v`` are CUDA tensors [n_pages][page_size][n_kv_heads][head_dim] of
     bfloat16 or float16 whose last dimension is contiguous (other strides as they are)."""
-    if not _kv_types:
-        _kv_setup()
+    _kv_setup()
     for name, a in (("k", k), ("v", v)):
         _on_device(name, a)
         if a.dtype not in _kv_types:
@@ -428,19 +444,25 @@ def kvdro_kv_plan(ctx, page_size: int, cached, new_len, held, table, ring, pool,
                   slot, pos=None, reserve=None, stream=None) -> None:
     """Pages and slots of one step (include/kvdro.h): int32 CUDA tensors; ``table`` is [B][max_pages], ``ring`` holds
     one element per page and ``slot`` one per new token."""
-    if getattr(table, "ndim", 0) != 2:
-        raise ValueError("table must be [B][max_pages]")
-    B, max_pages = table.shape
-    T = _numel(slot)
-    p = [_dev("cached", cached, "int32", B), _dev("new_len", new_len, "int32", B),
-         None if reserve is None else _dev("reserve", reserve, "int32", B), _dev("held", held, "int32", B),
-         _dev("table", table, "int32"), _dev("ring", ring, "int32"), _dev("pool", pool, "int32", 2),
-         _dev("held_out", held_out, "int32", B), _dev("pool_out", pool_out, "int32", 2),
-         _dev("q_off", q_off, "int32", B + 1), _dev("kv_len", kv_len, "int32", B), _dev("slot", slot, "int32"),
-         None if pos is None else _dev("pos", pos, "int32", T)]
-    st = load_library().kvdro_kv_plan(ctx, page_size, ring.numel(), B, max_pages, T, *p, _stream(stream))
+    lib = _lib_kv or _kv_setup()
+    B, max_pages = _table(table)
+    T, i32 = _numel(slot), _i32
+    st = lib.kvdro_kv_plan(
+        ctx, page_size, _numel(ring), B, max_pages, T, _dev("cached", cached, i32, B), _dev("new_len", new_len, i32, B),
+        None if reserve is None else _dev("reserve", reserve, i32, B), _dev("held", held, i32, B), _dev("table", table, i32),
+        _dev("ring", ring, i32), _dev("pool", pool, i32, 2), _dev("held_out", held_out, i32, B),
+        _dev("pool_out", pool_out, i32, 2), _dev("q_off", q_off, i32, B + 1), _dev("kv_len", kv_len, i32, B),
+        _dev("slot", slot, i32), None if pos is None else _dev("pos", pos, i32, T), None if stream is None else _stream(stream))
     if st:
         _check(ctx, st)
+
+
+def _table(table):
+    try:
+        B, max_pages = table.shape
+    except (AttributeError, ValueError):
+        raise ValueError("table must be [B][max_pages]") from None
+    return B, max_pages
 
 
 def _open_handle(cache: KvdroKv):
@@ -451,11 +473,11 @@ def _open_handle(cache: KvdroKv):
 
 def kvdro_kv_append(cache: KvdroKv, k, v, slot, stream=None) -> None:
     """Write the new tokens' keys and values, [T][n_kv_heads][head_dim] (last dimension contiguous), into their slots."""
-    kp, ks = _heads(cache, "k", k, None, cache.heads)
-    T = k.shape[0]
-    vp, vs = _heads(cache, "v", v, T, cache.heads)
-    st = load_library().kvdro_kv_append(_open_handle(cache), T, kp, ks, vp, vs, _dev("slot", slot, "int32", T),
-                                        _stream(stream))
+    lib = _lib_kv or _kv_setup()
+    kp, ks, T, heads = _heads(cache, "k", k, None, cache.heads)
+    vp, vs, T, heads = _heads(cache, "v", v, T, heads)
+    st = lib.kvdro_kv_append(_open_handle(cache), T, kp, ks, vp, vs, _dev("slot", slot, _i32, T),
+                             None if stream is None else _stream(stream))
     if st:
         _check(cache.ctx, st)
 
@@ -464,17 +486,14 @@ def kvdro_kv_attend(cache: KvdroKv, q, q_off, kv_len, table, out, lse=None, scal
                     window: int = 0, softcap: float = 0.0, max_q: int = 0, stream=None) -> None:
     """Attention of the new tokens ``q`` [T][n_heads][head_dim] over their requests' pages into ``out`` (and ``lse``
     [T][n_heads] float32); ``scale`` defaults to head_dim ** -0.5."""
-    qp, qs = _heads(cache, "q", q)
-    T, heads, d = q.shape
-    op, os_ = _heads(cache, "out", out, T, heads)
-    if getattr(table, "ndim", 0) != 2:
-        raise ValueError("table must be [B][max_pages]")
-    B, max_pages = table.shape
-    st = load_library().kvdro_kv_attend(
-        _open_handle(cache), B, T, heads, max_q, qp, qs, _dev("q_off", q_off, "int32", B + 1),
-        _dev("kv_len", kv_len, "int32", B), _dev("table", table, "int32"), max_pages,
-        d ** -0.5 if scale is None else scale, 1 if causal else 0, window, softcap, op, os_,
-        None if lse is None else _dev("lse", lse, "float32", T * heads), _stream(stream))
+    lib = _lib_kv or _kv_setup()
+    qp, qs, T, heads = _heads(cache, "q", q)
+    op, os_, _, _ = _heads(cache, "out", out, T, heads)
+    B, max_pages = _table(table)
+    st = lib.kvdro_kv_attend(
+        _open_handle(cache), B, T, heads, max_q, qp, qs, _dev("q_off", q_off, _i32, B + 1), _dev("kv_len", kv_len, _i32, B),
+        _dev("table", table, _i32), max_pages, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+        softcap, op, os_, None if lse is None else _dev("lse", lse, _f32, T * heads), None if stream is None else _stream(stream))
     if st:
         _check(cache.ctx, st)
 
