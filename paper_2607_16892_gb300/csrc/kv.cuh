@@ -51,6 +51,9 @@ struct AttendArgs {
     int64_t q_tok, q_head, out_tok, out_head, v_page, v_slot, v_head;  // in elements
     const int32_t *q_off, *kv_len, *table;
     int32_t B, T, heads, kv_heads, group, head_dim, n_pages, page_shift, max_pages, window;
+    uint32_t group_mul;  // a row's token: row / group = row * group_mul >> group_shift, for rows below 2^31
+    int32_t group_shift;
+    int32_t min_q, max_q;  // a launch's requests: more than min_q tokens, at most max_q
     bool half, causal;
     float scale, cap;    // cap 0: none
     float* pieces;       // sums of tiles that several CTAs share
@@ -65,6 +68,7 @@ cudaError_t kv_decode_prepare();
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 cudaError_t kv_chunk_prepare();
-cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s);
+// `after_few`: beside a launch of kv_decode for the requests of few rows, directly before it, on other scratch.
+cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s);
 
 }  // namespace kvdro

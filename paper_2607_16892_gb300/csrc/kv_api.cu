@@ -98,7 +98,7 @@ int prepare_attend(kvdro_ctx* ctx) {
     KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_chunk_prepare(), "preparing the attention kernels");
     if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
-    const size_t pieces = std::max(kvdro::kv_decode_piece_bytes(ctx->sms), kvdro::kv_chunk_piece_bytes(ctx->sms));
+    const size_t pieces = kvdro::kv_decode_piece_bytes(ctx->sms) + kvdro::kv_chunk_piece_bytes(ctx->sms);
     if (int rc = ensure(ctx, ctx->kv_pieces, pieces)) return rc;
     if (int rc = ensure(ctx, ctx->kv_joins, sizeof(kvdro::Join) * (size_t)ctx->sms)) return rc;
     const size_t tickets = 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);
@@ -299,6 +299,12 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.heads = n_heads;
     a.kv_heads = kv->heads;
     a.group = n_heads / kv->heads;
+    // p = 31 + ceil(log2 group), mul = ceil(2^p / group) < 2^32: row * mul >> p is exact for rows below 2^31, since
+    // mul * group exceeds 2^p by less than group <= 2^(p - 31).
+    a.group_shift = 31 + log2_of(a.group);
+    a.group_mul = (uint32_t)((((uint64_t)1 << a.group_shift) + a.group - 1) / a.group);
+    a.min_q = 0;
+    a.max_q = 0x7fffffff;
     a.head_dim = kv->head_dim;
     a.n_pages = kv->n_pages;
     a.page_shift = kv->page_shift;
@@ -319,9 +325,24 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
     const bool captured = capture != cudaStreamCaptureStatusNone;
     if (!captured && ctx->kv_used && ctx->kv_stream != s) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
+    // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
+    // both runs on both, each request on its own.
     const int64_t most = max_q > 0 ? max_q : T > B ? T : 1;  // new tokens of a request, as far as is known
-    if (most * a.group <= kFewRows) KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, most * a.group <= 8, ctx->sms, s), "attention kernel");
-    else KV_CUDA(kvdro::launch_kv_chunk(a, kv->maps, ctx->sms, s), "attention kernel");
+    const bool eight = a.group <= 8 && most * a.group <= 8;
+    if (most * a.group <= kFewRows) {
+        KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, eight, ctx->sms, s), "attention kernel");
+    } else {
+        const int32_t few = (a.group <= 8 ? 8 : kFewRows) / a.group;
+        const bool both = few > 0 && (max_q == 0 || (int64_t)max_q * B != T);
+        if (both) {
+            a.max_q = few;
+            KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, a.group <= 8, ctx->sms, s), "attention kernel");
+            a.min_q = few;
+            a.max_q = 0x7fffffff;
+            a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
+        }
+        KV_CUDA(kvdro::launch_kv_chunk(a, kv->maps, both, ctx->sms, s), "attention kernel");
+    }
     if (!captured) {
         KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
         ctx->kv_stream = s;

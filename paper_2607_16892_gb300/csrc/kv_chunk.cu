@@ -40,8 +40,8 @@ using ChunkLine = Line<kRows, kKeys, kKeys>;
 struct Shared {
     uint64_t kv_full[10], kv_empty[10], v_clean[10];
     uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2], done;
-    int64_t base, warp_sum[kThreads / 32];  // where the requests of thread `found` begin in the line
-    int found, dead;
+    Stretch<kThreads> part;
+    int dead;
     uint32_t tmem;
     uint32_t skip[kNotes];  // by block: 16-slot slices whose page number is none
     int2 odd[2][kNotes];    // by looking warp and piece: first and last block with elements replaced, first > last if none
@@ -161,29 +161,9 @@ __device__ __forceinline__ void wait(uint64_t& bar, uint32_t parity, int& dead) 
     if (!mbar_try(smem_u32(&bar), parity)) wait_slow(smem_u32(&bar), parity, &dead);
 }
 
-// The pieces of this CTA's stretch, in order: each role walks them for itself.
-struct Walk {
-    ChunkLine& line;
-    Cursor<ChunkLine> at;
-    int left;      // blocks of the stretch from this piece on
-    int p0, p1;    // the piece: blocks of the tile
-    int piece = 0;
-
-    __device__ __forceinline__ Walk(ChunkLine& l, const Shared& s, int per, int64_t u0, int64_t u1) : line(l) {
-        at.seek(line, s.found * per, s.base, u0);
-        left = (int)(u1 - u0);
-        p0 = (int)(u0 - at.start);
-        p1 = min(at.t.blocks, p0 + left);
-    }
-    __device__ __forceinline__ bool next() {
-        left -= p1 - p0;
-        if (left == 0) return false;
-        at.next(line);
-        p0 = 0;
-        p1 = min(at.t.blocks, left);
-        piece++;
-        return true;
-    }
+// What the roles, each walking the pieces for itself, ask about one.
+struct Pieces : Walk<ChunkLine> {
+    using Walk<ChunkLine>::Walk;
     // Rows of a half, and its blocks in the piece: [x, y), empty if no row sees any.
     __device__ __forceinline__ int half_rows(int i) const {
         return min(kHalfRows, at.r.rows - at.rt * kRows - i * kHalfRows);
@@ -191,15 +171,15 @@ struct Walk {
     __device__ __forceinline__ int2 half_blocks(int i) const {
         const int rows = half_rows(i);
         if (rows <= 0) return make_int2(0, 0);
-        const int first = at.rt * kRows + i * kHalfRows, g = line.a.group;
-        const int hi = line.seen(at.r, (first + rows - 1) / g).y, lo = min(line.seen(at.r, first / g).x, hi);
+        const int first = at.rt * kRows + i * kHalfRows;
+        const int hi = line.seen(at.r, line.token(first + rows - 1)).y, lo = min(line.seen(at.r, line.token(first)).x, hi);
         const int b0 = max(p0, (lo - at.t.lo) / kKeys), b1 = min(p1, (hi - at.t.lo + kKeys - 1) / kKeys);
         return make_int2(b0, max(b0, b1));
     }
     // Positions that every row of the tile sees.
     __device__ __forceinline__ int2 all_see() const {
         const int first = at.rt * kRows, last = min(first + kRows, at.r.rows) - 1;
-        return make_int2(line.seen(at.r, last / line.a.group).x, line.seen(at.r, first / line.a.group).y);
+        return make_int2(line.seen(at.r, line.token(last)).x, line.seen(at.r, line.token(first)).y);
     }
     __device__ __forceinline__ bool edge(int blk, int2 all) const {
         const int j0 = at.t.lo + blk * kKeys;
@@ -209,7 +189,7 @@ struct Walk {
 
 // Q of a half into shared memory: rows of 16-byte chunks, sixteen (or eight) lanes to a row.
 template <int D>
-__device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int half, char* to, int tid) {
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Pieces& w, int half, char* to, int tid) {
     constexpr int C = D / 8, kRowsAtOnce = kHalfRows / C, N = kHalfRows / kRowsAtOnce;
     const int rows = w.half_rows(half), c = tid % C;
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
@@ -219,7 +199,7 @@ __device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int h
         const int r = tid / C + i * kRowsAtOnce;
         x[i] = make_uint4(0, 0, 0, 0);
         if (r < rows) {
-            const int row = w.at.rt * kRows + half * kHalfRows + r, tok = row / a.group, g = row - tok * a.group;
+            const int row = w.at.rt * kRows + half * kHalfRows + r, tok = w.line.token(row), g = row - tok * a.group;
             x[i] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.at.r.q0 + tok) * a.q_tok +
                                                    (int64_t)(w.at.h * a.group + g) * a.q_head + c * 8);
         }
@@ -264,48 +244,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (warp == 8) tc_alloc(smem_u32(&sh.tmem));
 
-    // The line's length, and where each thread's requests begin in it.
-    const int per = (a.B + kThreads - 1) / kThreads;
-    int64_t mine = 0;
-    for (int b = min(tid * per, a.B), b1 = min(b + per, a.B); b < b1; b++) mine += line.cost(line.request(b));
-    int64_t incl = mine;
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(~0u, incl, o);
-        if (lane >= o) incl += x;
-    }
-    if (lane == 31) sh.warp_sum[warp] = incl;
+    if (tid == 0) a.joins[blockIdx.x].last = -1;
+    sh.part.find(line, s_raw);
+    clear_rest<D, kThreads>(a);
+    fence_proxy_async();  // the tiles' memory served as scratch
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    int64_t before = 0, total = 0;
-    for (int w = 0; w < kThreads / 32; w++) {
-        if (w == warp) before = total;
-        total += sh.warp_sum[w];
-    }
-    before += incl - mine;
-    const int64_t share = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
-    const int64_t u0 = blockIdx.x * share, u1 = min(u0 + share, total);
-    if (u0 >= before && u0 < before + mine) {
-        sh.found = tid;
-        sh.base = before;
-    }
-    if (tid == 0) a.joins[blockIdx.x].last = -1;
-    __syncthreads();
     const uint32_t tmem = sh.tmem;
 
-    {  // tokens of no request: out = 0
-        const int end = max(0, min(a.q_off[a.B], a.T));
-        const int64_t vecs = (int64_t)(a.T - end) * a.heads * (D / 8);
-        for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < vecs; i += (int64_t)gridDim.x * kThreads) {
-            const int64_t row = i / (D / 8);
-            const int t = end + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
-            *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
-            if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
-        }
-    }
-
     bool range = false;
-    if (u0 < u1) {
+    if (!sh.part.empty()) {
         if (warp < 8) {
             // ---------------------------------------------------------- weights and results of a half
             asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -318,9 +267,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             char* const q_to = smem_ptr + half * kTile;
             uint32_t n_s = 0, n_o = 0;  // products awaited so far
             int note = 0;               // blocks of the stretch before this piece
-            Walk w(line, sh, per, u0, u1);
-            bool loaded = false, more = true;
-            while (more) {
+            Pieces w(line, sh.part);
+            bool loaded = false;
+            while (w.more) {
                 const int rows = w.half_rows(half);
                 const int2 blocks = w.half_blocks(half);
                 if (!loaded && blocks.x < blocks.y) {
@@ -329,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(smem_u32(&sh.q_full[half]));
                 }
                 loaded = false;
-                const int row = w.at.rt * kRows + half * kHalfRows + row_in, tok = row / a.group;
+                const int row = w.at.rt * kRows + half * kHalfRows + row_in, tok = line.token(row);
                 const bool valid = row_in < rows;
                 const int2 see = valid ? line.seen(w.at.r, tok) : make_int2(0, 0x7fffffff);
                 // Blocks inside [whole_lo, whole_hi) are seen whole by every row of the warp.
@@ -423,10 +372,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     n_o++;
                 }
                 // The next piece's Q while the last product runs.
-                const Walk cur = w;
+                const Pieces cur = w;
                 note += cur.p1 - cur.p0;
-                more = w.next();
-                if (more && blocks.x < blocks.y) {
+                w.next();
+                if (w.more && blocks.x < blocks.y) {
                     const int2 nb = w.half_blocks(half);
                     if (nb.x < nb.y) {
                         load_q<D>(a, w, half, q_to, row_in);
@@ -442,12 +391,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc_fence_after();
                 }
                 if (rows <= 0) continue;
-                const int64_t c0 = cur.at.start / share, c1 = (cur.at.start + cur.at.t.blocks - 1) / share;
                 const int cta = blockIdx.x, g = row - tok * a.group, h = cur.at.h * a.group + g;
                 const int64_t t = cur.at.r.q0 + tok;
-                const bool whole = c0 == c1;
+                const bool whole = cur.whole(sh.part), begins = cur.begins(sh.part);
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                float* const piece = a.pieces + (int64_t)(2 * cta + (c0 == cta)) * Sh::kPieceFloats;
+                float* const piece = a.pieces + (int64_t)(2 * cta + begins) * Sh::kPieceFloats;
                 const int prow = half * kHalfRows + row_in;
                 int2 odd = make_int2(1, 0);
                 const int2 all = cur.all_see();
@@ -507,18 +455,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                         reinterpret_cast<float2*>(piece + kRows * D)[prow] = make_float2(m, l);
                     }
                 }
-                if (!whole && c0 == cta && row_in == 0 && half == 0) {
+                if (!whole && begins && row_in == 0 && half == 0) {
                     Join& j = a.joins[cta];
                     j.b = cur.at.b;
                     j.rt = cur.at.rt;
                     j.h = cur.at.h;
-                    j.last = (int)c1;
+                    j.last = (int)((cur.at.start + cur.at.t.blocks - 1) / sh.part.share);
                 }
                 tc_fence_before();
             }
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-            Walk w(line, sh, per, u0, u1);
+            Pieces w(line, sh.part);
             int stage = 0;
             uint32_t round = 0;  // of the ring
             auto advance = [&] {
@@ -561,8 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     n_p[i] += act_prev[i];
                 };
-                bool more = true;
-                while (more) {
+                while (w.more) {
                     int2 hb[2] = {w.half_blocks(0), w.half_blocks(1)};
                     const int2 all = w.all_see();
                     for (int blk = w.p0; blk < w.p1; blk++) {
@@ -604,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         advance();
                     }
-                    more = w.next();
+                    w.next();
                 }
                 issue_o(0, false);
                 issue_o(1, true);
@@ -616,11 +563,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
             } else if (warp == 9) {
                 // ------------------------------------------------------ copies
-                bool ok = true, more = true;
+                bool ok = true;
                 uint32_t turns = 0;
                 int note = 0;
                 const int n = kKeys >> a.page_shift;
-                while (more && ok) {
+                while (w.more && ok) {
                     for (int blk = w.p0; blk < w.p1 && ok; blk++, note++) {
                         const int j = w.at.t.lo + blk * kKeys + (lane << a.page_shift);
                         int page = a.n_pages;  // past the last page: zeros
@@ -657,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             advance();
                         }
                     }
-                    more = w.next();
+                    w.next();
                 }
                 if (!ok) {  // what is in flight must land before the CTA's memory is given away
                     const uint32_t left = turns < (uint32_t)kStages ? turns : kStages;
@@ -669,11 +616,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             } else {
                 // ------------------------------------------------------ V that not every row sees
-                bool more = true;
                 const int part = warp - 10;
-                while (more) {
+                while (w.more) {
                     const int2 all = w.all_see();
-                    const int seen_lo = line.seen(w.at.r, w.at.rt * kRows / a.group).x;
+                    const int seen_lo = line.seen(w.at.r, line.token(w.at.rt * kRows)).x;
                     int2 odd = make_int2(0x7fffffff, -1);
                     if (lane == 0) sh.odd[part][w.piece & (kNotes - 1)] = odd;
                     for (int blk = w.p0; blk < w.p1; blk++) {
@@ -711,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             advance();
                         }
                     }
-                    more = w.next();
+                    w.next();
                 }
             }
         }
@@ -722,6 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     if (tid == 0 && sh.dead) atomicOr(a.err, kKvErrTimeout);
     if (warp == 8) tc_free(tmem);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // a launch for few rows before this one, which ran beside it, is done
 }
 
 // Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
@@ -760,7 +707,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int tok = row / a.group, h = j.h * a.group + row - tok * a.group;
+    const int tok = line.token(row), h = j.h * a.group + row - tok * a.group;
     const int64_t t = r.q0 + tok;
     uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + part * (D / 4));
 #pragma unroll
@@ -776,18 +723,22 @@ cudaError_t prepare() {
 }
 
 template <bool H, int D>
-cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
-    k_kv_chunk<H, D><<<sms, kThreads, Shape<D>::kSmem, s>>>(a, maps.k, maps.v);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute early[1];  // set up while the first kernel ends
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s) {
+    cudaLaunchAttribute early[1];  // starts while the launch before ends
     early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(sms, kRows / kJoinRows);
-    c.blockDim = dim3(kJoinThreads);
+    c.gridDim = dim3(sms);
+    c.blockDim = dim3(kThreads);
+    c.dynamicSmemBytes = Shape<D>::kSmem;
     c.stream = s;
     c.attrs = early;
+    c.numAttrs = after_few ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&c, k_kv_chunk<H, D>, a, maps.k, maps.v);
+    if (e != cudaSuccess) return e;
+    c.gridDim = dim3(sms, kRows / kJoinRows);
+    c.blockDim = dim3(kJoinThreads);
+    c.dynamicSmemBytes = 0;
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a);
 }
@@ -804,9 +755,9 @@ cudaError_t kv_chunk_prepare() {
     return prepare<true, 128>();
 }
 
-cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, int sms, cudaStream_t s) {
-    if (a.half) return a.head_dim == 128 ? launch<true, 128>(a, maps, sms, s) : launch<true, 64>(a, maps, sms, s);
-    return a.head_dim == 128 ? launch<false, 128>(a, maps, sms, s) : launch<false, 64>(a, maps, sms, s);
+cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s) {
+    if (a.half) return a.head_dim == 128 ? launch<true, 128>(a, maps, after_few, sms, s) : launch<true, 64>(a, maps, after_few, sms, s);
+    return a.head_dim == 128 ? launch<false, 128>(a, maps, after_few, sms, s) : launch<false, 64>(a, maps, after_few, sms, s);
 }
 
 }  // namespace kvdro

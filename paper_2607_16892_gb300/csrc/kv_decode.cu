@@ -29,6 +29,7 @@ struct Ring {  // a stage: K or V of a slice
     static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? 4 : 2);  // per SM
     static constexpr int kBytes = kSlice * D * 2, kStages = D == 128 ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6);
     static constexpr int kSmem = kWarps * kStages * kBytes + 1024;
+    static_assert(Stretch<kThreads>::kScratch <= kSmem, "the ring is scratch first");
 };
 // A piece in global memory: rows of D sums, then their maxima and sums of weights.
 template <int D>
@@ -79,63 +80,30 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     using DecodeLine = Line<kRows, kKeys, kSlice>;
     constexpr int kRowFloats = D + 4;  // of a row of sums in shared memory: no bank conflicts
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
-    __shared__ int64_t s_base, s_warp_sum[kWarps];  // where the requests of thread `s_found` begin in the line
+    __shared__ Stretch<kThreads> s_part;
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
-    __shared__ int s_found, s_last;
+    __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(s_raw), ring = ((raw + 1023) & ~1023u) + warp * kStages * kStage;
     char* const ring_ptr = s_raw + (ring - raw);
     DecodeLine line(a);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // a launch for many rows may fill SMs that this one leaves
 
     if (lane < kStages) mbar_init(smem_u32(&s_bar[warp][lane]), 1);
     fence_mbar_init();
 
-    // The line's length, and where each thread's requests begin in it.
-    const int per = (a.B + kThreads - 1) / kThreads;
-    int64_t mine = 0;
-    for (int b = min(tid * per, a.B), b1 = min(b + per, a.B); b < b1; b++) mine += line.cost(line.request(b));
-    int64_t incl = mine;
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(~0u, incl, o);
-        if (lane >= o) incl += x;
-    }
-    if (lane == 31) s_warp_sum[warp] = incl;
+    s_part.find(line, s_raw);
+    clear_rest<D, kThreads>(a);
+    fence_proxy_async();  // the ring served as scratch
     __syncthreads();
-    int64_t before = 0, total = 0;
-    for (int w = 0; w < kWarps; w++) {
-        if (w == warp) before = total;
-        total += s_warp_sum[w];
-    }
-    before += incl - mine;
-    const int64_t share = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x);
-    const int64_t u0 = blockIdx.x * share, u1 = min(u0 + share, total);
-    if (u0 >= before && u0 < before + mine) {
-        s_found = tid;
-        s_base = before;
-    }
-    __syncthreads();
-
-    // Tokens of no request: out = 0.
-    {
-        const int end = max(0, min(a.q_off[a.B], a.T));
-        const int64_t vecs = (int64_t)(a.T - end) * a.heads * (D / 8);
-        for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < vecs; i += (int64_t)gridDim.x * kThreads) {
-            const int64_t row = i / (D / 8);
-            const int t = end + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
-            *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
-            if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
-        }
-    }
-    if (u0 >= u1) {
+    if (s_part.empty()) {
         if (line.bad && tid == 0) atomicOr(a.err, kKvErrRange);
         return;
     }
 
     // Units in the order K, V of a slice, K, V of the next.
-    Cursor<DecodeLine> in, at;  // of the copies, and of the sums
-    in.seek(line, s_found * per, s_base, u0);
-    at = in;
-    int in_blk = (int)(u0 - in.start), in_left = (int)(u1 - u0);
+    Walk<DecodeLine> in(line, s_part), w = in;  // of the copies, and of the sums
+    int in_blk = in.p0;
     bool in_v = false;
 
     // Page numbers of this warp's slices of 32 blocks, one per lane; a slice has two pages if they have 16 slots.
@@ -146,17 +114,17 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     uint32_t gaps = 0;               // by stage, two bits: 16 positions whose page number is none
     auto fetch = [&](int stage) {
         filled &= ~(1u << stage);
-        if (in_left == 0) return;
-        if (in.b != pg_b || in.rt != pg_rt || (in_blk >> 5) != pg_blk) {
-            pg_b = in.b;
-            pg_rt = in.rt;
+        if (!in.more) return;
+        if (in.at.b != pg_b || in.at.rt != pg_rt || (in_blk >> 5) != pg_blk) {
+            pg_b = in.at.b;
+            pg_rt = in.at.rt;
             pg_blk = in_blk >> 5;
-            const int j = in.t.lo + ((in_blk & ~31) + lane) * kKeys + warp * kSlice;
+            const int j = in.at.t.lo + ((in_blk & ~31) + lane) * kKeys + warp * kSlice;
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 pg[i] = -1;
-                if (j + 16 * i < in.t.hi) {
-                    const int page = a.table[(int64_t)in.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
+                if (j + 16 * i < in.at.t.hi) {
+                    const int page = a.table[(int64_t)in.at.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
                     if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
                     else range = true;
                 }
@@ -166,23 +134,22 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
         gaps = (gaps & ~(3u << 2 * stage)) | ((p0 < 0 ? 1u : 0u) | (p1 < 0 ? 2u : 0u)) << 2 * stage;
         if (p0 >= 0 || p1 >= 0) {
             if (lane == 0) {
-                const int slot = (in.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1);
+                const int slot = (in.at.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1);
                 const uint32_t bar = smem_u32(&s_bar[warp][stage]), to = ring + stage * kStage;
                 const CUtensorMap* const map = in_v ? &vmap : &kmap;
                 mbar_expect(bar, kStage);
 #pragma unroll
                 for (int d = 0; d < D / 64; d++) {  // a page that is none reads as zeros
-                    load_box(to + d * (kSlice * 128), map, d * 64, slot, in.h, p0 >= 0 ? p0 : a.n_pages, bar);
-                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, in.h, p1 >= 0 ? p1 : a.n_pages, bar);
+                    load_box(to + d * (kSlice * 128), map, d * 64, slot, in.at.h, p0 >= 0 ? p0 : a.n_pages, bar);
+                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, in.at.h, p1 >= 0 ? p1 : a.n_pages, bar);
                 }
             }
             filled |= 1u << stage;
         }
         in_v = !in_v;
         if (in_v) return;
-        in_left--;
-        if (++in_blk == in.t.blocks && in_left) {
-            in.next(line);
+        if (++in_blk == in.p1) {
+            in.next();
             in_blk = 0;
         }
     };
@@ -196,8 +163,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     int2 see[NR][2];
     int2 all_see, any_see;  // positions that every row of the tile sees, and that some row does
     bool dead = false;
-    int stage = 0, blk = (int)(u0 - at.start);
-    bool fresh = true;
+    int stage = 0;
 
     // The slice in `stage`, once it is there; false if there is none.
     auto ready = [&] {
@@ -211,14 +177,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
         stage = stage + 1 == kStages ? 0 : stage + 1;
     };
 
-    for (int64_t u = u0; u < u1; u++) {
-        if (fresh) {  // a tile begins here, or this CTA's piece of it
-            fresh = false;
+    while (w.more) {
+        Cursor& at = w.at;
+        {  // a tile begins here, or this CTA's piece of it
             const int first = at.rt * kRows, rows = min(kRows, at.r.rows - first);
 #pragma unroll
             for (int n = 0; n < NR; n++) {
                 {
-                    const int r = first + min(8 * n + (lane >> 2), rows - 1), tok = r / a.group, g = r - tok * a.group;
+                    const int r = first + min(8 * n + (lane >> 2), rows - 1), tok = line.token(r), g = r - tok * a.group;
                     const uint16_t* const q = a.q + (int64_t)(at.r.q0 + tok) * a.q_tok + (int64_t)(at.h * a.group + g) * a.q_head + 2 * (lane & 3);
 #pragma unroll
                     for (int k = 0; k < KS; k++) {
@@ -228,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                 }
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    see[n][i] = line.seen(at.r, (first + min(8 * n + 2 * (lane & 3) + i, rows - 1)) / a.group);
+                    see[n][i] = line.seen(at.r, line.token(first + min(8 * n + 2 * (lane & 3) + i, rows - 1)));
                     m[n][i] = -INFINITY;
                     l[n][i] = 0.f;
                 }
@@ -237,10 +203,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
 #pragma unroll
                     for (int i = 0; i < 4; i++) o[n][d][i] = 0.f;
             }
-            const int2 s0 = line.seen(at.r, first / a.group), s1 = line.seen(at.r, (first + rows - 1) / a.group);
+            const int2 s0 = line.seen(at.r, line.token(first)), s1 = line.seen(at.r, line.token(first + rows - 1));
             all_see = make_int2(s1.x, s0.y);
             any_see = make_int2(s0.x, s1.y);
         }
+        for (int blk = w.p0; blk < w.p1; blk++) {
         const int j0 = at.t.lo + blk * kKeys + warp * kSlice;
         const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || (gaps >> 2 * stage & 3);
         const uint32_t gap = gaps >> 2 * stage & 3;
@@ -396,8 +363,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             }
         }
 
-        blk++;
-        if (blk == at.t.blocks || u + 1 == u1) {  // the end of a tile, or of this CTA's piece of it
+        if (blk + 1 < w.p1) {
+            __syncwarp();
+            advance();
+        }
+        }
+        {  // the end of a tile, or of this CTA's piece of it
             const int first = at.rt * kRows, rows = min(kRows, at.r.rows - first);
 #pragma unroll
             for (int n = 0; n < NR; n++)
@@ -411,11 +382,10 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                     }
                 }
             __syncthreads();
-            const int64_t c0 = at.start / share, c1 = (at.start + at.t.blocks - 1) / share;  // CTAs with a piece
-            const int cta = blockIdx.x;
-            float* const piece = a.pieces + (int64_t)(2 * cta + (c0 == cta)) * kPieceFloats<D>;
+            const bool whole = w.whole(s_part);
+            float* const piece = a.pieces + (int64_t)(2 * blockIdx.x + w.begins(s_part)) * kPieceFloats<D>;
             auto row_out = [&](int r, int c, float4 x, float to, float sum) {
-                const int tok = (first + r) / a.group, g = first + r - tok * a.group;
+                const int tok = line.token(first + r), g = first + r - tok * a.group;
                 const int64_t t = at.r.q0 + tok;
                 const int h = at.h * a.group + g;
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -453,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                         x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
                         sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
                     }
-                    if (c0 == c1) {
+                    if (whole) {
                         row_out(r, c, x, to, sum);
                     } else {
                         *reinterpret_cast<float4*>(piece + r * D + c) = x;
@@ -462,7 +432,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                 }
             }
             __syncthreads();
-            if (c0 != c1) {
+            if (!whole) {
+                const int64_t c0 = at.start / s_part.share, c1 = (at.start + at.t.blocks - 1) / s_part.share;  // CTAs with a piece
                 if (tid == 0) {
                     __threadfence();
                     const unsigned arrived = atomicAdd(a.tickets + c0, 1u);
@@ -494,16 +465,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                     }
                 }
             }
+            w.next();
             fence_proxy_async();
             __syncwarp();
-            if (u + 1 < u1) {
-                at.next(line);
-                blk = 0;
-                fresh = true;
-            }
+            advance();
         }
-        __syncwarp();
-        advance();
     }
     if (dead) {  // what is still in flight must land before the CTA's memory is given away
         for (int s = 0; s < kStages; s++)

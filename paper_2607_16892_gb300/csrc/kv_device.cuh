@@ -97,23 +97,26 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 
 // The requests' rows are dealt to tiles of `kRows` rows (a token's query heads of one key head are neighbours), and a tile's
 // positions to blocks of `kKeys`.  All blocks of all tiles stand in one line -- request, row tile, key head, block --
-// and each CTA takes an equal stretch of it, so that long contexts are shared by many CTAs and short ones share a CTA.
+// with one more place behind a tile's last block for what a tile costs beside its blocks (its Q, its results), and each
+// CTA takes an equal stretch of the line, so that long contexts are shared by many CTAs and short ones share a CTA.
 // A tile that crosses from one stretch into the next is joined from its pieces.
 struct Request {
-    int q0, n, rows, kv;  // first token, tokens, rows (tokens inside T times the group), positions
+    int q0, n, rows, kv;  // first token, tokens, rows (tokens inside T times the group; 0: not this launch's), positions
 };
 
 struct Tile {
-    int lo, hi, blocks;  // positions [lo, hi), lo on a slice of 16
+    int lo, hi, blocks;  // positions [lo, hi), lo aligned
 };
 
-template <int kRows, int kKeys, int kAlign>
+template <int kRowsOf, int kKeysOf, int kAlign>
 struct Line {
+    static constexpr int kRows = kRowsOf, kKeys = kKeysOf;
     const AttendArgs& a;
     bool bad = false;
 
     __device__ __forceinline__ explicit Line(const AttendArgs& args) : a(args) {}
 
+    __device__ __forceinline__ int token(int row) const { return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift); }
     __device__ __forceinline__ Request request(int b) {
         Request r;
         r.q0 = a.q_off[b];
@@ -125,7 +128,7 @@ struct Line {
             return r;
         }
         r.n = q1 - r.q0;
-        r.rows = max(0, min(q1, a.T) - r.q0) * a.group;
+        r.rows = r.n > a.min_q && r.n <= a.max_q ? max(0, min(q1, a.T) - r.q0) * a.group : 0;
         if (r.kv < 0 || (int64_t)r.kv > ((int64_t)a.max_pages << a.page_shift)) {
             bad = true;
             r.kv = 0;
@@ -142,48 +145,69 @@ struct Line {
     __device__ __forceinline__ Tile tile(const Request& r, int rt) const {
         const int first = rt * kRows, last = min(first + kRows, r.rows) - 1;
         Tile t;
-        t.hi = seen(r, last / a.group).y;
-        t.lo = min(seen(r, first / a.group).x, t.hi) & ~(kAlign - 1);
+        t.hi = seen(r, token(last)).y;
+        t.lo = min(seen(r, token(first)).x, t.hi) & ~(kAlign - 1);
         t.blocks = max(1, (t.hi - t.lo + kKeys - 1) / kKeys);
         return t;
     }
     __device__ __forceinline__ int row_tiles(const Request& r) const { return (r.rows + kRows - 1) / kRows; }
-    __device__ __forceinline__ int64_t cost(const Request& r) const {
+    // Places of row tiles first, first + step, ...
+    __device__ __forceinline__ int64_t cost(const Request& r, int first = 0, int step = 1) const {
         int64_t c = 0;
-        for (int rt = 0, n = row_tiles(r); rt < n; rt++) c += tile(r, rt).blocks;
+        for (int rt = first, n = row_tiles(r); rt < n; rt += step) c += tile(r, rt).blocks + 1;
         return c * a.kv_heads;
     }
 };
 
-// A place in the line: a tile and where its blocks begin.
-template <class L>
+__device__ __forceinline__ int64_t warp_sum(int64_t x) {
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    return x;
+}
+
+// A place in the line: a tile and where it begins.
 struct Cursor {
     Request r;
     Tile t;
     int b, rt, h;
-    int64_t start;  // the tile's first block in the line
+    int64_t start;
 
-    // The tile that holds block `u`, walking from request `b0`, whose blocks begin at `base` (u lies in it or later).
-    __device__ __forceinline__ void seek(L& line, int b0, int64_t base, int64_t u) {
+    // The tile that holds place `u`, walking from request `b0`, whose places begin at `base` (u lies in it or later).  By a
+    // whole warp.
+    template <class L>
+    __device__ __forceinline__ void seek(L& line, int b0, int64_t base, int64_t u, int lane) {
         b = b0;
         for (;; b++) {
             r = line.request(b);
-            const int64_t c = line.cost(r);
+            const int64_t c = warp_sum(line.cost(r, lane, 32));
             if (u < base + c || b + 1 >= line.a.B) break;
             base += c;
         }
-        for (rt = 0;; rt++) {
-            t = line.tile(r, rt);
-            const int64_t c = (int64_t)t.blocks * line.a.kv_heads;
-            if (u < base + c || rt + 1 >= line.row_tiles(r)) break;
-            base += c;
+        for (rt = 0;; rt += 32) {  // 32 row tiles at a time
+            const bool there = rt + lane < line.row_tiles(r);
+            const int64_t mine = there ? (int64_t)(line.tile(r, rt + lane).blocks + 1) * line.a.kv_heads : 0;
+            int64_t incl = mine;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(~0u, incl, o);
+                if (lane >= o) incl += x;
+            }
+            const unsigned at = __ballot_sync(~0u, there && u < base + incl);
+            if (at) {
+                const int l = __ffs(at) - 1;
+                base += __shfl_sync(~0u, incl - mine, l);
+                rt += l;
+                break;
+            }
+            base += __shfl_sync(~0u, incl, 31);
+            if (rt + 32 >= line.row_tiles(r)) break;
         }
-        h = (int)((u - base) / t.blocks);
-        start = base + (int64_t)h * t.blocks;
+        t = line.tile(r, rt);
+        h = (int)((u - base) / (t.blocks + 1));
+        start = base + (int64_t)h * (t.blocks + 1);
     }
     // On to the next tile (there is one).
+    template <class L>
     __device__ __forceinline__ void next(L& line) {
-        start += t.blocks;
+        start += t.blocks + 1;
         if (++h < line.a.kv_heads) return;
         h = 0;
         if (++rt >= line.row_tiles(r)) {
@@ -196,6 +220,135 @@ struct Cursor {
         t = line.tile(r, rt);
     }
 };
+
+// A CTA's stretch of the line, in shared memory.
+template <int kThreads>
+struct Stretch {
+    static constexpr int kScratch = 8 * kThreads + 2 * kKvMaxRequests;  // bytes that find() needs
+    int64_t warp_sums[kThreads / 32];
+    int many, found;
+    int64_t base;
+    Cursor first;
+    int64_t u0, u1, share;
+
+    // Finds it.  By all threads; `scratch`: shared memory that nothing else uses meanwhile.
+    template <class L>
+    __device__ __forceinline__ void find(L& line, char* scratch) {
+        constexpr int kFew = 4;  // row tiles that one thread counts by itself
+        const AttendArgs& a = line.a;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = (a.B + kThreads - 1) / kThreads;
+        unsigned long long* const more = reinterpret_cast<unsigned long long*>(scratch);  // places of a thread's requests of many row tiles
+        uint16_t* const list = reinterpret_cast<uint16_t*>(more + kThreads);               // those requests
+        if (tid == 0) many = 0;
+        more[tid] = 0;
+        __syncthreads();
+        int64_t mine = 0;
+        for (int b = min(tid * per, a.B), b1 = min(b + per, a.B); b < b1; b++) {
+            const Request r = line.request(b);
+            if (line.row_tiles(r) <= kFew) mine += line.cost(r);
+            else list[atomicAdd(&many, 1)] = (uint16_t)b;
+        }
+        __syncthreads();
+        for (int i = warp; i < many; i += kThreads / 32) {
+            const int64_t c = warp_sum(line.cost(line.request(list[i]), lane, 32));
+            if (lane == 0) atomicAdd(&more[list[i] / per], (unsigned long long)c);
+        }
+        __syncthreads();
+        mine += (int64_t)more[tid];
+        int64_t incl = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(~0u, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        int64_t before = 0, total = 0;
+        for (int w = 0; w < kThreads / 32; w++) {
+            if (w == warp) before = total;
+            total += warp_sums[w];
+        }
+        before += incl - mine;
+        const int64_t each = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x), at = blockIdx.x * each;
+        if (tid == 0) {
+            share = each;
+            u0 = at;
+            u1 = min(at + each, total);
+        }
+        if (at >= before && at < before + mine) {
+            found = tid;
+            base = before;
+        }
+        __syncthreads();
+        if (warp == 0 && at < total) {
+            Cursor c;
+            c.seek(line, found * per, base, at, lane);
+            if (lane == 0) first = c;
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool empty() const { return u0 >= u1; }
+};
+
+// The pieces of a stretch, in order: the part of each tile's blocks [p0, p1) that lies in it.
+template <class L>
+struct Walk {
+    L& line;
+    Cursor at;
+    int left;    // places of the stretch from this tile on
+    int used;    // of them this tile's
+    int p0, p1;
+    int piece = 0;
+    bool more;   // there is a piece
+
+    template <class S>
+    __device__ __forceinline__ Walk(L& l, const S& s) : line(l) {
+        at = s.first;
+        left = (int)(s.u1 - s.u0);
+        const int from = (int)(s.u0 - at.start);
+        p0 = min(from, at.t.blocks);
+        used = min(at.t.blocks + 1 - from, left);
+        p1 = min(from + used, at.t.blocks);
+        more = true;
+        if (p0 == p1) {  // the place behind the last block alone
+            next();
+            piece = 0;
+        }
+    }
+    __device__ __forceinline__ void next() {
+        left -= used;
+        piece++;
+        if (left == 0) {
+            more = false;
+            return;
+        }
+        at.next(line);
+        p0 = 0;
+        used = min(at.t.blocks + 1, left);
+        p1 = min(used, at.t.blocks);
+    }
+    // Whether the tile begins in this stretch, and whether it lies in it whole.
+    template <class S>
+    __device__ __forceinline__ bool begins(const S& s) const {
+        return at.start >= s.u0;
+    }
+    template <class S>
+    __device__ __forceinline__ bool whole(const S& s) const {
+        return at.start >= s.u0 && at.start + at.t.blocks <= s.u1;
+    }
+};
+
+// Tokens of no request: out = 0.
+template <int D, int kThreads>
+__device__ __forceinline__ void clear_rest(const AttendArgs& a) {
+    const int end = max(0, min(a.q_off[a.B], a.T));
+    const int64_t vecs = (int64_t)(a.T - end) * a.heads * (D / 8);
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vecs; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / (D / 8);
+        const int t = end + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
+        *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
+        if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
+    }
+}
 
 }  // namespace kv
 }  // namespace kvdro
