@@ -109,6 +109,16 @@ __device__ __forceinline__ void tc_load16(uint32_t (&r)[16], uint32_t at) {
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(at));
 }
+__device__ __forceinline__ void tc_store32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
 __device__ __forceinline__ void tc_store16(uint32_t at, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
@@ -187,32 +197,62 @@ struct Pieces : Walk<ChunkLine> {
     }
 };
 
-// Q of a half into shared memory: rows of 16-byte chunks, sixteen (or eight) lanes to a row.
+// Q of a half into shared memory, by its four warps: rows of 16-byte chunks, sixteen (or eight) lanes to a row; arrives at
+// `bar` (128 arrivals) once it is there, while the threads go on.  Rows beyond the half's are zero; a negative scale turns Q's
+// sign, so that the largest score is the largest product.
 template <int D>
-__device__ __forceinline__ void load_q(const AttendArgs& a, const Pieces& w, int half, char* to, int tid) {
-    constexpr int C = D / 8, kRowsAtOnce = kHalfRows / C, N = kHalfRows / kRowsAtOnce;
-    const int rows = w.half_rows(half), c = tid % C;
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    uint4 x[N];
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int r = tid / C + i * kRowsAtOnce;
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows) {
-            const int row = w.at.rt * kRows + half * kHalfRows + r, tok = w.line.token(row), g = row - tok * a.group;
-            x[i] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.at.r.q0 + tok) * a.q_tok +
-                                                   (int64_t)(w.at.h * a.group + g) * a.q_head + c * 8);
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Pieces& w, int half, uint32_t to, int tid, uint32_t bar) {
+    constexpr int C = D / 8, kAtOnce = kHalfRows / C;
+    const int rows = w.half_rows(half), c = tid % C, row0 = w.at.rt * kRows + half * kHalfRows;
+    const uint32_t at = to + (c >> 3) * (kHalfRows * 128);
+    const uint16_t* const q = a.q + (int64_t)w.at.r.q0 * a.q_tok + (int64_t)w.at.h * a.group * a.q_head + c * 8;
+#pragma unroll 4
+    for (int r = tid / C; r < kHalfRows; r += kAtOnce) {
+        const int row = row0 + min(r, rows - 1), tok = w.line.token(row), g = row - tok * a.group;
+        const uint16_t* const from = q + (int64_t)tok * a.q_tok + (int64_t)g * a.q_head;
+        const uint32_t dst = at + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+        if (a.scale >= 0.f) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(r < rows ? 16 : 0) : "memory");
+        } else {
+            uint4 x = *reinterpret_cast<const uint4*>(from);
+            if (r >= rows) x = make_uint4(0, 0, 0, 0);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x.x ^ 0x80008000u), "r"(x.y ^ 0x80008000u),
+                         "r"(x.z ^ 0x80008000u), "r"(x.w ^ 0x80008000u)
+                         : "memory");
         }
     }
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 16-bit results of 32 columns, 32 or 16 bytes a store.
+__device__ __forceinline__ void store_row(uint16_t* to, const uint32_t (&x)[16], bool wide) {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int r = tid / C + i * kRowsAtOnce;
-        *reinterpret_cast<uint4*>(to + (c >> 3) * (kHalfRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
-            make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
+        for (int i = 0; i < 16; i += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 2 * i), "r"(x[i]), "r"(x[i + 1]),
+                         "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+                         : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(to + 2 * i) = make_uint4(x[i], x[i + 1], x[i + 2], x[i + 3]);
     }
 }
 
-template <bool H, int D>
+// Two scores through the cap, in units of log2: cap2 (1 - 2 / (1 + 2^y)), the two reciprocals from one.  Beyond 2^60 the
+// quotient is far below half a unit in the last place of 1; NaN stays NaN (and spreads to both).
+__device__ __forceinline__ void cap_pair(uint32_t& x0, uint32_t& x1, float mul, float cap2) {
+    float2 y = fma2(make_float2(__uint_as_float(x0), __uint_as_float(x1)), make_float2(mul, mul), make_float2(0.f, 0.f));
+    asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(y.x));
+    asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(y.y));
+    const float2 a = add2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), make_float2(1.f, 1.f));
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a.x * a.y));
+    y = fma2(make_float2(r * a.y, r * a.x), make_float2(-2.f * cap2, -2.f * cap2), make_float2(cap2, cap2));
+    x0 = __float_as_uint(y.x);
+    x1 = __float_as_uint(y.y);
+}
+
+template <bool H, int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1)
     k_kv_chunk(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ char s_raw[];
@@ -262,9 +302,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t lanes = (uint32_t)(warp & 3) << 21;
             const uint32_t s_at = tmem + half * 128 + lanes, o_at = tmem + 256 + half * D + lanes;
             const float cap2 = a.cap * kLog2e, scale = fmaxf(fabsf(a.scale), 0x1p-100f);
-            const float mul_in = a.cap > 0.f ? 2.f * kLog2e * scale / a.cap : kLog2e * scale;
-            const float mul = a.cap > 0.f ? 1.f : mul_in;
-            char* const q_to = smem_ptr + half * kTile;
+            const float mul_in = CAP ? 2.f * kLog2e * scale / a.cap : kLog2e * scale, mul = CAP ? 1.f : mul_in;
+            const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(2 * a.out_tok) | (uintptr_t)(2 * a.out_head)) & 31) == 0;
             uint32_t n_s = 0, n_o = 0;  // products awaited so far
             int note = 0;               // blocks of the stretch before this piece
             Pieces w(line, sh.part);
@@ -272,11 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             while (w.more) {
                 const int rows = w.half_rows(half);
                 const int2 blocks = w.half_blocks(half);
-                if (!loaded && blocks.x < blocks.y) {
-                    load_q<D>(a, w, half, q_to, row_in);
-                    fence_proxy_async();
-                    mbar_arrive(smem_u32(&sh.q_full[half]));
-                }
+                if (!loaded && blocks.x < blocks.y) load_q<D>(a, w, half, q_at + half * kTile, row_in, smem_u32(&sh.q_full[half]));
                 loaded = false;
                 const int row = w.at.rt * kRows + half * kHalfRows + row_in, tok = line.token(row);
                 const bool valid = row_in < rows;
@@ -289,37 +324,53 @@ __global__ void __launch_bounds__(kThreads, 1)
                     __syncwarp();
                     n_s++;
                     tc_fence_after();
-                    uint32_t s[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; i++) tc_load32(s[i], s_at + 32 * i);
                     const int j0 = w.at.t.lo + blk * kKeys;
                     const uint32_t skip = sh.skip[(note + blk - w.p0) & (kNotes - 1)];
                     const bool masked = j0 < whole_lo || j0 + kKeys > whole_hi || skip;
-                    tc_wait_ld(s);
-                    if (a.cap > 0.f) {
+                    // What the row sees of the block's positions 32 i .. 32 i + 31.
+                    auto keeps = [&](int i) {
+                        const int x = min(max(see.x - j0 - 32 * i, 0), 32), y = min(max(see.y - j0 - 32 * i, 0), 32);
+                        return (y == 32 ? ~0u : (1u << y) - 1u) & (x == 32 ? 0u : ~0u << x) & (skip >> (2 * i) & 1 ? 0xffff0000u : ~0u) &
+                               (skip >> (2 * i + 1) & 1 ? 0xffffu : ~0u);
+                    };
+                    auto put = [](auto& x, uint32_t keep, uint32_t v) {
 #pragma unroll
-                        for (int i = 0; i < 128; i++)
-                            s[i >> 5][i & 31] = __float_as_uint(score(__uint_as_float(s[i >> 5][i & 31]), mul_in, cap2));
-                    }
-                    if (masked) {
-                        const int x = min(max(see.x - j0, 0), kKeys), y = min(max(see.y - j0, 0), kKeys);
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const int x0 = min(max(x - 32 * i, 0), 32), y0 = min(max(y - 32 * i, 0), 32);
-                            uint32_t keep = (y0 == 32 ? ~0u : (1u << y0) - 1u) & (x0 == 32 ? 0u : ~0u << x0);
-                            keep &= (skip >> (2 * i) & 1 ? 0xffff0000u : ~0u) & (skip >> (2 * i + 1) & 1 ? 0xffffu : ~0u);
-#pragma unroll
-                            for (int c = 0; c < 32; c++)
-                                if (!(keep >> c & 1)) s[i][c] = 0xff800000u;
-                        }
-                    }
+                        for (int c = 0; c < (int)(sizeof(x) / 4); c++)
+                            if (!(keep >> c & 1)) x[c] = v;
+                    };
                     float tops[4];
+                    uint32_t s[CAP ? 1 : 4][32];
+                    if (CAP) {  // 32 positions at a time, and back.  Rolled: unrolled, the loop leaves the instruction cache
+                        tops[0] = tops[1] = tops[2] = tops[3] = -INFINITY;
+#pragma unroll 1
+                        for (int i = 0; i < 4; i++) {
+                            tc_load32(s[0], s_at + 32 * i);
+                            const uint32_t keep = masked ? keeps(i) : ~0u;
+                            tc_wait_ld(s);
+                            if (masked) put(s[0], keep, 0u);  // a NaN that the row does not see would spread
 #pragma unroll
-                    for (int i = 0; i < 4; i++) tops[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
+                            for (int c = 0; c < 32; c += 2) cap_pair(s[0][c], s[0][c + 1], mul_in, cap2);
+                            if (masked) put(s[0], keep, 0xff800000u);
 #pragma unroll
-                    for (int c = 2; c < 32; c += 2)
+                            for (int c = 0; c < 32; c += 2)
+                                tops[c >> 1 & 3] = max3(tops[c >> 1 & 3], __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
+                            tc_store32(s_at + 32 * i, s[0]);
+                        }
+                        tc_wait_st();
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) tops[i] = max3(tops[i], __uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1]));
+                        for (int i = 0; i < (CAP ? 1 : 4); i++) tc_load32(s[i], s_at + 32 * i);
+                        tc_wait_ld(s);
+#pragma unroll
+                        for (int i = 0; i < (CAP ? 1 : 4); i++) {
+                            if (masked) put(s[i], keeps(i), 0xff800000u);
+                            tops[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
+                        }
+#pragma unroll
+                        for (int c = 2; c < 32; c += 2)
+#pragma unroll
+                            for (int i = 0; i < (CAP ? 1 : 4); i++) tops[i] = max3(tops[i], __uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1]));
+                    }
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * mul;
                     // Raise the maximum that the weights refer to, and rescale what is summed: rarely.
                     const bool raise = top > m + kRaise || (m == -INFINITY && top > m);
@@ -348,9 +399,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 4; i++) {
                         float2 y[16];
                         uint32_t p[16];
+                        uint32_t(&x)[32] = s[CAP ? 0 : i];
+                        if (CAP) {
+                            tc_load32(x, s_at + 32 * i);
+                            tc_wait_ld(s);
+                        }
 #pragma unroll
                         for (int c = 0; c < 16; c++) {
-                            y[c] = fma2(make_float2(__uint_as_float(s[i][2 * c]), __uint_as_float(s[i][2 * c + 1])), make_float2(mul, mul),
+                            y[c] = fma2(make_float2(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1])), make_float2(mul, mul),
                                         make_float2(-shift, -shift));
                             y[c] = make_float2(exp2_fast(y[c].x), exp2_fast(y[c].y));
                         }
@@ -378,9 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (w.more && blocks.x < blocks.y) {
                     const int2 nb = w.half_blocks(half);
                     if (nb.x < nb.y) {
-                        load_q<D>(a, w, half, q_to, row_in);
-                        fence_proxy_async();
-                        mbar_arrive(smem_u32(&sh.q_full[half]));
+                        load_q<D>(a, w, half, q_at + half * kTile, row_in, smem_u32(&sh.q_full[half]));
                         loaded = true;
                     }
                 }
@@ -432,16 +486,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (!valid) continue;
                     if (whole) {
-                        uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c);
+                        uint32_t x[16];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint4 x;
-                            x.x = pack2<H>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-                            x.y = pack2<H>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-                            x.z = pack2<H>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-                            x.w = pack2<H>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-                            out[i / 8] = x;
-                        }
+                        for (int i = 0; i < 16; i++) x[i] = pack2<H>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                        store_row(a.out + t * a.out_tok + h * a.out_head + c, x, wide);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
@@ -522,7 +570,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (any_prev) issue_o(i, i == 1);
                             const bool act = blk >= hb[i].x && blk < hb[i].y;
                             if (i == 0) wait(k_full, k_round, sh.dead);
-                            if (act && blk == hb[i].x) wait(sh.q_full[i], n_q[i]++ & 1, sh.dead);
+                            if (act && blk == hb[i].x) {
+                                wait(sh.q_full[i], n_q[i]++ & 1, sh.dead);
+                                fence_proxy_async();  // Q came by ordinary copies
+                            }
                             tc_fence_after();
                             const uint64_t qd = descriptor(__shfl_sync(~0u, q_at + i * kTile, 0), 16, 1024);
                             const uint64_t kd = descriptor(__shfl_sync(~0u, k_at, 0), 16, 1024);
@@ -719,7 +770,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
 
 template <bool H, int D>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(k_kv_chunk<H, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(k_kv_chunk<H, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(k_kv_chunk<H, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
 }
 
 template <bool H, int D>
@@ -734,7 +786,7 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool after_few, int 
     c.stream = s;
     c.attrs = early;
     c.numAttrs = after_few ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&c, k_kv_chunk<H, D>, a, maps.k, maps.v);
+    const cudaError_t e = cudaLaunchKernelEx(&c, a.cap > 0.f ? k_kv_chunk<H, D, true> : k_kv_chunk<H, D, false>, a, maps.k, maps.v);
     if (e != cudaSuccess) return e;
     c.gridDim = dim3(sms, kRows / kJoinRows);
     c.blockDim = dim3(kJoinThreads);
