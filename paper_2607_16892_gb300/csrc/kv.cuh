@@ -40,7 +40,7 @@ struct KvMaps {
 
 // A tile of the chunk kernel that several CTAs share, noted by the first of them.
 struct Join {
-    int32_t b, rt, h;
+    int32_t q0, h, row0, rows;  // the request's first token; key head; the tile's rows
     int32_t last;  // the last CTA with a piece; -1: no tile
 };
 

@@ -25,6 +25,7 @@ using namespace kv;
 constexpr int kHalfRows = 128, kRows = 2 * kHalfRows, kKeys = 128;
 constexpr int kThreads = 384;
 constexpr int kNotes = 16;  // blocks that the copies are ahead of the weights, at most (a power of two)
+constexpr int kOver = 2;   // a tile's fixed cost, in blocks
 constexpr float kRaise = 8.f;
 
 template <int D>
@@ -35,7 +36,7 @@ struct Shape {
     static constexpr int kPieceFloats = kRows * (D + 2);
 };
 
-using ChunkLine = Line<kRows, kKeys, kKeys>;
+using ChunkLine = Line<kRows, kKeys, kKeys, kOver>;
 
 struct Shared {
     uint64_t kv_full[10], kv_empty[10], v_clean[10];
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (tid == 0) a.joins[blockIdx.x].last = -1;
     sh.part.find(line, s_raw);
-    clear_rest<D, kThreads>(a);
+    clear_rest<D, kThreads>(line);
     fence_proxy_async();  // the tiles' memory served as scratch
     tc_fence_before();
     __syncthreads();
@@ -505,9 +506,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (!whole && begins && row_in == 0 && half == 0) {
                     Join& j = a.joins[cta];
-                    j.b = cur.at.b;
-                    j.rt = cur.at.rt;
+                    j.q0 = cur.at.r.q0;
                     j.h = cur.at.h;
+                    j.row0 = cur.at.rt * kRows;
+                    j.rows = min(kRows, cur.at.r.rows - j.row0);
                     j.last = (int)((cur.at.start + cur.at.t.blocks - 1) / sh.part.share);
                 }
                 tc_fence_before();
@@ -723,43 +725,62 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
-// last of CTA c; four threads a row's sums, lanes along the rows as the pieces are laid out.
-constexpr int kJoinThreads = 128, kJoinRows = 32;
+// last of CTA c; four threads a row's sums, lanes along the rows as the pieces are laid out.  Bound by the latency of its
+// three dependent reads (what to join, the pieces), so four pieces are read at a time.
+constexpr int kJoinThreads = 128, kJoinRows = 32, kJoinAtOnce = 4;
+
+// A load that stays where it stands, so that several are in flight.
+__device__ __forceinline__ float4 load_now(const float* p) {
+    float4 x;
+    asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
+    return x;
+}
 
 template <bool H, int D>
 __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Join j = a.joins[blockIdx.x];
-    if (j.last < 0) return;
-    ChunkLine line(a);
-    const Request r = line.request(j.b);
     const int row_in = blockIdx.y * kJoinRows + (threadIdx.x & 31), part = threadIdx.x >> 5;
-    const int row = j.rt * kRows + row_in;
-    if (row >= r.rows) return;
+    if (j.last < 0 || row_in >= j.rows) return;
     constexpr int kFloats = Shape<D>::kPieceFloats, N = D / 16;  // 16-byte vectors of a part
-    auto piece = [&](int c) { return a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats; };
     float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-    for (int c = blockIdx.x; c <= j.last; c++) m = fmaxf(m, reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in].x);
-    const float shift = m == -INFINITY ? 0.f : m;
     float4 o[N];
 #pragma unroll
     for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int c = blockIdx.x; c <= j.last; c++) {
-        const float2 ml = reinterpret_cast<const float2*>(piece(c) + kRows * D)[row_in];
-        const float f = exp2_fast(ml.x - shift);
-        l += ml.y * f;
-        const float4* p = reinterpret_cast<const float4*>(piece(c)) + part * N * kRows + row_in;
+    for (int c0 = blockIdx.x; c0 <= j.last; c0 += kJoinAtOnce) {
+        float2 ml[kJoinAtOnce];
+        float4 x[kJoinAtOnce][N];
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const float4 x = p[i * kRows];
-            o[i] = make_float4(fmaf(x.x, f, o[i].x), fmaf(x.y, f, o[i].y), fmaf(x.z, f, o[i].z), fmaf(x.w, f, o[i].w));
+        for (int k = 0; k < kJoinAtOnce; k++) {
+            const int c = min(c0 + k, j.last);
+            const float* const piece = a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats;
+            ml[k] = reinterpret_cast<const float2*>(piece + kRows * D)[row_in];
+            if (c0 + k > j.last) ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[k][i] = load_now(piece + 4 * ((part * N + i) * kRows + row_in));
+        }
+        float to = m;
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; k++) to = fmaxf(to, ml[k].x);
+        const float shift = to == -INFINITY ? 0.f : to, keep = exp2_fast(m - shift);
+        m = to;
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < N; i++) o[i] = make_float4(o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep);
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; k++) {
+            if (c0 + k > j.last) break;
+            const float f = exp2_fast(ml[k].x - shift);
+            l += ml[k].y * f;
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                o[i] = make_float4(fmaf(x[k][i].x, f, o[i].x), fmaf(x[k][i].y, f, o[i].y), fmaf(x[k][i].z, f, o[i].z), fmaf(x[k][i].w, f, o[i].w));
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int tok = line.token(row), h = j.h * a.group + row - tok * a.group;
-    const int64_t t = r.q0 + tok;
+    const ChunkLine line(a);
+    const int row = j.row0 + row_in, tok = line.token(row), h = j.h * a.group + row - tok * a.group;
+    const int64_t t = j.q0 + tok;
     uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + part * (D / 4));
 #pragma unroll
     for (int i = 0; i < N; i += 2)

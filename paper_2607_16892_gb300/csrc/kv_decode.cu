@@ -22,6 +22,8 @@ using namespace kv;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16, kSlice = 32, kKeys = kSlice * kWarps;
 constexpr int kMostCtas = 4;  // per SM
+constexpr int kOver = 2;      // a tile's fixed cost, in blocks
+constexpr int kAtOnce = 8;    // pieces read at a time
 constexpr float kRaise = 8.f;
 
 template <int D, int NR>
@@ -77,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     extern __shared__ char s_raw[];
     constexpr int kStages = Ring<D, NR>::kStages, kStage = Ring<D, NR>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
-    using DecodeLine = Line<kRows, kKeys, kSlice>;
+    using DecodeLine = Line<kRows, kKeys, kSlice, kOver>;
     constexpr int kRowFloats = D + 4;  // of a row of sums in shared memory: no bank conflicts
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
     __shared__ Stretch<kThreads> s_part;
@@ -93,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     fence_mbar_init();
 
     s_part.find(line, s_raw);
-    clear_rest<D, kThreads>(a);
+    clear_rest<D, kThreads>(line);
     fence_proxy_async();  // the ring served as scratch
     __syncthreads();
     if (s_part.empty()) {
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                         row_out(r, c, x, to, sum);
                     } else {
                         *reinterpret_cast<float4*>(piece + r * D + c) = x;
-                        if (c == 0) *reinterpret_cast<float2*>(piece + kRows * D + 2 * r) = make_float2(to, sum);
+                        if (c == 0) *reinterpret_cast<float2*>(piece + kMostRows * D + 2 * r) = make_float2(to, sum);
                     }
                 }
             }
@@ -448,20 +450,46 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                     auto piece_of = [&](int64_t c) {
                         return a.pieces + (2 * c + (c == c0)) * kPieceFloats<D>;
                     };
-                    for (int i = tid; i < rows * kQuads; i += kThreads) {
-                        const int r = i / kQuads, c = 4 * (i % kQuads);
-                        float to = -INFINITY, sum = 0.f;
-                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int64_t p = c0; p <= c1; p++) {
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece_of(p) + kRows * D + 2 * r));
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(piece_of(p) + r * D + c));
-                            const float up = fmaxf(to, ml.x), shift = up == -INFINITY ? 0.f : up;
-                            const float f = exp2_fast(to - shift), g = exp2_fast(ml.x - shift);
-                            x = make_float4(x.x * f + y.x * g, x.y * f + y.y * g, x.z * f + y.z * g, x.w * f + y.w * g);
-                            sum = sum * f + ml.y * g;
+                    // A warp to a row: the factors of 32 pieces at once, a piece per lane, then their sums, loads of several in
+                    // flight.
+                    constexpr int V = D / 32;
+                    for (int r = warp; r < rows; r += kWarps) {
+                        float to = -INFINITY, sum = 0.f, x[V] = {};
+                        for (int64_t p0 = c0; p0 <= c1; p0 += 32) {
+                            const int n = (int)min((int64_t)32, c1 - p0 + 1);
+                            float2 ml = make_float2(-INFINITY, 0.f);
+                            if (lane < n) ml = __ldcg(reinterpret_cast<const float2*>(piece_of(p0 + lane) + kMostRows * D + 2 * r));
+                            float up = ml.x;
+                            for (int o = 16; o; o >>= 1) up = fmaxf(up, __shfl_xor_sync(~0u, up, o));
+                            up = fmaxf(up, to);
+                            const float shift = up == -INFINITY ? 0.f : up, keep = exp2_fast(to - shift), f = exp2_fast(ml.x - shift);
                             to = up;
+                            float l = ml.y * f;
+                            for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+                            sum = sum * keep + l;
+                            for (int i = 0; i < V; i++) x[i] *= keep;
+                            for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+                                float y[kAtOnce][V];
+#pragma unroll
+                                for (int k = 0; k < kAtOnce; k++) {
+                                    const float* const from = piece_of(p0 + min(k0 + k, n - 1)) + r * D + V * lane;
+                                    if constexpr (V == 4) *reinterpret_cast<float4*>(y[k]) = __ldcg(reinterpret_cast<const float4*>(from));
+                                    else *reinterpret_cast<float2*>(y[k]) = __ldcg(reinterpret_cast<const float2*>(from));
+                                }
+#pragma unroll
+                                for (int k = 0; k < kAtOnce; k++) {
+                                    const float fk = __shfl_sync(~0u, f, (k0 + k) & 31);
+                                    for (int i = 0; i < V; i++)
+                                        if (k0 + k < n) x[i] = fmaf(y[k][i], fk, x[i]);
+                                }
+                            }
                         }
-                        row_out(r, c, x, to, sum);
+                        const int tok = line.token(first + r), g = first + r - tok * a.group, h = at.h * a.group + g;
+                        const int64_t t = at.r.q0 + tok;
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        uint32_t* const to_out = reinterpret_cast<uint32_t*>(a.out + t * a.out_tok + h * a.out_head + V * lane);
+                        for (int i = 0; i < V; i += 2) to_out[i / 2] = pack2<H>(x[i] * inv, x[i + 1] * inv);
+                        if (a.lse && lane == 0) a.lse[t * a.heads + h] = sum == 0.f ? -INFINITY : kLn2 * (to + log2f(sum));
                     }
                 }
             }

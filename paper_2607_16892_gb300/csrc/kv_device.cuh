@@ -97,20 +97,20 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 
 // The requests' rows are dealt to tiles of `kRows` rows (a token's query heads of one key head are neighbours), and a tile's
 // positions to blocks of `kKeys`.  All blocks of all tiles stand in one line -- request, row tile, key head, block --
-// with one more place behind a tile's last block for what a tile costs beside its blocks (its Q, its results), and each
+// with kOver more places behind a tile's last block for what a tile costs beside its blocks (its Q, its results), and each
 // CTA takes an equal stretch of the line, so that long contexts are shared by many CTAs and short ones share a CTA.
 // A tile that crosses from one stretch into the next is joined from its pieces.
 struct Request {
-    int q0, n, rows, kv;  // first token, tokens, rows (tokens inside T times the group; 0: not this launch's), positions
+    int q0, n, rows, kv;  // first token, tokens, rows (tokens inside T times the group; 0: no positions, or not this launch's), positions
 };
 
 struct Tile {
     int lo, hi, blocks;  // positions [lo, hi), lo aligned
 };
 
-template <int kRowsOf, int kKeysOf, int kAlign>
+template <int kRowsOf, int kKeysOf, int kAlign, int kOverOf>
 struct Line {
-    static constexpr int kRows = kRowsOf, kKeys = kKeysOf;
+    static constexpr int kRows = kRowsOf, kKeys = kKeysOf, kOver = kOverOf;
     const AttendArgs& a;
     bool bad = false;
 
@@ -128,11 +128,11 @@ struct Line {
             return r;
         }
         r.n = q1 - r.q0;
-        r.rows = r.n > a.min_q && r.n <= a.max_q ? max(0, min(q1, a.T) - r.q0) * a.group : 0;
         if (r.kv < 0 || (int64_t)r.kv > ((int64_t)a.max_pages << a.page_shift)) {
             bad = true;
             r.kv = 0;
         }
+        r.rows = r.kv > 0 && r.n > a.min_q && r.n <= a.max_q ? max(0, min(q1, a.T) - r.q0) * a.group : 0;
         return r;
     }
     // Visible positions [lo, hi) of token i of a request.
@@ -154,7 +154,7 @@ struct Line {
     // Places of row tiles first, first + step, ...
     __device__ __forceinline__ int64_t cost(const Request& r, int first = 0, int step = 1) const {
         int64_t c = 0;
-        for (int rt = first, n = row_tiles(r); rt < n; rt += step) c += tile(r, rt).blocks + 1;
+        for (int rt = first, n = row_tiles(r); rt < n; rt += step) c += tile(r, rt).blocks + kOver;
         return c * a.kv_heads;
     }
 };
@@ -184,7 +184,7 @@ struct Cursor {
         }
         for (rt = 0;; rt += 32) {  // 32 row tiles at a time
             const bool there = rt + lane < line.row_tiles(r);
-            const int64_t mine = there ? (int64_t)(line.tile(r, rt + lane).blocks + 1) * line.a.kv_heads : 0;
+            const int64_t mine = there ? (int64_t)(line.tile(r, rt + lane).blocks + L::kOver) * line.a.kv_heads : 0;
             int64_t incl = mine;
             for (int o = 1; o < 32; o <<= 1) {
                 const int64_t x = __shfl_up_sync(~0u, incl, o);
@@ -201,13 +201,13 @@ struct Cursor {
             if (rt + 32 >= line.row_tiles(r)) break;
         }
         t = line.tile(r, rt);
-        h = (int)((u - base) / (t.blocks + 1));
-        start = base + (int64_t)h * (t.blocks + 1);
+        h = (int)((u - base) / (t.blocks + L::kOver));
+        start = base + (int64_t)h * (t.blocks + L::kOver);
     }
     // On to the next tile (there is one).
     template <class L>
     __device__ __forceinline__ void next(L& line) {
-        start += t.blocks + 1;
+        start += t.blocks + L::kOver;
         if (++h < line.a.kv_heads) return;
         h = 0;
         if (++rt >= line.row_tiles(r)) {
@@ -306,10 +306,10 @@ struct Walk {
         left = (int)(s.u1 - s.u0);
         const int from = (int)(s.u0 - at.start);
         p0 = min(from, at.t.blocks);
-        used = min(at.t.blocks + 1 - from, left);
+        used = min(at.t.blocks + L::kOver - from, left);
         p1 = min(from + used, at.t.blocks);
         more = true;
-        if (p0 == p1) {  // the place behind the last block alone
+        if (p0 == p1) {  // places behind the last block alone
             next();
             piece = 0;
         }
@@ -323,7 +323,7 @@ struct Walk {
         }
         at.next(line);
         p0 = 0;
-        used = min(at.t.blocks + 1, left);
+        used = min(at.t.blocks + L::kOver, left);
         p1 = min(used, at.t.blocks);
     }
     // Whether the tile begins in this stretch, and whether it lies in it whole.
@@ -337,16 +337,24 @@ struct Walk {
     }
 };
 
-// Tokens of no request: out = 0.
-template <int D, int kThreads>
-__device__ __forceinline__ void clear_rest(const AttendArgs& a) {
+// Tokens of no request, and of requests without positions: out = 0.
+template <int D, int kThreads, class L>
+__device__ __forceinline__ void clear_rest(L& line) {
+    const AttendArgs& a = line.a;
+    auto clear = [&](int t0, int t1, int from, int step) {
+        const int64_t vecs = (int64_t)(t1 - t0) * a.heads * (D / 8);
+        for (int64_t i = (int64_t)from * kThreads + threadIdx.x; i < vecs; i += (int64_t)step * kThreads) {
+            const int64_t row = i / (D / 8);
+            const int t = t0 + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
+            *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
+            if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
+        }
+    };
     const int end = max(0, min(a.q_off[a.B], a.T));
-    const int64_t vecs = (int64_t)(a.T - end) * a.heads * (D / 8);
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vecs; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t row = i / (D / 8);
-        const int t = end + (int)(row / a.heads), h = (int)(row % a.heads), c = (int)(i % (D / 8));
-        *reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + c * 8) = make_uint4(0, 0, 0, 0);
-        if (a.lse && c == 0) a.lse[(int64_t)t * a.heads + h] = -INFINITY;
+    if (end < a.T) clear(end, a.T, blockIdx.x, gridDim.x);
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const Request r = line.request(b);
+        if (r.kv == 0 && r.n > a.min_q && r.n <= a.max_q && r.q0 < a.T) clear(r.q0, min(r.q0 + r.n, a.T), 0, 1);
     }
 }
 
