@@ -298,7 +298,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!sh.part.empty()) {
         if (warp < 8) {
             // ---------------------------------------------------------- weights and results of a half
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
             const int half = warp >> 2, row_in = tid & 127;
             const uint32_t lanes = (uint32_t)(warp & 3) << 21;
             const uint32_t s_at = tmem + half * 128 + lanes, o_at = tmem + 256 + half * D + lanes;
@@ -340,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (!(keep >> c & 1)) x[c] = v;
                     };
                     float tops[4];
-                    uint32_t s[CAP ? 1 : 4][32];
+                    uint32_t s[1][32];
                     if (CAP) {  // 32 positions at a time, and back.  Rolled: unrolled, the loop leaves the instruction cache
                         tops[0] = tops[1] = tops[2] = tops[3] = -INFINITY;
 #pragma unroll 1
@@ -359,18 +358,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         tc_wait_st();
                     } else {
+                        tops[0] = tops[1] = tops[2] = tops[3] = -INFINITY;
+#pragma unroll 2
+                        for (int i = 0; i < 4; i++) {
+                            tc_load32(s[0], s_at + 32 * i);
+                            tc_wait_ld(s);
+                            if (masked) put(s[0], keeps(i), 0xff800000u);
 #pragma unroll
-                        for (int i = 0; i < (CAP ? 1 : 4); i++) tc_load32(s[i], s_at + 32 * i);
-                        tc_wait_ld(s);
-#pragma unroll
-                        for (int i = 0; i < (CAP ? 1 : 4); i++) {
-                            if (masked) put(s[i], keeps(i), 0xff800000u);
-                            tops[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
+                            for (int c = 0; c < 32; c += 2)
+                                tops[c >> 1 & 3] = max3(tops[c >> 1 & 3], __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
                         }
-#pragma unroll
-                        for (int c = 2; c < 32; c += 2)
-#pragma unroll
-                            for (int i = 0; i < (CAP ? 1 : 4); i++) tops[i] = max3(tops[i], __uint_as_float(s[i][c]), __uint_as_float(s[i][c + 1]));
                     }
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * mul;
                     // Raise the maximum that the weights refer to, and rescale what is summed: rarely.
@@ -396,15 +393,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     const float shift = m == -INFINITY ? 0.f : m;
                     float2 sum[4] = {};
-#pragma unroll
+#pragma unroll 2
                     for (int i = 0; i < 4; i++) {
                         float2 y[16];
                         uint32_t p[16];
-                        uint32_t(&x)[32] = s[CAP ? 0 : i];
-                        if (CAP) {
-                            tc_load32(x, s_at + 32 * i);
-                            tc_wait_ld(s);
-                        }
+                        uint32_t(&x)[32] = s[0];
+                        tc_load32(x, s_at + 32 * i);
+                        tc_wait_ld(s);
+                        if (!CAP && masked) put(x, keeps(i), 0xff800000u);
 #pragma unroll
                         for (int c = 0; c < 16; c++) {
                             y[c] = fma2(make_float2(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1])), make_float2(mul, mul),
@@ -515,7 +511,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_fence_before();
             }
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
             Pieces w(line, sh.part);
             int stage = 0;
             uint32_t round = 0;  // of the ring
