@@ -80,7 +80,7 @@ typedef enum {
  * KVDRO_TEST_SKIP_CHUNK=c makes this context's grid kernels leave staged chunk c uncopied with a
  * wait bound of 1 ms, so every bounded wait on it runs out (KVDRO_ETIMEOUT).  The hook travels
  * with this context's launches only; other contexts, on the same device or not, keep the
- * production bound.
+ * production bound.  kvdro_kv_attend leaves out the c-th copies of each CTA, to the same effect.
  * Bounded waits: a grid kernel gives up waiting for a staged sample chunk only after 2 s of the
  * GPU's global timer AND a minimum number of polls made while it was running, so a CTA that is
  * descheduled (time-slicing, preemption) does not report a timeout on a copy that lands once it

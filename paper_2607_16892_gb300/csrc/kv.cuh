@@ -59,6 +59,8 @@ struct AttendArgs {
     float* pieces;       // sums of tiles that several CTAs share
     unsigned* tickets;   // by CTA: arrivals at the tile that its stretch ends in, zero between calls
     Join* joins;         // by CTA
+    unsigned long long wait_ns;  // bound of a wait
+    int32_t skip;        // test hook: each CTA leaves this copy out, so that the wait for it runs out; -1: none
     int32_t* err;
 };
 size_t kv_decode_piece_bytes(int sms);

@@ -21,6 +21,7 @@ namespace {
 constexpr int64_t kMaxStride = (int64_t)1 << 39;  // elements: what a tensor map's 40 bits of bytes hold
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
+constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
 constexpr int64_t kFewRows = 16;  // rows that share a key head, up to which the kernel for single tokens runs
 
 int log2_of(int32_t v) {
@@ -317,6 +318,8 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.pieces = static_cast<float*>(ctx->kv_pieces.p);
     a.tickets = static_cast<unsigned*>(ctx->kv_tickets.p);
     a.joins = static_cast<kvdro::Join*>(ctx->kv_joins.p);
+    a.wait_ns = ctx->skip_chunk >= 0 ? kTestWaitNs : kWaitNs;
+    a.skip = ctx->skip_chunk;
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->last_stream = s;

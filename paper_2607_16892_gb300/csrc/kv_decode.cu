@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     Walk<DecodeLine> in(line, s_part), w = in;  // of the copies, and of the sums
     int in_blk = in.p0;
     bool in_v = false;
+    int fetched = 0;
 
     // Page numbers of this warp's slices of 32 blocks, one per lane; a slice has two pages if they have 16 slots.
     const int slots = min(kSlice, 1 << a.page_shift);
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
         const int p0 = __shfl_sync(~0u, pg[0], in_blk & 31), p1 = __shfl_sync(~0u, pg[1], in_blk & 31);
         gaps = (gaps & ~(3u << 2 * stage)) | ((p0 < 0 ? 1u : 0u) | (p1 < 0 ? 2u : 0u)) << 2 * stage;
         if (p0 >= 0 || p1 >= 0) {
-            if (lane == 0) {
+            if (lane == 0 && fetched != a.skip) {  // a test's wait runs out
                 const int slot = (in.at.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1);
                 const uint32_t bar = smem_u32(&s_bar[warp][stage]), to = ring + stage * kStage;
                 const CUtensorMap* const map = in_v ? &vmap : &kmap;
@@ -148,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             }
             filled |= 1u << stage;
         }
+        fetched++;
         in_v = !in_v;
         if (in_v) return;
         if (++in_blk == in.p1) {
@@ -170,7 +172,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     // The slice in `stage`, once it is there; false if there is none.
     auto ready = [&] {
         if (!(filled >> stage & 1) || dead) return false;
-        if (__all_sync(~0u, mbar_wait(smem_u32(&s_bar[warp][stage]), phase >> stage & 1))) phase ^= 1u << stage;
+        const uint32_t bar = smem_u32(&s_bar[warp][stage]), parity = phase >> stage & 1;
+        if (__all_sync(~0u, mbar_try(bar, parity) || mbar_wait_slow(bar, parity, a.wait_ns, nullptr))) phase ^= 1u << stage;
         else dead = true;
         return !dead;
     };
@@ -435,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             }
             __syncthreads();
             if (!whole) {
-                const int64_t c0 = at.start / s_part.share, c1 = (at.start + at.t.blocks - 1) / s_part.share;  // CTAs with a piece
+                const int64_t c0 = divide(at.start, s_part.share), c1 = divide(at.start + at.t.blocks - 1, s_part.share);  // CTAs with a piece
                 if (tid == 0) {
                     __threadfence();
                     const unsigned arrived = atomicAdd(a.tickets + c0, 1u);
@@ -500,8 +503,10 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
         }
     }
     if (dead) {  // what is still in flight must land before the CTA's memory is given away
-        for (int s = 0; s < kStages; s++)
-            if (filled >> s & 1) mbar_wait(smem_u32(&s_bar[warp][s]), phase >> s & 1);
+        for (int s = 0; s < kStages; s++) {
+            const uint32_t bar = smem_u32(&s_bar[warp][s]), parity = phase >> s & 1;
+            if ((filled >> s & 1) && !mbar_try(bar, parity)) mbar_wait_slow(bar, parity, a.wait_ns, nullptr);
+        }
         if (lane == 0) atomicOr(a.err, kKvErrTimeout);
     }
     if (__any_sync(~0u, range || line.bad) && lane == 0) atomicOr(a.err, kKvErrRange);

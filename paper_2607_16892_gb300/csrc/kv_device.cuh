@@ -72,19 +72,20 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// Waits for a phase, for about 2 s at most: 2 s of the GPU's timer and 2^14 polls made while running.
-static __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+// Waits for a phase, for `limit` ns of the GPU's timer at most (and, where that is long, 2^14 polls made while running);
+// ends at once where `dead` (if there is one) says that another wait ran out.  False, and `dead` set, if it ran out.
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, unsigned long long limit, volatile int* dead) {
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    const unsigned least = limit > 100000000ull ? 1u << 14 : 16u;
     for (unsigned polls = 0; polls < (1u << 28); polls++) {
         if (mbar_try(bar, parity)) return true;
+        if (dead && *dead) return false;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-        if (polls > (1u << 14) && t - t0 > 2000000000ull) return false;
+        if (polls > least && t - t0 > limit) break;
     }
+    if (dead) *dead = 1;
     return false;
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-    return mbar_try(bar, parity) || mbar_wait_slow(bar, parity);
 }
 
 // A box of one page: coordinates d, slot, head, page.  Out-of-range pages read as zeros.
@@ -159,6 +160,11 @@ struct Line {
     }
 };
 
+// x / y for x >= 0, y > 0: a 64-bit division takes some 500 cycles, a 32-bit one a fifth of that.
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 __device__ __forceinline__ int64_t warp_sum(int64_t x) {
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
     return x;
@@ -201,7 +207,7 @@ struct Cursor {
             if (rt + 32 >= line.row_tiles(r)) break;
         }
         t = line.tile(r, rt);
-        h = (int)((u - base) / (t.blocks + L::kOver));
+        h = (int)divide(u - base, t.blocks + L::kOver);
         start = base + (int64_t)h * (t.blocks + L::kOver);
     }
     // On to the next tile (there is one).
@@ -268,7 +274,7 @@ struct Stretch {
             total += warp_sums[w];
         }
         before += incl - mine;
-        const int64_t each = max((int64_t)1, (total + gridDim.x - 1) / gridDim.x), at = blockIdx.x * each;
+        const int64_t each = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x)), at = blockIdx.x * each;
         if (tid == 0) {
             share = each;
             u0 = at;

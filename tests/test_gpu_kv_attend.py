@@ -211,6 +211,42 @@ def test_offsets_past_32_bits(ctx):
     check(ctx, case)
 
 
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [("bf16", 128, 4, 1), ("fp16", 64, 6, 2)])
+@pytest.mark.parametrize("max_q", [1, 0])
+def test_many_requests(ctx, dtype, D, Hq, Hkv, max_q):
+    """More requests than threads, so that a thread counts several; some with more row tiles than it counts by itself."""
+    rng = np.random.default_rng(D)
+    lens = [(int(rng.integers(0, 4)), int(rng.integers(0, 60))) for _ in range(1500)]
+    for b, n in ((3, 900), (700, 2100), (1499, 400)):
+        lens[b] = (n if max_q == 0 else 30, n + 100)
+    case = Case(lens, dtype, D, Hq, Hkv, 16, seed=1)
+    out, lse = case.run(ctx, max_q=max_q)
+    case.check(out, lse, only=set(range(0, 1500, 23)) | {3, 700, 1499})
+    kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("skip", [0, 1, 2, 5, 6])
+@pytest.mark.parametrize("lens", [[(1, 9000)] * 40, [(300, 4000)] * 6, [(1, 9000)] * 20 + [(300, 4000)] * 4], ids=["decode", "chunk", "both"])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(monkeypatch, ctx, skip, lens):
+    """Failure detection without a fault: every CTA leaves one copy out, so nothing completes its barrier, and the
+    bounded wait for it (1 ms under the hook) gives up."""
+    case = Case(lens, "bf16", 128, 8, 2, 16, seed=1)
+    monkeypatch.setenv("KVDRO_TEST_SKIP_CHUNK", str(skip))
+    broken = kvdro.kvdro_create(0)
+    monkeypatch.delenv("KVDRO_TEST_SKIP_CHUNK")
+    try:
+        for _ in range(2):
+            case.run(broken)
+            with pytest.raises(kvdro.KvdroError) as e:
+                kvdro.kvdro_sync(broken)
+            assert e.value.status == kvdro.KVDRO_ETIMEOUT
+        kvdro.kvdro_sync(broken)
+    finally:
+        kvdro.kvdro_destroy(broken)
+    case.check(*case.run(ctx), only={0, len(lens) - 1})
+    kvdro.kvdro_sync(ctx)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3])
 def test_injected_allocation_failure_reports_enomem(monkeypatch, n):
     monkeypatch.setenv("KVDRO_TEST_FAIL_ALLOC", str(n))
