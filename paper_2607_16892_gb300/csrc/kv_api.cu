@@ -22,7 +22,9 @@ constexpr int64_t kMaxStride = (int64_t)1 << 39;  // elements: what a tensor map
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
 constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
-constexpr int64_t kFewRows = 16;  // rows that share a key head, up to which the kernel for single tokens runs
+// Rows that share a key head, up to which the kernel for single tokens runs.  32 requests of 3000 positions, 8 key heads of 128:
+// 12 rows 77 us there; 20 to 32 rows 140 us there, 85 on the kernel for chunks; 64 rows 249 and 85.
+constexpr int64_t kFewRows = 16;
 
 int log2_of(int32_t v) {
     int s = 0;

@@ -3,10 +3,10 @@
 // A tile is 256 rows (tokens times the heads that share a key head) in two halves of 128, a block 128 positions.  Per block and
 // half: S = Q K^T (128 x 128 into tensor memory), weights P = 2^(S - m) by four warps, a row per thread, back into
 // tensor memory over S, and O += P V.  Both halves use the same K and V out of a ring of shared-memory stages; while the
-// four warps of one half exponentiate, the tensor cores work for the other:
+// four warps of one half exponentiate, the tensor cores work for the other, in the fixed order
 //     S0(0) S1(0) | PV0(0) S0(1) PV1(0) S1(1) | PV0(1) S0(2) ...
-// Bound by the tensor cores (4 D operations per row and position) where contexts are long; a row's 128 exponentials per
-// block and half are the next limit.  The maximum m that weights refer to is raised only when a row's
+// which keeps the halves out of step.  (With a warp of its own to issue each half's products they fell into step and waited
+// for the same things: 1760 us for the case below.)  The maximum m that weights refer to is raised only when a row's
 // true maximum passes it by 2^8, so that O is rescaled in a few blocks at most; sums are exact in any case, for l and O
 // refer to the same m.  The line of all blocks is dealt to one CTA per SM (kv_device.cuh); pieces of tiles that
 // cross CTAs go through global memory and a second small kernel joins them in a fixed order.
@@ -14,6 +14,12 @@
 // Roles: warps 0-3 and 4-7 the halves' weights, Q and results; 8 issues the products; 9 the copies; 10 and 11 look
 // through V of blocks that some row does not see whole: a weight of 0 times infinity or NaN is not 0, so such elements are
 // replaced by 0 there, and the rows that do see them get them added at the end.
+//
+// Bound by the tensor cores where contexts are long.  A block of both halves takes about 3000 cycles: 16 S products of 70 cycles
+// and 16 PV products of 81 by themselves (64 at peak), 90 to 100 each beside the copies into shared memory and the weights' traffic
+// in tensor memory.  Measured (bf16, 32 heads of 128 over 8 key heads): 4096 tokens at the end of 32768, 2.06 TFLOP in
+// 1376 us = 1.50 PFLOP/s, 0.79 of the measured 1.89 (1545 us in a loop that heats the GPU); 512 tokens over 4099 45 us,
+// of which 4 are the search of the line, 6 the join and 3 the launch.
 #include "kv_device.cuh"
 
 namespace kvdro {
@@ -25,7 +31,7 @@ using namespace kv;
 constexpr int kHalfRows = 128, kRows = 2 * kHalfRows, kKeys = 128;
 constexpr int kThreads = 384;
 constexpr int kNotes = 16;  // blocks that the copies are ahead of the weights, at most (a power of two)
-constexpr int kOver = 2;   // a tile's fixed cost, in blocks
+constexpr int kOver = 2;   // a tile's fixed cost, in blocks (1 / 2 / 3: mixed batch 148 / 132 / 132 us, capped prompts 95 / 96.5 / 99)
 constexpr float kRaise = 8.f;
 
 template <int D>
@@ -351,6 +357,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tc_wait_st();
                     } else {
                         tops[0] = tops[1] = tops[2] = tops[3] = -INFINITY;
+                        // S is read twice, 32 positions at a time: held whole (128 values a thread) and unrolled, the loop left the
+                        // instruction cache and the mixed batch took 128 us instead of 122.
 #pragma unroll 2
                         for (int i = 0; i < 4; i++) {
                             tc_load32(s[0], s_at + 32 * i);

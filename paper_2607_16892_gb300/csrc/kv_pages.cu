@@ -74,7 +74,8 @@ __device__ __forceinline__ Sums scan(Sums x, int lane, Sums& all) {
 // keeps the prefix sums in shared memory; then the CTAs share the tokens and the pages, each found by a binary search there.
 // One launch, and no CTA waits for another: nothing that a CTA writes is read by any (a new token's page is
 // looked up in the ring, not in the table that another CTA may not have written yet).  Bound by the latency of its chain of
-// dependent reads: lengths, sums, search, page.
+// dependent reads: lengths, sums, search, page.  8 requests 11 us a call (the host's share), 4096 requests with 424 k new tokens
+// 12.4 us (17 with a request per thread and turn, 21 with 64-bit sums by every warp).
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(PlanArgs a) {
     extern __shared__ int32_t sm[];
     int32_t* s_q = sm;             // [B] first token
@@ -257,7 +258,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(PlanArgs a) {
     if (bad) atomicOr(a.err, kKvErrRange);
 }
 
-// A copy with a lookup: bound by the bytes read and written.  A token's row is dealt to 2^lanes_shift lanes, 16 bytes
+// A copy with a lookup: bound by the bytes read and written (65539 tokens of 8 heads of 128, 526 MB, 81 us = 6.5 TB/s; a copy runs
+// at 6.8).  A token's row is dealt to 2^lanes_shift lanes, 16 bytes
 // each at a time, keys and values together, so that a lane has up to eight loads in flight.
 constexpr int kAppendThreads = 256, kAppendDeep = 4;
 
