@@ -253,7 +253,7 @@ int kvdro_kv_close(kvdro_kv* kv);
  *   new_len < 0   the request is done: its pages go back, to be handed out from the next call on.
  * Free pages are a ring of n_pages page numbers: pool = {head, count}; pages are taken at head and
  * returned behind the last.  Every page number is in the ring or in one request's table.
- *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size <= 2^31 - 256.
+ *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size <= 2^30.
  *   cached, new_len, held  int32[B];  reserve: int32[B] or NULL (no reservations).
  *   table      int32[B][max_pages], updated: entries held[b] <= j < held_out[b] are written.
  *   ring       int32[n_pages], updated: returned pages are written behind the last.
@@ -290,13 +290,14 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
  * weights are rounded to the cache's dtype for the product with v.
  *   B          requests, 1 <= B <= 16384;  T: tokens, T >= 0; tokens beyond T are left out, and T tokens of out and lse
  *              are written (zeros and -infinity for tokens of no request).
- *   n_heads    a multiple of n_kv_heads, at most 4096.
+ *   n_heads    a multiple of n_kv_heads, at most 4096; T * n_heads <= 2^30.
  *   max_q      the most new tokens of one request, as far as the caller knows, 0 if unknown.  It chooses among
  *              kernels; the results are right whatever it says.
  *   q, out     element (t, h, d) at t * stride[0] + h * stride[1] + d (NULL: contiguous [T][n_heads][head_dim]), of the
  *              cache's dtype; 16-byte aligned, strides multiples of 8.
- *   q_off      int32[B+1], ascending from 0;  kv_len: int32[B];  table: int32[B][max_pages].
- *   scale      finite;  causal: 0 or 1;  window >= 0 (0: none; needs causal);  softcap finite, >= 0 (0: none).
+ *   q_off      int32[B+1], ascending from 0;  kv_len: int32[B];  table: int32[B][max_pages], max_pages * page_size <= 2^30.
+ *   scale      finite;  causal: 0 or 1;  window >= 0 (0: none; needs causal);  softcap 0 (none) or in
+ *              [2^-20, 1000]; capped scores are off by up to 2^-21 softcap.
  *   lse        float [T][n_heads], log sum_j exp(s_j); may be NULL.
  */
 int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,

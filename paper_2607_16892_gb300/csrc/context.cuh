@@ -63,7 +63,7 @@ struct kvdro_ctx {
     kvdro::Buf kv_err;           // the word in which its kernels report what they met
     kvdro::Buf kv_pieces, kv_tickets, kv_joins;  // scratch of the attention kernels
     cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it
-    cudaStream_t kv_stream = nullptr;  // that call's stream
+    unsigned long long kv_stream = 0;  // that call's stream, by its number
     bool kv_used = false;
     bool kv_plan_ready = false, kv_ready = false;
 };

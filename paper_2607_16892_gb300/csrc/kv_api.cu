@@ -19,7 +19,7 @@ using kvdro::NvtxRange;
 namespace {
 
 constexpr int64_t kMaxStride = (int64_t)1 << 39;  // elements: what a tensor map's 40 bits of bytes hold
-constexpr int32_t kMaxTokens = 1 << 30;
+constexpr int32_t kMaxTokens = 1 << 30, kMaxPositions = 1 << 30, kMaxRows = 1 << 30;  // with room for a tile in 32 bits
 constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
 constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
 // Rows that share a key head, up to which the kernel for single tokens runs.  32 requests of 3000 positions, 8 key heads of 128:
@@ -43,8 +43,8 @@ int check_pages(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages) {
 int check_requests(kvdro_ctx* ctx, int32_t B, int32_t T, int32_t max_pages, int32_t page_size) {
     if (B < 1 || B > kvdro::kKvMaxRequests) return fail(ctx, KVDRO_EINVAL, "B = %d outside [1, %d]", B, kvdro::kKvMaxRequests);
     if (T < 0 || T > kMaxTokens) return fail(ctx, KVDRO_EINVAL, "T = %d outside [0, 2^30]", T);
-    if (max_pages < 1 || (int64_t)max_pages * page_size > 0x7fffff00LL)
-        return fail(ctx, KVDRO_EINVAL, "max_pages = %d: max_pages * page_size outside [page_size, 2^31 - 256]", max_pages);
+    if (max_pages < 1 || (int64_t)max_pages * page_size > kMaxPositions)
+        return fail(ctx, KVDRO_EINVAL, "max_pages = %d: max_pages * page_size outside [page_size, 2^30]", max_pages);
     return KVDRO_OK;
 }
 
@@ -267,12 +267,12 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
         return fail(ctx, KVDRO_EINVAL, "n_heads = %d is not a multiple of n_kv_heads = %d up to %d", n_heads, kv->heads, kMaxHeads);
     if (max_q < 0) return fail(ctx, KVDRO_EINVAL, "max_q = %d is negative", max_q);
     if (!std::isfinite((float)scale)) return fail(ctx, KVDRO_EINVAL, "scale = %g is not finite", scale);
-    if (!std::isfinite((float)softcap) || softcap < 0.0 || (softcap > 0.0 && (float)softcap < 1e-30f))
-        return fail(ctx, KVDRO_EINVAL, "softcap = %g is neither 0 nor finite and at least 1e-30", softcap);
+    if (!(softcap == 0.0 || (softcap >= 0x1p-20 && softcap <= 1000.0)))
+        return fail(ctx, KVDRO_EINVAL, "softcap = %g is neither 0 nor in [2^-20, 1000]", softcap);
     if (causal != 0 && causal != 1) return fail(ctx, KVDRO_EINVAL, "causal must be 0 or 1");
     if (window < 0 || (window > 0 && !causal)) return fail(ctx, KVDRO_EINVAL, "window = %d: not negative, and with causal only", window);
     if (T == 0) return KVDRO_OK;
-    if ((int64_t)T * n_heads > 0x7fffffffLL) return fail(ctx, KVDRO_EINVAL, "T * n_heads = %lld passes 2^31 - 1", (long long)T * n_heads);
+    if ((int64_t)T * n_heads > kMaxRows) return fail(ctx, KVDRO_EINVAL, "T * n_heads = %lld passes 2^30", (long long)T * n_heads);
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
     if (int rc = check_device(ctx, {{"q", q}, {"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"out", out}})) return rc;
@@ -325,11 +325,14 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->last_stream = s;
-    // Calls share the scratch: one on another stream than the last waits for that one.
+    // Calls share the scratch: one on another stream than the last waits for that one.  (By the streams' numbers: a new stream
+    // may have an old one's handle.  Waiting in every case cost a small call 2 us.)
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
     const bool captured = capture != cudaStreamCaptureStatusNone;
-    if (!captured && ctx->kv_used && ctx->kv_stream != s) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
+    unsigned long long number = 0;
+    if (!captured) KV_CUDA(cudaStreamGetId(s, &number), "asking for the stream's number");
+    if (!captured && ctx->kv_used && ctx->kv_stream != number) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
     // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
     // both runs on both, each request on its own.
     const int64_t most = max_q > 0 ? max_q : T > B ? T : 1;  // new tokens of a request, as far as is known
@@ -350,7 +353,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     }
     if (!captured) {
         KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
-        ctx->kv_stream = s;
+        ctx->kv_stream = number;
         ctx->kv_used = true;
     }
     return KVDRO_OK;

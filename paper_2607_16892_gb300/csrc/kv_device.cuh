@@ -275,10 +275,12 @@ struct Stretch {
         }
         before += incl - mine;
         const int64_t each = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x)), at = blockIdx.x * each;
+        const bool countable = each < 0x7fffffff;  // a stretch is counted in 32 bits; a longer one would take days
+        if (!countable) line.bad = true;
         if (tid == 0) {
             share = each;
             u0 = at;
-            u1 = min(at + each, total);
+            u1 = countable ? min(at + each, total) : at;
         }
         if (at >= before && at < before + mine) {
             found = tid;

@@ -33,14 +33,15 @@ def check(ctx, case, **opt):
 @pytest.mark.parametrize("dtype,D,Hq,Hkv,page,layout", [
     ("bf16", 128, 8, 2, 16, "dense"), ("fp16", 64, 8, 8, 32, "packed"), ("bf16", 64, 14, 2, 64, "heads_first"),
     ("fp16", 128, 5, 1, 128, "heads_first"), ("bf16", 128, 16, 1, 16, "packed"), ("fp16", 128, 40, 1, 32, "dense"),
-    ("bf16", 64, 3, 3, 16, "dense"), ("bf16", 128, 12, 2, 64, "dense")])
+    ("bf16", 64, 3, 3, 16, "dense"), ("bf16", 128, 12, 2, 64, "dense"), ("fp16", 64, 8, 4, 128, "packed"),
+    ("bf16", 64, 32, 1, 128, "dense")])
 def test_types_heads_and_layouts(ctx, lens, dtype, D, Hq, Hkv, page, layout):
     check(ctx, Case(lens, dtype, D, Hq, Hkv, page, seed=D + Hq, layout=layout))
 
 
 @pytest.mark.parametrize("lens", [MIX, DECODE], ids=["mix", "decode"])
 @pytest.mark.parametrize("opt", [dict(causal=False), dict(window=1), dict(window=7), dict(window=130), dict(softcap=5.0),
-                                 dict(softcap=30.0, window=64), dict(scale=0.5), dict(scale=-0.1), dict(scale=0.0)],
+                                 dict(softcap=30.0, window=64), dict(softcap=800.0), dict(softcap=0.01), dict(scale=0.5), dict(scale=-0.1), dict(scale=0.0)],
                          ids=lambda o: "-".join(f"{k}{v}" for k, v in o.items()))
 def test_masks_caps_and_scales(ctx, lens, opt):
     check(ctx, Case(lens, "bf16", 64, 8, 2, 16, seed=5), **opt)

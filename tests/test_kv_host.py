@@ -74,7 +74,13 @@ def test_refusals():
     refused(att, *args, scale=float("nan"), match="scale")
     refused(att, *args, softcap=-1.0, match="softcap")
     refused(att, *args, softcap=float("inf"), match="softcap")
+    refused(att, *args, softcap=1001.0, match="softcap")
+    refused(att, *args, softcap=1e-9, match="softcap")
     refused(att, *args, max_q=-1, match="max_q")
+    lib, p = kvdro.load_library(), q.data_ptr()  # sizes that no array here has
+    for T, max_pages, text in ((1 << 29, 1, "2^30"), (3, (1 << 26) + 1, "2^30"), ((1 << 30) + 1, 1, "2^30")):
+        st = lib.kvdro_kv_attend(c.handle, 1, T, 4, 0, p, None, p, p, p, max_pages, 1.0, 1, 0, 0.0, p, None, None, None)
+        assert st == kvdro.KVDRO_EINVAL and text in kvdro.kvdro_last_error(ctx)
     refused(att, c, dev(3, 3, 64), *args[2:5], dev(3, 3, 64), match="n_heads")
     refused(att, c, dev(3, 4, 68)[..., :64], *args[2:], match="multiple of 8")
     refused(att, *args[:5], dev(3 * 4 * 64 + 1)[1:].view(3, 4, 64), match="aligned")
