@@ -63,11 +63,6 @@ __device__ __forceinline__ void tc_alloc(uint32_t at) {
 __device__ __forceinline__ void tc_free(uint32_t tmem) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -722,16 +717,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
-// last of CTA c; four threads a row's sums, lanes along the rows as the pieces are laid out.  Bound by the latency of its
-// three dependent reads (what to join, the pieces), so four pieces are read at a time.
-constexpr int kJoinThreads = 128, kJoinRows = 32, kJoinAtOnce = 4;
-
-// A load that stays where it stands, so that several are in flight.
-__device__ __forceinline__ float4 load_now(const float* p) {
-    float4 x;
-    asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
-    return x;
-}
+// last of CTA c; eight threads a row's sums, lanes along the rows as the pieces are laid out.  Bound by the latency of its
+// dependent reads (what to join, the pieces), so many threads read little each, four pieces at a time.
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinAtOnce = 4;
 
 template <bool H, int D>
 __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
@@ -739,7 +727,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
     const Join j = a.joins[blockIdx.x];
     const int row_in = blockIdx.y * kJoinRows + (threadIdx.x & 31), part = threadIdx.x >> 5;
     if (j.last < 0 || row_in >= j.rows) return;
-    constexpr int kFloats = Shape<D>::kPieceFloats, N = D / 16;  // 16-byte vectors of a part
+    constexpr int kFloats = Shape<D>::kPieceFloats, N = D * 8 / kJoinThreads;  // 16-byte vectors of a part
     float m = -INFINITY, l = 0.f;
     float4 o[N];
 #pragma unroll
@@ -754,7 +742,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
             ml[k] = reinterpret_cast<const float2*>(piece + kRows * D)[row_in];
             if (c0 + k > j.last) ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-            for (int i = 0; i < N; i++) x[k][i] = load_now(piece + 4 * ((part * N + i) * kRows + row_in));
+            for (int i = 0; i < N; i++) x[k][i] = reinterpret_cast<const float4*>(piece)[(part * N + i) * kRows + row_in];
         }
         float to = m;
 #pragma unroll
@@ -778,11 +766,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
     const ChunkLine line(a);
     const int row = j.row0 + row_in, tok = line.token(row), h = j.h * a.group + row - tok * a.group;
     const int64_t t = j.q0 + tok;
-    uint4* const out = reinterpret_cast<uint4*>(a.out + t * a.out_tok + h * a.out_head + part * (D / 4));
+    uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + part * (4 * N));
 #pragma unroll
-    for (int i = 0; i < N; i += 2)
-        out[i / 2] = make_uint4(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv),
-                                pack2<H>(o[i + 1].x * inv, o[i + 1].y * inv), pack2<H>(o[i + 1].z * inv, o[i + 1].w * inv));
+    for (int i = 0; i < N; i++) out[i] = make_uint2(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv));
     if (a.lse && part == 0) a.lse[t * a.heads + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 

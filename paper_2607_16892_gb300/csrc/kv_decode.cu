@@ -142,15 +142,16 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
         const int p0 = __shfl_sync(~0u, pg[0], in_blk & 31), p1 = __shfl_sync(~0u, pg[1], in_blk & 31);
         gaps = (gaps & ~(3u << 2 * stage)) | ((p0 < 0 ? 1u : 0u) | (p1 < 0 ? 2u : 0u)) << 2 * stage;
         if (p0 >= 0 || p1 >= 0) {
-            if (lane == 0 && fetched != a.skip) {  // a test's wait runs out
-                const int slot = (in.at.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1);
-                const uint32_t bar = smem_u32(&s_bar[warp][stage]), to = ring + stage * kStage;
+            const int slot = __shfl_sync(~0u, (in.at.t.lo + in_blk * kKeys + warp * kSlice) & ((1 << a.page_shift) - 1), 0);
+            const int head = __shfl_sync(~0u, in.at.h, 0);
+            const uint32_t bar = __shfl_sync(~0u, smem_u32(&s_bar[warp][stage]), 0), to = __shfl_sync(~0u, ring + stage * kStage, 0);
+            if (fetched != a.skip && elect_one()) {  // (left out: a test's wait runs out)
                 const CUtensorMap* const map = in_v ? &vmap : &kmap;
                 mbar_expect(bar, kStage);
 #pragma unroll
                 for (int d = 0; d < D / 64; d++) {  // a page that is none reads as zeros
-                    load_box(to + d * (kSlice * 128), map, d * 64, slot, in.at.h, p0 >= 0 ? p0 : a.n_pages, bar);
-                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, in.at.h, p1 >= 0 ? p1 : a.n_pages, bar);
+                    load_box(to + d * (kSlice * 128), map, d * 64, slot, head, p0 >= 0 ? p0 : a.n_pages, bar);
+                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, head, p1 >= 0 ? p1 : a.n_pages, bar);
                 }
             }
             filled |= 1u << stage;
@@ -293,10 +294,10 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             for (int n = 0; n < NR; n++)
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
+                    const float shift[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const float to = m[n][i & 1];
-                        s[n][t][i] = exp2_fast(s[n][t][i] - (to == -INFINITY ? 0.f : to));
+                        s[n][t][i] = exp2_fast(s[n][t][i] - shift[i & 1]);
                         l[n][i & 1] += s[n][t][i];
                     }
                     pf[n][t][0] = transpose8(pack2<H>(s[n][t][0], s[n][t][1]));

@@ -88,6 +88,13 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
     return false;
 }
 
+// One lane of a whole warp, the same every time: what it issues takes its operands from uniform registers.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // A box of one page: coordinates d, slot, head, page.  Out-of-range pages read as zeros.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int d, int slot, int head, int page, uint32_t bar) {
     asm volatile(
