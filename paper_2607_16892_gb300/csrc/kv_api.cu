@@ -223,7 +223,7 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
     if (int rc = check_device(ctx, {{"k", k}, {"v", v}, {"slot", slot}})) return rc;
     const int64_t dense[2] = {(int64_t)kv->heads * kv->head_dim, kv->head_dim};
-    int64_t ks[2], vs[2];
+    int64_t ks[2] = {}, vs[2] = {};
     if (int rc = rows(ctx, "k", k, k_stride, 2, dense, ks)) return rc;
     if (int rc = rows(ctx, "v", v, v_stride, 2, dense, vs)) return rc;
     kvdro::AppendArgs a;
@@ -279,7 +279,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     if (lse)
         if (int rc = check_device(ctx, {{"lse", lse}})) return rc;
     const int64_t dense[2] = {(int64_t)n_heads * kv->head_dim, kv->head_dim};
-    int64_t qs[2], os[2];
+    int64_t qs[2] = {}, os[2] = {};
     if (int rc = rows(ctx, "q", q, q_stride, 2, dense, qs)) return rc;
     if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
     kvdro::AttendArgs a;

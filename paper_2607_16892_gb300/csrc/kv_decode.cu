@@ -13,8 +13,8 @@
 // The weights are rounded to the cache's type for the second product, which adds about as much error as the result's own
 // rounding.
 //
-// Measured (bf16, 8 key heads of 128, four query heads each): 64 requests of lognormal lengths up to 8192, 557 MB, 95 us =
-// 5.9 TB/s; 4 requests of 131072 with eight query heads each, 2148 MB, 328 us = 6.5 TB/s (a copy runs at 6.8); one request of
+// Measured (bf16, 8 key heads of 128, four query heads each): 64 requests of lognormal lengths up to 8192, 557 MB, 96 us =
+// 5.8 TB/s; 4 requests of 131072 with eight query heads each, 2148 MB, 325 us = 6.6 TB/s (a copy runs at 6.8); one request of
 // 1000, 10.4 us, all latency.
 #include "kv_device.cuh"
 

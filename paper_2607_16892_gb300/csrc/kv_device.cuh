@@ -295,7 +295,7 @@ struct Stretch {
         }
         __syncthreads();
         if (warp == 0 && at < total) {
-            Cursor c;
+            Cursor c = {};
             c.seek(line, found * per, base, at, lane);
             if (lane == 0) first = c;
         }

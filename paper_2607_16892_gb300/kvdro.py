@@ -348,6 +348,12 @@ class KvdroKv:
 
     __slots__ = ("handle", "ctx", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
 
+    def __del__(self):
+        try:
+            kvdro_kv_close(self)
+        except (AttributeError, TypeError):  # never opened, or the interpreter is going down
+            pass
+
 
 # A serving step makes these calls once per layer, so their host time counts: the checks of a good argument take few
 # attribute reads, and what is wrong with a bad one is found out afterwards.
