@@ -223,6 +223,7 @@ int kvdro_destroy(kvdro_ctx* ctx) {
     if (ctx->copy_done) cudaEventDestroy(ctx->copy_done);
     if (ctx->kv_done) cudaEventDestroy(ctx->kv_done);
     if (ctx->copy_stream) cudaStreamDestroy(ctx->copy_stream);
+    if (ctx->kv_side) cudaStreamDestroy(ctx->kv_side);
     cudaGetLastError();
     delete ctx;
     return KVDRO_OK;

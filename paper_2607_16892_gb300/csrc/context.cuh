@@ -62,10 +62,11 @@ struct kvdro_ctx {
     kvdro_kv* caches = nullptr;  // open handles
     kvdro::Buf kv_err;           // the word in which its kernels report what they met
     kvdro::Buf kv_pieces, kv_tickets, kv_joins;  // scratch of the attention kernels
+    cudaStream_t kv_side = nullptr;    // clears scratch and the status word; ordered with no caller's stream
     cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it
     unsigned long long kv_stream = 0;  // that call's stream, by its number
     bool kv_used = false;
-    bool kv_plan_ready = false, kv_ready = false;
+    bool kv_err_ready = false, kv_plan_ready = false, kv_ready = false;
 };
 
 // A page cache that the caller owns.

@@ -95,6 +95,15 @@ int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const i
     return KVDRO_OK;
 }
 
+// Zeros, there when the call returns, whatever stream uses them next.  (A memset on the default stream is neither waited for
+// by the host nor ordered with non-blocking streams, and would wait for the caller's work on that stream.)
+int clear(kvdro_ctx* ctx, void* p, size_t bytes) {
+    if (!ctx->kv_side) KV_CUDA(cudaStreamCreateWithFlags(&ctx->kv_side, cudaStreamNonBlocking), "creating a stream");
+    KV_CUDA(cudaMemsetAsync(p, 0, bytes, ctx->kv_side), "clearing scratch");
+    KV_CUDA(cudaStreamSynchronize(ctx->kv_side), "clearing scratch");
+    return KVDRO_OK;
+}
+
 // What the attention kernels need once per context: attributes, scratch.
 int prepare_attend(kvdro_ctx* ctx) {
     if (ctx->kv_ready) return KVDRO_OK;
@@ -106,16 +115,17 @@ int prepare_attend(kvdro_ctx* ctx) {
     if (int rc = ensure(ctx, ctx->kv_joins, sizeof(kvdro::Join) * (size_t)ctx->sms)) return rc;
     const size_t tickets = 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);
     if (int rc = ensure(ctx, ctx->kv_tickets, tickets)) return rc;
-    KV_CUDA(cudaMemset(ctx->kv_tickets.p, 0, tickets), "clearing scratch");
+    if (int rc = clear(ctx, ctx->kv_tickets.p, tickets)) return rc;
     ctx->kv_ready = true;
     return KVDRO_OK;
 }
 
 // The word in which page cache kernels report what they met.
 int error_word(kvdro_ctx* ctx) {
-    if (ctx->kv_err.p) return KVDRO_OK;
+    if (ctx->kv_err_ready) return KVDRO_OK;
     if (int rc = ensure(ctx, ctx->kv_err, 16)) return rc;
-    KV_CUDA(cudaMemset(ctx->kv_err.p, 0, 16), "clearing status");
+    if (int rc = clear(ctx, ctx->kv_err.p, 16)) return rc;
+    ctx->kv_err_ready = true;
     return KVDRO_OK;
 }
 
@@ -365,7 +375,7 @@ namespace kvdro {
 
 // What the page cache's kernels reported, cleared.  The stream has been waited for.
 int check_kv_errors(kvdro_ctx* ctx) {
-    if (!ctx->kv_err.p) return KVDRO_OK;
+    if (!ctx->kv_err_ready) return KVDRO_OK;
     int32_t bits = 0;
     KV_CUDA(cudaMemcpy(&bits, ctx->kv_err.p, sizeof(bits), cudaMemcpyDeviceToHost), "reading kernel status");
     if (!bits) return KVDRO_OK;
