@@ -305,9 +305,10 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
                     int32_t max_pages, double scale, int causal, int32_t window, double softcap, void* out,
                     const int64_t* out_stride, float* lse, void* stream);
 
-/* Wait for the context's last call's stream and report any asynchronous CUDA error, kernel timeout or value out
- * of range.  (Page cache calls on several streams: what kernels on the others found is reported
- * once they are done.) */
+/* Wait for the context's device work -- the streams of its last call outside the page cache and of its last page cache
+ * call, and its last kvdro_kv_attend -- and report any asynchronous CUDA error, kernel timeout or value out
+ * of range.  (Earlier page cache calls on yet other streams: what their kernels found is reported once they are
+ * done.) */
 int kvdro_sync(kvdro_ctx* ctx);
 
 /* Text of the last error on this context ("" if none).  Valid until the next call on ctx. */

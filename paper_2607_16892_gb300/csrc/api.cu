@@ -809,7 +809,10 @@ int kvdro_sync(kvdro_ctx* ctx) {
     ctx->err.clear();
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
-    KV_CUDA(cudaStreamSynchronize(ctx->last_stream), "synchronising");
+    const bool kv = ctx->kv_err_ready;  // there was a page cache call; was there another?
+    if (!kv || ctx->loaded || ctx->last_stream) KV_CUDA(cudaStreamSynchronize(ctx->last_stream), "synchronising");
+    if (kv)
+        if (int rc = kvdro::wait_kv(ctx)) return rc;
     KV_CUDA(cudaGetLastError(), "asynchronous error");
     if (int rc = check_kernel_errors(ctx, ctx->last_stream)) return rc;
     return kvdro::check_kv_errors(ctx);

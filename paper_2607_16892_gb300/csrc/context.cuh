@@ -30,7 +30,7 @@ struct kvdro_ctx {
     int fail_after = -1;  // test hook: the fail_after-th allocation of this context fails
     int skip_chunk = -1;  // test hook: grid kernels never copy this chunk, so their waits run out
     int allocs = 0;
-    cudaStream_t last_stream = nullptr;
+    cudaStream_t last_stream = nullptr;  // of the last call that is not one of the page cache's
 
     bool loaded = false;
     bool quads = false;  // the staged form of the loaded samples
@@ -66,6 +66,7 @@ struct kvdro_ctx {
     cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it
     unsigned long long kv_stream = 0;  // that call's stream, by its number
     bool kv_used = false;
+    cudaStream_t kv_last = nullptr;    // of the last page cache call
     bool kv_err_ready = false, kv_plan_ready = false, kv_ready = false;
 };
 
@@ -161,7 +162,8 @@ inline bool is_device_ptr(const void* p) {
     return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged;
 }
 
-int check_kv_errors(kvdro_ctx* ctx);  // kv_api.cu
+int wait_kv(kvdro_ctx* ctx);  // kv_api.cu
+int check_kv_errors(kvdro_ctx* ctx);
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

@@ -216,7 +216,7 @@ int kvdro_kv_plan(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages, int32_t B,
     kvdro::PlanArgs a{log2_of(page_size), n_pages, B, max_pages, T, cached, new_len, reserve, held, pool, table, ring, held_out,
                       pool_out, q_off, kv_len, slot, pos, static_cast<int32_t*>(ctx->kv_err.p)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    ctx->last_stream = s;
+    ctx->kv_last = s;
     KV_CUDA(kvdro::launch_kv_plan(a, ctx->sms, s), "plan kernel");
     return KVDRO_OK;
 }
@@ -259,7 +259,7 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
     a.vec_shift = log2_of(kv->head_dim / 8);
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    ctx->last_stream = s;
+    ctx->kv_last = s;
     KV_CUDA(kvdro::launch_kv_append(a, s), "append kernel");
     return KVDRO_OK;
 }
@@ -334,7 +334,7 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     a.skip = ctx->skip_chunk;
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    ctx->last_stream = s;
+    ctx->kv_last = s;
     // Calls share the scratch: one on another stream than the last waits for that one.  (By the streams' numbers: a new stream
     // may have an old one's handle.  Waiting in every case cost a small call 2 us.)
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
@@ -373,7 +373,14 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
 
 namespace kvdro {
 
-// What the page cache's kernels reported, cleared.  The stream has been waited for.
+// Waits for the last page cache call, and for the last attention call, which may be on another stream.
+int wait_kv(kvdro_ctx* ctx) {
+    KV_CUDA(cudaStreamSynchronize(ctx->kv_last), "synchronising");
+    if (ctx->kv_used) KV_CUDA(cudaEventSynchronize(ctx->kv_done), "synchronising");
+    return KVDRO_OK;
+}
+
+// What the page cache's kernels reported, cleared.  They have been waited for.
 int check_kv_errors(kvdro_ctx* ctx) {
     if (!ctx->kv_err_ready) return KVDRO_OK;
     int32_t bits = 0;

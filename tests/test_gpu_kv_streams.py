@@ -1,5 +1,6 @@
 """Page cache calls on several streams: scratch, status and what kvdro_sync waits for."""
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -46,3 +47,59 @@ def test_scratch_of_a_new_context_is_clear_whatever_stream_uses_it_first(lens):
             kvdro.kvdro_sync(ctx)
         finally:
             kvdro.kvdro_destroy(ctx)
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def small_plan(ctx, stream=None):
+    a = [ints(0), ints(1), ints(0), ints(-1)[None], ints(0, 1), ints(0, 2), ints(0), ints(0, 0), ints(0, 0), ints(0), ints(0)]
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    kvdro.kvdro_kv_plan(ctx, 16, *a, stream=stream)
+    return a
+
+
+def test_sync_waits_for_a_grid_call_on_another_stream():
+    ctx = kvdro.kvdro_create(0)
+    try:
+        kvdro.kvdro_load_samples(ctx, 1, np.array([0, 100]), np.arange(100, dtype=np.int32), np.array([100], np.int32), None)
+        r, side = np.arange(10, dtype=np.int32), torch.cuda.Stream()
+        cost = torch.zeros((1, 1, 1, 10), dtype=torch.float64, device="cuda")
+
+        def grid(stream):
+            kvdro.kvdro_eval_dual(ctx, 10, r, 1, [1.0], 1, [10.0], [1.0], cost=cost, stream=stream)
+        grid(side)
+        want = cost.clone()
+        small_plan(ctx)
+        kvdro.kvdro_sync(ctx)
+        cost.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(A_WHILE)
+        grid(side)
+        small_plan(ctx)
+        kvdro.kvdro_sync(ctx)
+        assert side.query()
+        assert torch.equal(cost, want)
+    finally:
+        kvdro.kvdro_destroy(ctx)
+
+
+def test_sync_waits_for_the_last_attention_on_another_stream():
+    case = Case([(1, 9000)] * 4, "bf16", 128, 8, 2, 16, seed=1)
+    ctx, side = kvdro.kvdro_create(0), torch.cuda.Stream()
+    try:
+        case.check(*case.run(ctx, stream=side))
+        cache, out = kvdro.kvdro_kv_open(ctx, case.k, case.v), torch.empty_like(case.q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(A_WHILE)
+        kvdro.kvdro_kv_attend(cache, case.q, case.q_off, case.kv_len, case.table, out, stream=side)
+        small_plan(ctx)
+        kvdro.kvdro_sync(ctx)
+        assert side.query()
+        case.check(out, None)
+    finally:
+        kvdro.kvdro_destroy(ctx)
