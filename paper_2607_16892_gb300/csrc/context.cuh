@@ -60,7 +60,7 @@ struct kvdro_ctx {
 
     // The page cache
     kvdro_kv* caches = nullptr;  // open handles
-    kvdro::Buf kv_err;           // the word in which its kernels report what they met
+    kvdro::Buf kv_err;           // the word in which its kernels report what they met, and the one it is taken to
     kvdro::Buf kv_pieces, kv_tickets, kv_joins;  // scratch of the attention kernels
     cudaStream_t kv_side = nullptr;    // clears scratch and the status word; ordered with no caller's stream
     cudaEvent_t kv_done = nullptr;     // completes when the last attention call outside captures is done with it

@@ -7,11 +7,13 @@
 
 namespace kvdro {
 
-// Error bits that page cache kernels report in ctx->kv_err.
+// Error bits that page cache kernels report in the first word of ctx->kv_err.
 constexpr int kKvErrRange = 1;
 constexpr int kKvErrTimeout = 2;
 
 constexpr int kKvMaxRequests = 16384;
+
+cudaError_t launch_kv_take(int32_t* err, cudaStream_t s);  // moves the first word to the second
 
 struct PlanArgs {
     int32_t page_shift, n_pages, B, max_pages, T;

@@ -380,15 +380,24 @@ int wait_kv(kvdro_ctx* ctx) {
     return KVDRO_OK;
 }
 
-// What the page cache's kernels reported, cleared.  They have been waited for.
+// What the page cache's kernels reported, cleared.  They have been waited for, but earlier calls on other streams may still
+// run: the word is taken in one step, so that what they report meanwhile is kept for the next time.
 int check_kv_errors(kvdro_ctx* ctx) {
     if (!ctx->kv_err_ready) return KVDRO_OK;
+    auto read = [&](int i, int32_t* to) {
+        KV_CUDA(cudaMemcpyAsync(to, static_cast<int32_t*>(ctx->kv_err.p) + i, sizeof(*to), cudaMemcpyDeviceToHost, ctx->kv_side),
+                "reading kernel status");
+        KV_CUDA(cudaStreamSynchronize(ctx->kv_side), "reading kernel status");
+        return (int)KVDRO_OK;
+    };
     int32_t bits = 0;
-    KV_CUDA(cudaMemcpy(&bits, ctx->kv_err.p, sizeof(bits), cudaMemcpyDeviceToHost), "reading kernel status");
+    if (int rc = read(0, &bits)) return rc;
     if (!bits) return KVDRO_OK;
-    KV_CUDA(cudaMemset(ctx->kv_err.p, 0, sizeof(bits)), "clearing status");
-    if (bits & kKvErrTimeout) {  // arrivals may be missing
-        KV_CUDA(cudaMemset(ctx->kv_tickets.p, 0, ctx->kv_tickets.bytes), "clearing scratch");
+    KV_CUDA(launch_kv_take(static_cast<int32_t*>(ctx->kv_err.p), ctx->kv_side), "taking kernel status");
+    if (int rc = read(1, &bits)) return rc;
+    if (bits & kKvErrTimeout) {  // arrivals may be missing; replays of captured calls may be counting theirs
+        KV_CUDA(cudaDeviceSynchronize(), "synchronising");
+        if (int rc = clear(ctx, ctx->kv_tickets.p, ctx->kv_tickets.bytes)) return rc;
         return fail(ctx, KVDRO_ETIMEOUT, "an attention kernel gave up a bounded wait");
     }
     return fail(ctx, KVDRO_ERANGE, "a page cache kernel met a page number, slot or length outside its range");

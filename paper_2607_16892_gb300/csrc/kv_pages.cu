@@ -297,7 +297,14 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(AppendArgs a, int 
     }
 }
 
+__global__ void k_kv_take(int32_t* err) { err[1] = atomicExch(err, 0); }
+
 }  // namespace
+
+cudaError_t launch_kv_take(int32_t* err, cudaStream_t s) {
+    k_kv_take<<<1, 1, 0, s>>>(err);
+    return cudaGetLastError();
+}
 
 cudaError_t kv_plan_prepare() {
     return cudaFuncSetAttribute(k_kv_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * 4 * kKvMaxRequests);

@@ -103,3 +103,62 @@ def test_sync_waits_for_the_last_attention_on_another_stream():
         case.check(out, None)
     finally:
         kvdro.kvdro_destroy(ctx)
+
+
+def test_reports_are_neither_lost_nor_repeated():
+    """Bad slots on a side stream at about the time when another stream's report is taken."""
+    ctx, side = kvdro.kvdro_create(0), torch.cuda.Stream()
+    k = torch.zeros((2, 16, 1, 64), dtype=torch.bfloat16, device="cuda")
+    bad, new = ints(32), torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+
+    def reports():
+        try:
+            kvdro.kvdro_sync(ctx)
+        except kvdro.KvdroError as e:
+            assert e.status == kvdro.KVDRO_ERANGE
+            return True
+        return False
+    try:
+        cache = kvdro.kvdro_kv_open(ctx, k, k.clone())
+        torch.cuda.synchronize()
+        for i in range(100):
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(1 + 500 * i)
+            kvdro.kvdro_kv_append(cache, new, new, bad, stream=side)
+            late = not side.query()
+            kvdro.kvdro_kv_append(cache, new, new, bad)
+            assert reports(), i
+            late &= not side.query()
+            side.synchronize()
+            assert reports() or not late, i
+            assert not reports(), i
+    finally:
+        kvdro.kvdro_destroy(ctx)
+
+
+def test_scratch_is_clear_after_a_wait_that_ran_out(monkeypatch):
+    """A context whose kernels leave out every CTA's 31st copy: a large call runs out of its wait, small ones do not come
+    that far.  They follow at once, on the same stream and on others, their rows split over many CTAs."""
+    big, small = (Case(lens, "bf16", 64, 4, 2, 16, seed=1) for lens in ([(1, 20000)] * 60, [(1, 20000)]))
+    monkeypatch.setenv("KVDRO_TEST_SKIP_CHUNK", "30")
+    ctx = kvdro.kvdro_create(0)
+    monkeypatch.delenv("KVDRO_TEST_SKIP_CHUNK")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    try:
+        caches = [kvdro.kvdro_kv_open(ctx, c.k, c.v) for c in (big, small)]
+        out, outs = torch.empty_like(big.q), [torch.empty_like(small.q) for _ in range(8)]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            kvdro.kvdro_kv_attend(caches[0], big.q, big.q_off, big.kv_len, big.table, out, stream=streams[0], max_q=1)
+            small_plan(ctx)
+            with pytest.raises(kvdro.KvdroError) as e:
+                kvdro.kvdro_sync(ctx)
+            assert e.value.status == kvdro.KVDRO_ETIMEOUT
+            for i, o in enumerate(outs):
+                kvdro.kvdro_kv_attend(caches[1], small.q, small.q_off, small.kv_len, small.table, o, stream=streams[i % 2], max_q=1)
+            kvdro.kvdro_sync(ctx)
+            torch.cuda.synchronize()
+            for o in outs:
+                small.check(o, None)
+    finally:
+        kvdro.kvdro_destroy(ctx)
