@@ -257,12 +257,13 @@ int kvdro_kv_close(kvdro_kv* kv);
  *   cached, new_len, held  int32[B];  reserve: int32[B] or NULL (no reservations).
  *   table      int32[B][max_pages], updated: entries held[b] <= j < held_out[b] are written.
  *   ring       int32[n_pages], updated: returned pages are written behind the last.
- *   pool       int32[2];  pool_out: int32[2];  held_out: int32[B] (held and pool are not changed, and
- *              must not overlap their outputs: the same call again gives the same results).
+ *   pool       int32[2];  pool_out: int32[2];  held_out: int32[B] (held and pool are not changed: the same
+ *              call again gives the same results).
  *   q_off      int32[B+1]  prefix sums of max(new_len, 0): request b's tokens are q_off[b] .. q_off[b+1]-1.
  *   kv_len     int32[B]    cached + new_len, the tokens that kvdro_kv_attend sees; 0 if refused or done.
  *   slot, pos  int32[T] (pos may be NULL; T >= 0)  page * page_size + offset, and the position in the request, of every
  *              new token; -1 behind the last token.  More new tokens than T is a range error (the rest is left out).
+ * No array that is written (kv_len over cached, say) may overlap another of the call: KVDRO_EINVAL.
  */
 int kvdro_kv_plan(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages, int32_t B, int32_t max_pages, int32_t T,
                   const int32_t* cached, const int32_t* new_len, const int32_t* reserve, const int32_t* held,

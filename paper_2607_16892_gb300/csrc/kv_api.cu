@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
+#include <iterator>
 #include <new>
 
 #include "context.cuh"
@@ -59,6 +60,17 @@ int check_device(kvdro_ctx* ctx, std::initializer_list<Arg> args) {
         if (!is_device_ptr(x.p)) return fail(ctx, KVDRO_EINVAL, "%s must be device memory", x.name);
     }
     return KVDRO_OK;
+}
+
+struct Extent {
+    const char* name;
+    const int32_t* p;
+    int64_t n;
+};
+
+bool overlap(const Extent& x, const Extent& y) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+    return a < b + 4 * (uintptr_t)y.n && b < a + 4 * (uintptr_t)x.n && x.n > 0 && y.n > 0;
 }
 
 // Strides of rows of 16-byte vectors: `n` of them into `out`, from the caller's or the contiguous ones.
@@ -206,8 +218,16 @@ int kvdro_kv_plan(kvdro_ctx* ctx, int32_t page_size, int32_t n_pages, int32_t B,
         if (int rc = check_device(ctx, {{"slot", slot}})) return rc;
     if (T > 0 && pos)
         if (int rc = check_device(ctx, {{"pos", pos}})) return rc;
-    if (held_out < held + B && held < held_out + B) return fail(ctx, KVDRO_EINVAL, "held_out overlaps held");
-    if (pool_out < pool + 2 && pool < pool_out + 2) return fail(ctx, KVDRO_EINVAL, "pool_out overlaps pool");
+    // CTAs read lengths again after others have written results, in no order.
+    const Extent written[] = {{"held_out", held_out, B}, {"pool_out", pool_out, 2}, {"q_off", q_off, B + 1}, {"kv_len", kv_len, B},
+                              {"slot", slot, T}, {"pos", pos, pos ? T : 0}, {"table", table, (int64_t)B * max_pages}, {"ring", ring, n_pages}};
+    const Extent read[] = {{"held", held, B}, {"pool", pool, 2}, {"cached", cached, B}, {"new_len", new_len, B}, {"reserve", reserve, reserve ? B : 0}};
+    for (const Extent* w = std::begin(written); w != std::end(written); w++) {
+        for (const Extent& r : read)
+            if (overlap(*w, r)) return fail(ctx, KVDRO_EINVAL, "%s overlaps %s", w->name, r.name);
+        for (const Extent* o = std::begin(written); o != w; o++)
+            if (overlap(*w, *o)) return fail(ctx, KVDRO_EINVAL, "%s overlaps %s", w->name, o->name);
+    }
     if (!ctx->kv_plan_ready) {
         KV_CUDA(kvdro::kv_plan_prepare(), "preparing the plan kernel");
         ctx->kv_plan_ready = true;
