@@ -192,7 +192,8 @@ struct Pieces : Walk<ChunkLine> {
 
 // Q of a half into shared memory, by its four warps: rows of 16-byte chunks, sixteen (or eight) lanes to a row; arrives at
 // `bar` (128 arrivals) once it is there, while the threads go on.  Rows beyond the half's are zero; a negative scale turns Q's
-// sign, so that the largest score is the largest product.
+// sign, so that the largest score is the largest product: by ordinary stores, each thread's made known to the tensor cores' proxy
+// and released by its arrival (the arrival of asynchronous copies would order none of them).
 template <int D>
 __device__ __forceinline__ void load_q(const AttendArgs& a, const Pieces& w, int half, uint32_t to, int tid, uint32_t bar) {
     constexpr int C = D / 8, kAtOnce = kHalfRows / C;
@@ -214,7 +215,12 @@ __device__ __forceinline__ void load_q(const AttendArgs& a, const Pieces& w, int
                          : "memory");
         }
     }
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+    if (a.scale >= 0.f) {
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+    } else {
+        fence_proxy_async();
+        mbar_arrive(bar);
+    }
 }
 
 // 16-bit results of 32 columns, 32 or 16 bytes a store.
