@@ -419,6 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[half][i >> 1]));
+                            __syncwarp();
                         }
                     }
                     sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
@@ -457,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
+                    __syncwarp();  // lanes came through loops of their own; the load takes a whole warp
                     uint32_t got[1][32];
                     uint32_t(&o)[32] = got[0];
                     if (some) {
@@ -482,13 +484,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                     }
-                    if (!valid) continue;
-                    if (whole) {
+                    if (valid && whole) {
                         uint32_t x[16];
 #pragma unroll
                         for (int i = 0; i < 16; i++) x[i] = pack2<H>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
                         store_row(a.out + t * a.out_tok + h * a.out_head + c, x, wide);
-                    } else {
+                    } else if (valid) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             reinterpret_cast<uint4*>(piece)[(c + i) / 4 * kRows + prow] = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
@@ -509,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     j.rows = min(kRows, cur.at.r.rows - j.row0);
                     j.last = (int)divide(cur.at.start + cur.at.t.blocks - 1, sh.part.share);
                 }
+                __syncwarp();
                 tc_fence_before();
             }
         } else {
