@@ -256,7 +256,9 @@ int kvdro_kv_close(kvdro_kv* kv);
  *   page_size, n_pages   as in kvdro_kv_open;  1 <= B <= 16384;  max_pages >= 1, max_pages * page_size <= 2^30.
  *   cached, new_len, held  int32[B];  reserve: int32[B] or NULL (no reservations).
  *   table      int32[B][max_pages], updated: entries held[b] <= j < held_out[b] are written.
- *   ring       int32[n_pages], updated: returned pages are written behind the last.
+ *   ring       int32[n_pages], updated: returned pages are written behind the last.  An entry, of a table or of the
+ *              ring, that is no page number is a range error each time it is returned or handed out; it stays in the ring, and in
+ *              the table of the request that gets it, as -1 (tokens there have slot -1).
  *   pool       int32[2];  pool_out: int32[2];  held_out: int32[B] (held and pool are not changed: the same
  *              call again gives the same results).
  *   q_off      int32[B+1]  prefix sums of max(new_len, 0): request b's tokens are q_off[b] .. q_off[b+1]-1.

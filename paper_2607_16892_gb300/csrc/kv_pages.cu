@@ -213,7 +213,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(PlanArgs a) {
         }
         int64_t to = (int64_t)head + n_free;
         to = ring_at(ring_at(to) + i);
-        a.ring[to] = a.table[(int64_t)lo * a.max_pages + (i - (s_back[lo] & 0x7fffffff))];
+        int32_t page = a.table[(int64_t)lo * a.max_pages + (i - (s_back[lo] & 0x7fffffff))];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) {  // none, and stays none in the ring
+            bad = true;
+            page = -1;
+        }
+        a.ring[to] = page;
     }
     // Tokens four at a time: mostly of one request and one page, found once.
     const int tokens = (int)min(all.q, (uint32_t)a.T), mask = (1 << a.page_shift) - 1;

@@ -1,0 +1,55 @@
+"""Values out of range in device memory: what is left out, what is reported, and what is nobody's business."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2607_16892_gb300 import kvdro  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    c = kvdro.kvdro_create(0)
+    yield c
+    kvdro.kvdro_destroy(c)
+
+
+def reported(ctx):
+    with pytest.raises(kvdro.KvdroError) as e:
+        kvdro.kvdro_sync(ctx)
+    assert e.value.status == kvdro.KVDRO_ERANGE
+    kvdro.kvdro_sync(ctx)  # once
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("bad", [-1, 20, 2 ** 31 - 1])
+def test_a_returned_page_that_is_none_is_reported_and_stays_none(ctx, bad):
+    """Request 1 is done; one of its three entries holds no page number."""
+    n, page = 20, 16
+    table = torch.full((2, 6), -1, dtype=torch.int32, device="cuda")
+    table[0, :2], table[1, :3] = ints(4, 5), ints(7, bad, 9)
+    ring = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    ring[18:], ring[:13] = ints(0, 1), ints(2, 3, 6, *range(10, 20))
+    pool, held = ints(18, 15), ints(2, 3)
+    held_out, pool_out, q_off, kv_len, slot = ints(0, 0), ints(0, 0), ints(0, 0, 0), ints(0, 0), ints(0)
+    kvdro.kvdro_kv_plan(ctx, page, ints(20, 40), ints(1, -1), held, table, ring, pool, held_out, pool_out, q_off, kv_len, slot)
+    reported(ctx)
+    assert pool_out.tolist() == [18, 18] and held_out.tolist() == [2, 0]
+    assert ring[13:16].tolist() == [7, -1, 9]
+    assert slot.tolist() == [5 * page + 4]
+    # the next request gets it: reported again, its token there has no slot
+    table, held = table.clone(), ints(2, 0)
+    slot, pos = torch.full((260,), 99, dtype=torch.int32, device="cuda"), torch.full((260,), 99, dtype=torch.int32, device="cuda")
+    table = torch.cat([table, torch.full((2, 11), -1, dtype=torch.int32, device="cuda")], 1)
+    kvdro.kvdro_kv_plan(ctx, page, ints(21, 0), ints(0, 260), held, table, ring, pool_out.clone(), held_out, pool_out, q_off, kv_len, slot, pos)
+    reported(ctx)
+    assert held_out.tolist() == [2, 17] and pool_out.tolist() == [15, 1] and kv_len.tolist() == [21, 260]
+    assert table[1].tolist() == [0, 1, 2, 3, 6, *range(10, 20), 7, -1]
+    assert pos.tolist() == list(range(260))
+    assert slot.tolist() == [page * p + i for p in (0, 1, 2, 3, 6, *range(10, 20), 7) for i in range(page)] + [-1] * 4
