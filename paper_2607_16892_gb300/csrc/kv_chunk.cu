@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                     }
-                    const float shift = m == -INFINITY ? 0.f : m;
+                    const float shift = (m == -INFINITY ? 0.f : m) - kLift<H>;
                     float2 sum[4] = {};
 #pragma unroll 2
                     for (int i = 0; i < 4; i++) {
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (valid) {
                     if (whole) {
-                        if (a.lse) a.lse[t * a.heads + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+                        if (a.lse) a.lse[t * a.heads + h] = log_sum<H>(m, l);
                     } else {
                         reinterpret_cast<float2*>(piece + kRows * D)[prow] = make_float2(m, l);
                     }
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
     uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + part * (4 * N));
 #pragma unroll
     for (int i = 0; i < N; i++) out[i] = make_uint2(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv));
-    if (a.lse && part == 0) a.lse[t * a.heads + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+    if (a.lse && part == 0) a.lse[t * a.heads + h] = log_sum<H>(m, l);
 }
 
 template <bool H, int D>

@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             for (int n = 0; n < NR; n++)
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
-                    const float shift[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
+                    const float shift[2] = {(m[n][0] == -INFINITY ? 0.f : m[n][0]) - kLift<H>, (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kLift<H>};
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         s[n][t][i] = exp2_fast(s[n][t][i] - shift[i & 1]);
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 *reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + c) =
                     make_uint2(pack2<H>(x.x * inv, x.y * inv), pack2<H>(x.z * inv, x.w * inv));
-                if (a.lse && c == 0) a.lse[t * a.heads + h] = sum == 0.f ? -INFINITY : kLn2 * (to + log2f(sum));
+                if (a.lse && c == 0) a.lse[t * a.heads + h] = log_sum<H>(to, sum);
             };
             constexpr int kQuads = D / 4;
             // Each warp's sums go over its own last stage, whose next copy waits for that; eight rows at a time.
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
                         const float inv = sum == 0.f ? 0.f : 1.f / sum;
                         uint32_t* const to_out = reinterpret_cast<uint32_t*>(a.out + t * a.out_tok + h * a.out_head + V * lane);
                         for (int i = 0; i < V; i += 2) to_out[i / 2] = pack2<H>(x[i] * inv, x[i + 1] * inv);
-                        if (a.lse && lane == 0) a.lse[t * a.heads + h] = sum == 0.f ? -INFINITY : kLn2 * (to + log2f(sum));
+                        if (a.lse && lane == 0) a.lse[t * a.heads + h] = log_sum<H>(to, sum);
                     }
                 }
             }

@@ -27,6 +27,17 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
     if constexpr (H) return __half22float2(*reinterpret_cast<__half2*>(&w));
     else return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&w));
 }
+// Weights are 2^(s - m + kLift), and so are their sums.  FP16 has no weights below 2^-25, and 32768 of them may be a result's
+// whole component: 2^7 moves that to 2^-32 of the row's largest, while the largest stays at or below 2^15 (m is raised
+// when a row's maximum passes it by 2^8).  BF16 has FP32's exponents.
+template <bool H>
+constexpr float kLift = H ? 7.f : 0.f;
+// The log sum of a row (natural), from the m that its sum refers to.
+template <bool H>
+__device__ __forceinline__ float log_sum(float m, float sum) {
+    return sum == 0.f ? -INFINITY : kLn2 * (m + (log2f(sum) - kLift<H>));
+}
+
 // Whether either half is an infinity or NaN: all exponent bits set, so that one more carries into the sign's place.
 template <bool H>
 __device__ __forceinline__ bool any_nonfinite(uint32_t w) {
