@@ -289,7 +289,7 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
  *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q . k_j),   f(x) = x, or softcap tanh(x / softcap)
  * over the positions j < kv_len[b] with j <= p (causal) and j > p - window (window > 0).  A token that sees
  * no position gets out = 0 and lse = -infinity.  What is stored at unseen positions does not
- * matter, NaN included.  Products are of the cache's dtype with FP32 sums; the softmax is FP32, its
+ * matter, NaN included, nor do the table's entries of pages that no token of the request sees (behind a window, say).  Products are of the cache's dtype with FP32 sums; the softmax is FP32, its
  * weights are rounded to the cache's dtype for the product with v.
  *   B          requests, 1 <= B <= 16384;  T: tokens, T >= 0; tokens beyond T are left out, and T tokens of out and lse
  *              are written (zeros and -infinity for tokens of no request).

@@ -619,11 +619,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 int note = 0;
                 const int n = kKeys >> a.page_shift;
                 while (w.more && ok) {
+                    const int seen_lo = line.seen(w.at.r, line.token(w.at.rt * kRows)).x;
                     for (int blk = w.p0; blk < w.p1 && ok; blk++, note++) {
                         const int j = w.at.t.lo + blk * kKeys + (lane << a.page_shift);
                         int page = a.n_pages;  // past the last page: zeros
                         bool none = false;
-                        if (lane < n && j < w.at.t.hi) {
+                        if (lane < n && j < w.at.t.hi && j + (1 << a.page_shift) > seen_lo) {  // else no row's business
                             page = a.table[(int64_t)w.at.b * a.max_pages + (j >> a.page_shift)];
                             if ((uint32_t)page >= (uint32_t)a.n_pages) {
                                 page = a.n_pages;

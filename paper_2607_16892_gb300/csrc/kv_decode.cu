@@ -129,10 +129,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
             pg_rt = in.at.rt;
             pg_blk = in_blk >> 5;
             const int j = in.at.t.lo + ((in_blk & ~31) + lane) * kKeys + warp * kSlice;
+            const int seen_lo = line.seen(in.at.r, line.token(in.at.rt * kRows)).x;
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 pg[i] = -1;
-                if (j + 16 * i < in.at.t.hi) {
+                if (j + 16 * i < in.at.t.hi && ((j + 16 * i) | (slots - 1)) >= seen_lo) {  // else no row's business
                     const int page = a.table[(int64_t)in.at.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
                     if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
                     else range = true;

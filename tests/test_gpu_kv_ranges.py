@@ -6,6 +6,8 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2607_16892_gb300 import kvdro  # noqa: E402
+from tests.kv_exact import worst  # noqa: E402
+from tests.kv_support import Case  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -53,3 +55,20 @@ def test_a_returned_page_that_is_none_is_reported_and_stays_none(ctx, bad):
     assert table[1].tolist() == [0, 1, 2, 3, 6, *range(10, 20), 7, -1]
     assert pos.tolist() == list(range(260))
     assert slot.tolist() == [page * p + i for p in (0, 1, 2, 3, 6, *range(10, 20), 7) for i in range(page)] + [-1] * 4
+
+
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("q", [1, 3, 40, 300])
+def test_pages_that_no_row_sees_are_nobodys_business(ctx, q, page):
+    """Behind a window a server may have given pages away: their entries are not looked at, however the blocks lie."""
+    for kv, window in ((500, 100), (777, 33), (1000, 512)):
+        case = Case([(q, kv), (1, 5)], "bf16", 128, 8, 2, page, seed=q)
+        first = max(0, kv - q - window + 1)  # the first position that a row sees
+        case.table[0, :first // page] = -1
+        out, lse = case.run(ctx, window=window)
+        kvdro.kvdro_sync(ctx)
+        assert worst(case, out, lse, 0, window=window) <= 1
+        if first // page < kv // page:  # one that rows do see
+            case.table[0, first // page] = -1
+            case.run(ctx, window=window)
+            reported(ctx)
