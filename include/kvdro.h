@@ -214,7 +214,7 @@ int kvdro_eval_grid_noalloc(int32_t K, const int64_t* offsets, const int32_t* le
  *     kvdro_kv_append   the new tokens' keys and values into those slots     (once per layer)
  *     kvdro_kv_attend   the new tokens' attention over their requests' pages (once per layer)
  * The paper's data plane runs a paged cache of this kind unchanged beneath its decisions (Fig. 1, Sec. 2).
- * All arrays are device memory and every call is asynchronous on `stream` and allocates nothing, so
+ * All arrays are memory of the context's device (or managed) and every call is asynchronous on `stream` and allocates nothing, so
  * that calls can be captured into a CUDA graph (after one call of the same kind outside a capture,
  * which loads its kernels).  A value in device memory that is out of range is never followed: the kernels leave
  * out what it stands for and the next kvdro_sync() returns KVDRO_ERANGE.

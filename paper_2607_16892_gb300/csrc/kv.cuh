@@ -13,6 +13,8 @@ constexpr int kKvErrTimeout = 2;
 
 constexpr int kKvMaxRequests = 16384;
 
+const char* kv_not_usable(const cudaPointerAttributes& at, int device);  // kv_api.cu
+
 cudaError_t launch_kv_take(int32_t* err, cudaStream_t s);  // moves the first word to the second
 
 struct PlanArgs {

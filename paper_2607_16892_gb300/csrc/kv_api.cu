@@ -14,7 +14,6 @@ using kvdro::cuda_fail;
 using kvdro::DeviceGuard;
 using kvdro::ensure;
 using kvdro::fail;
-using kvdro::is_device_ptr;
 using kvdro::NvtxRange;
 
 namespace {
@@ -57,7 +56,12 @@ struct Arg {
 int check_device(kvdro_ctx* ctx, std::initializer_list<Arg> args) {
     for (const Arg& x : args) {
         if (!x.p) return fail(ctx, KVDRO_EINVAL, "%s is required", x.name);
-        if (!is_device_ptr(x.p)) return fail(ctx, KVDRO_EINVAL, "%s must be device memory", x.name);
+        cudaPointerAttributes at;
+        if (cudaPointerGetAttributes(&at, x.p) != cudaSuccess) {
+            cudaGetLastError();
+            at = {};
+        }
+        if (const char* what = kvdro::kv_not_usable(at, ctx->device)) return fail(ctx, KVDRO_EINVAL, "%s must be %s", x.name, what);
     }
     return KVDRO_OK;
 }
@@ -392,6 +396,13 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
 }  // extern "C"
 
 namespace kvdro {
+
+// What memory with these attributes should be for a context of this device, or null if it is that.
+const char* kv_not_usable(const cudaPointerAttributes& at, int device) {
+    if (at.type == cudaMemoryTypeManaged) return nullptr;
+    if (at.type != cudaMemoryTypeDevice) return "device memory";
+    return at.device == device ? nullptr : "memory of the context's device";
+}
 
 // Waits for the last page cache call, and for the last attention call, which may be on another stream.
 int wait_kv(kvdro_ctx* ctx) {
