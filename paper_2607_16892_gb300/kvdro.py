@@ -8,8 +8,9 @@ cannot be loaded, the first call raises.
 
 Array arguments may be NumPy arrays (host memory) or torch tensors (host or
 CUDA memory); the library itself tells host from device pointers.  Streams may
-be a ``torch.cuda.Stream``, a raw ``cudaStream_t`` integer, or None (the legacy
-default stream).
+be a ``torch.cuda.Stream``, a raw ``cudaStream_t`` integer, or None: the legacy
+default stream, except for the page cache's calls, which take torch tensors only and
+go to torch's current stream then.
 """
 
 from __future__ import annotations
@@ -379,13 +380,15 @@ _I2, _I3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
 _lib_kv = _i32 = _f32 = None  # the loaded library and torch's dtypes
+_current_stream = None  # torch's current stream of a device, as a number (its public form takes a microsecond)
 
 
 def _kv_setup():
     """The library, once loaded."""
-    global _lib_kv, _i32, _f32
+    global _lib_kv, _i32, _f32, _current_stream
     if _i32 is None:
         import torch
+        _current_stream = torch._C._cuda_getCurrentRawStream
         _i32, _f32 = torch.int32, torch.float32
         _kv_types.update({torch.bfloat16: KVDRO_BF16, torch.float16: KVDRO_FP16})
     _lib_kv = load_library()
@@ -458,7 +461,8 @@ def kvdro_kv_plan(ctx, page_size: int, cached, new_len, held, table, ring, pool,
         None if reserve is None else _dev("reserve", reserve, i32, B), _dev("held", held, i32, B), _dev("table", table, i32),
         _dev("ring", ring, i32), _dev("pool", pool, i32, 2), _dev("held_out", held_out, i32, B),
         _dev("pool_out", pool_out, i32, 2), _dev("q_off", q_off, i32, B + 1), _dev("kv_len", kv_len, i32, B),
-        _dev("slot", slot, i32), None if pos is None else _dev("pos", pos, i32, T), None if stream is None else _stream(stream))
+        _dev("slot", slot, i32), None if pos is None else _dev("pos", pos, i32, T),
+        _current_stream(cached.get_device()) if stream is None else _stream(stream))
     if st:
         _check(ctx, st)
 
@@ -483,7 +487,7 @@ def kvdro_kv_append(cache: KvdroKv, k, v, slot, stream=None) -> None:
     kp, ks, T, heads = _heads(cache, "k", k, None, cache.heads)
     vp, vs, T, heads = _heads(cache, "v", v, T, heads)
     st = lib.kvdro_kv_append(_open_handle(cache), T, kp, ks, vp, vs, _dev("slot", slot, _i32, T),
-                             None if stream is None else _stream(stream))
+                             _current_stream(k.get_device()) if stream is None else _stream(stream))
     if st:
         _check(cache.ctx, st)
 
@@ -499,7 +503,8 @@ def kvdro_kv_attend(cache: KvdroKv, q, q_off, kv_len, table, out, lse=None, scal
     st = lib.kvdro_kv_attend(
         _open_handle(cache), B, T, heads, max_q, qp, qs, _dev("q_off", q_off, _i32, B + 1), _dev("kv_len", kv_len, _i32, B),
         _dev("table", table, _i32), max_pages, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
-        softcap, op, os_, None if lse is None else _dev("lse", lse, _f32, T * heads), None if stream is None else _stream(stream))
+        softcap, op, os_, None if lse is None else _dev("lse", lse, _f32, T * heads),
+        _current_stream(q.get_device()) if stream is None else _stream(stream))
     if st:
         _check(cache.ctx, st)
 

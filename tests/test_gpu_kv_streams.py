@@ -162,3 +162,63 @@ def test_scratch_is_clear_after_a_wait_that_ran_out(monkeypatch):
                 small.check(o, None)
     finally:
         kvdro.kvdro_destroy(ctx)
+
+
+def step(cache, ctx, new, out, stream=None):
+    """A plan for one request of 40 tokens, the write, the attention, with no stream named."""
+    a = {"cached": ints(0), "new_len": ints(40), "held": ints(0), "table": ints(-1, -1, -1)[None], "ring": ints(2, 0, 1), "pool": ints(0, 3),
+         "held_out": ints(0), "pool_out": ints(0, 0), "q_off": ints(0, 0), "kv_len": ints(0), "slot": torch.full_like(ints(*range(40)), -1)}
+
+    def go():
+        kvdro.kvdro_kv_plan(ctx, 16, **a, stream=stream)
+        kvdro.kvdro_kv_append(cache, new[:, :1], new[:, 1:], a["slot"], stream=stream)
+        kvdro.kvdro_kv_attend(cache, new[:, :1], a["q_off"], a["kv_len"], a["table"], out, max_q=40, stream=stream)
+    return go
+
+
+def test_calls_go_to_torchs_current_stream():
+    """Behind work of the current stream that fills what they read, and in a graph that is captured on it."""
+    ctx, side = kvdro.kvdro_create(0), torch.cuda.Stream()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    try:
+        k, v = (torch.zeros((3, 16, 1, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        cache = kvdro.kvdro_kv_open(ctx, k, v)
+        data = torch.randn((40, 2, 64), generator=g, device="cuda").bfloat16()
+        want, out, new = (torch.zeros((40, n, 64), dtype=torch.bfloat16, device="cuda") for n in (1, 1, 2))
+        new.copy_(data)
+        step(cache, ctx, new, want)()
+        kvdro.kvdro_sync(ctx)
+        assert want.abs().max() > 0
+        new.zero_()
+        go = step(cache, ctx, new, out)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(A_WHILE)
+            new.copy_(data)
+            go()
+            assert not side.query() and torch.cuda.default_stream().query()
+        side.synchronize()
+        kvdro.kvdro_sync(ctx)
+        assert torch.equal(out, want)
+        graph, new2, out2 = torch.cuda.CUDAGraph(), data.clone(), torch.zeros_like(out)
+        go = step(cache, ctx, new2, out2)
+        with torch.cuda.graph(graph):
+            go()
+        new2.copy_(data.flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(cache, ctx, new2, want)()
+        assert torch.equal(out2, want)
+        kvdro.kvdro_sync(ctx)
+        # a stream that is named is the one that is used
+        out.zero_()
+        go = step(cache, ctx, new2, out, stream=torch.cuda.default_stream())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(A_WHILE)
+            go()
+            torch.cuda.default_stream().synchronize()
+            assert not side.query()
+        assert torch.equal(out, want)
+    finally:
+        kvdro.kvdro_destroy(ctx)
