@@ -347,7 +347,7 @@ def kvdro_eval_grid_noalloc(K: int, offsets, lengths, L_max, L_in, R: int, r, NL
 class KvdroKv:
     """A handle of ``kvdro_kv_open`` and the tensors it describes, which it keeps alive."""
 
-    __slots__ = ("handle", "ctx", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
+    __slots__ = ("handle", "ctx", "owner", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
 
     def __del__(self):
         try:
@@ -375,7 +375,20 @@ def _dev(name: str, a: Any, dtype, n=None) -> int:
 
 
 _kv_types: dict = {}
-_caches: dict = {}  # handle of a context -> its open page caches, which kvdro_destroy closes
+
+class _Owner:
+    """What is open in one context: the library's handles, each closed once at most, and the objects that hold them."""
+
+    __slots__ = ("handles", "caches")
+
+    def __init__(self):
+        self.handles, self.caches = set(), weakref.WeakSet()
+
+
+_owners: dict = {}  # handle of a context -> what is open there, which kvdro_destroy closes
+# A cache may be closed by its finalizer, on whatever thread drops it and in the middle of any other call: the calls that
+# open, close and free handles run one at a time.
+_kv_lock = threading.RLock()
 _I2, _I3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
@@ -434,19 +447,25 @@ def kvdro_kv_open(ctx, k, v) -> KvdroKv:
     n, page, heads, d = k.shape
     strides = [_I3(*(t.stride(i) if t.shape[i] > 1 else 8 for i in range(3))) for t in (k, v)]
     h = ctypes.c_void_p()
-    _check(ctx, load_library().kvdro_kv_open(ctx, ctypes.byref(h), _kv_types[k.dtype], n, page, heads, d, k.data_ptr(),
-                                             strides[0], v.data_ptr(), strides[1]))
-    c = KvdroKv()
-    c.handle, c.ctx, c.k, c.v, c.dtype, c.heads, c.head_dim = h, ctx, k, v, k.dtype, heads, d
-    _caches.setdefault(getattr(ctx, "value", ctx), weakref.WeakSet()).add(c)
+    with _kv_lock:
+        _check(ctx, load_library().kvdro_kv_open(ctx, ctypes.byref(h), _kv_types[k.dtype], n, page, heads, d, k.data_ptr(),
+                                                 strides[0], v.data_ptr(), strides[1]))
+        c = KvdroKv()
+        c.owner = _owners.setdefault(getattr(ctx, "value", ctx), _Owner())
+        c.owner.handles.add(h.value)
+        c.handle, c.ctx, c.k, c.v, c.dtype, c.heads, c.head_dim = h, ctx, k, v, k.dtype, heads, d
+        c.owner.caches.add(c)
     return c
 
 
 def kvdro_kv_close(cache: KvdroKv) -> None:
-    if cache.handle:
-        load_library().kvdro_kv_close(cache.handle)
-        cache.handle = None
-        cache.k = cache.v = None
+    with _kv_lock:
+        handle, cache.handle = cache.handle, None
+        if handle:
+            cache.k = cache.v = None
+            if handle.value in cache.owner.handles:  # else freed with its context
+                cache.owner.handles.remove(handle.value)
+                load_library().kvdro_kv_close(handle)
 
 
 def kvdro_kv_plan(ctx, page_size: int, cached, new_len, held, table, ring, pool, held_out, pool_out, q_off, kv_len,
@@ -520,6 +539,10 @@ def kvdro_last_error(ctx) -> str:
 def kvdro_destroy(ctx) -> None:
     if ctx:
         _loaded.pop(getattr(ctx, "value", ctx), None)
-        for cache in list(_caches.pop(getattr(ctx, "value", ctx), ())):
-            kvdro_kv_close(cache)
-        load_library().kvdro_destroy(ctx)
+        with _kv_lock:
+            owner = _owners.pop(getattr(ctx, "value", ctx), None)
+            if owner is not None:
+                for cache in list(owner.caches):
+                    kvdro_kv_close(cache)
+                owner.handles.clear()  # of caches about to be finalized: the library frees them
+            load_library().kvdro_destroy(ctx)
