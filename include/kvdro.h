@@ -300,7 +300,7 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
  *              cache's dtype; 16-byte aligned, strides multiples of 8.
  *   q_off      int32[B+1], ascending from 0;  kv_len: int32[B];  table: int32[B][max_pages], max_pages * page_size <= 2^30.
  *   scale      finite;  causal: 0 or 1;  window >= 0 (0: none; needs causal);  softcap 0 (none) or in
- *              [2^-20, 1000]; capped scores are off by up to 2^-21 softcap.
+ *              [2^-20, 1000]; capped scores are off by up to 2^-20 softcap, also where they are small.
  *   lse        float [T][n_heads], log sum_j exp(s_j); may be NULL.
  */
 int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,

@@ -52,7 +52,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 // A score times log2(e), through the cap if there is one: cap tanh(y / cap) = cap (1 - 2 / (1 + exp(2 y / cap))), off by
-// a few 2^-24 of cap.  `mul` is scale * log2(e), or 2 log2(e) scale / cap; `cap2` is cap * log2(e).
+// 2^-20 of cap at most: 2^-22 of a quotient of up to 2 from the division, 2^-24 of it from its sum, 2^-23 and 2^-24 from the
+// exponential and its argument, 2^-24 from the difference.  `mul` is scale * log2(e), or 2 log2(e) scale / cap; `cap2` is cap * log2(e).
 __device__ __forceinline__ float score(float dot, float mul, float cap2) {
     const float y = dot * mul;
     if (cap2 == 0.f) return y;

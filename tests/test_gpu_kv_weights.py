@@ -1,4 +1,4 @@
-"""What the softmax weights and the pieces of split rows keep of a result, against 64 bits with tight bounds."""
+"""What the softmax weights, the cap and the pieces of split rows keep of a result, against 64 bits with tight bounds."""
 
 import numpy as np
 import pytest
@@ -68,3 +68,27 @@ def test_split_rows_within_bounds_of_their_weights(ctx, lens, D, Hq, Hkv, page):
     for b in range(len(lens)):
         assert worst(case, out, lse, b) <= 1
     kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("cap", [0.5, 30.0, 50.0, 1000.0])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("n", [1, 300])
+def test_a_capped_score_is_off_by_2_20_of_the_cap_at_most(ctx, cap, dtype, D, n):
+    """With one visible key the log sum is the capped score.  Queries and keys of one component, so that the product
+    is exact; scaling adds 2^-22 of the score, the units of log2 and back 2^-22 of the result."""
+    B = 300 // n
+    case = Case([(n, 1)] * B, dtype, D, 4, 1, 16, seed=1)
+    for b in range(B):
+        case.keys[b].zero_()
+        case.keys[b][..., 0] = 1.0
+        case.set(b, case.keys[b], case.values[b])
+    case.q.zero_()
+    x = torch.cat([torch.linspace(-5, 5, 600), torch.logspace(-6, 0, 300), -torch.logspace(-6, 0, 300)]).view(300, 4) * cap
+    case.q[..., 0] = x.to(case.dt).cuda()
+    out, lse = case.run(ctx, scale=1.0, softcap=cap, causal=False)
+    x = case.q[..., 0].double()
+    z = cap * torch.tanh(x / cap)
+    tol = 2.0 ** -20 * cap + 2.0 ** -22 * (x.abs() / torch.cosh(x / cap) ** 2 + z.abs())
+    assert ((lse.double() - z).abs() <= tol).all(), float(((lse.double() - z).abs() / tol).max())
+    want = torch.cat([case.values[b] for b in range(B)]).repeat_interleave(n, 0).expand(-1, 4, -1)
+    assert torch.equal(out, want)
