@@ -1,5 +1,6 @@
 """Values out of range in device memory: what is left out, what is reported, and what is nobody's business."""
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -72,3 +73,35 @@ def test_pages_that_no_row_sees_are_nobodys_business(ctx, q, page):
             case.table[0, first // page] = -1
             case.run(ctx, window=window)
             reported(ctx)
+
+
+@pytest.mark.parametrize("lens", [[(1, 200), (1, 100)], [(3, 200), (1, 100)], [(150, 200), (30, 40)]], ids=["token", "tokens", "chunk"])
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 16), ("fp16", 64, 32)])
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+def test_a_request_with_a_bad_page_gets_its_other_positions(ctx, lens, dtype, D, page, bad):
+    case = Case(lens, dtype, D, 8, 2, page, seed=4)
+    case.table[0, 2] = bad
+    out, lse = case.run(ctx)
+    reported(ctx)
+    assert worst(case, out, lse, 0, hidden=range(2 * page, 3 * page)) <= 1
+    assert worst(case, out, lse, 1) <= 1
+
+
+@pytest.mark.parametrize("T,Hkv,D", [(1, 1, 64), (33, 8, 128)])
+def test_a_slot_that_is_none_leaves_the_cache_as_it_is(ctx, T, Hkv, D):
+    n, page = 6, 16
+    k, v = (torch.randn((n, page, Hkv, D), device="cuda").bfloat16() for _ in range(2))
+    new = torch.randn((2, T, Hkv, D), device="cuda").bfloat16()
+    slot = np.random.default_rng(T).permutation(n * page)[:T].astype(np.int32)
+    cache = kvdro.kvdro_kv_open(ctx, k, v)
+    for bad in (n * page, 2 ** 31 - 1, -2):
+        slot[T // 2] = bad
+        want = k.clone(), v.clone()
+        for t in range(T):
+            if t != T // 2:
+                for w, x in zip(want, new):
+                    w[slot[t] // page, slot[t] % page] = x[t]
+        kvdro.kvdro_kv_append(cache, new[0], new[1], torch.from_numpy(slot).cuda())
+        reported(ctx)
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+    kvdro.kvdro_kv_close(cache)
