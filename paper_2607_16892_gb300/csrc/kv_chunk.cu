@@ -513,6 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 tc_fence_before();
             }
+            // Q that nobody waited for, once a wait ran out, must land before the CTA's memory is given away.
+            asm volatile("cp.async.wait_all;" ::: "memory");
         } else {
             Pieces w(line, sh.part);
             int stage = 0;

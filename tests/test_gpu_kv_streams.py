@@ -222,3 +222,32 @@ def test_calls_go_to_torchs_current_stream():
         assert torch.equal(out, want)
     finally:
         kvdro.kvdro_destroy(ctx)
+
+
+def test_a_call_that_gave_up_leaves_its_neighbours_alone(monkeypatch):
+    """Chunks whose waits run out, many times, beside another context's calls on the same SMs: what was still on its way
+    when a CTA gave up does not land in the next one's memory."""
+    lens = [(60, 300), (40, 3000), (300, 500), (200, 200), (20, 90)] * 6
+    case = Case(lens, "bf16", 128, 8, 2, 16, seed=1)
+    monkeypatch.setenv("KVDRO_TEST_SKIP_CHUNK", "0")
+    broken = kvdro.kvdro_create(0)
+    monkeypatch.delenv("KVDRO_TEST_SKIP_CHUNK")
+    ctx, sides = kvdro.kvdro_create(0), [torch.cuda.Stream() for _ in range(2)]
+    try:
+        want = torch.empty_like(case.q)
+        caches = [kvdro.kvdro_kv_open(c, case.k, case.v) for c in (broken, ctx)]
+        kvdro.kvdro_kv_attend(caches[1], case.q, case.q_off, case.kv_len, case.table, want, max_q=300)
+        case.check(want, None, only={0, 3, 29})
+        junk, outs = torch.empty_like(want), [torch.zeros_like(want) for _ in range(30)]
+        torch.cuda.synchronize()
+        for out in outs:
+            kvdro.kvdro_kv_attend(caches[0], case.q, case.q_off, case.kv_len, case.table, junk, max_q=300, stream=sides[0])
+            kvdro.kvdro_kv_attend(caches[1], case.q, case.q_off, case.kv_len, case.table, out, max_q=300, stream=sides[1])
+        with pytest.raises(kvdro.KvdroError) as e:
+            kvdro.kvdro_sync(broken)
+        assert e.value.status == kvdro.KVDRO_ETIMEOUT
+        kvdro.kvdro_sync(ctx)
+        assert all(torch.equal(out, want) for out in outs)
+    finally:
+        kvdro.kvdro_destroy(broken)
+        kvdro.kvdro_destroy(ctx)
