@@ -254,7 +254,7 @@ __device__ __forceinline__ void cap_pair(uint32_t& x0, uint32_t& x1, float mul, 
 template <bool H, int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1)
     k_kv_chunk(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
-    extern __shared__ char s_raw[];
+    extern __shared__ __align__(16) char s_raw[];  // 64-bit words of the search first
     __shared__ Shared sh;
     using Sh = Shape<D>;
     constexpr int kTile = Sh::kTile, kStages = Sh::kStages;

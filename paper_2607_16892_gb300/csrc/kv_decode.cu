@@ -82,7 +82,7 @@ __device__ __forceinline__ uint32_t chunk_at(int key, int c) {
 template <bool H, int D, int NR>
 __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
-    extern __shared__ char s_raw[];
+    extern __shared__ __align__(16) char s_raw[];  // 64-bit words of the search first
     constexpr int kStages = Ring<D, NR>::kStages, kStage = Ring<D, NR>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
     using DecodeLine = Line<kRows, kKeys, kSlice, kOver>;
