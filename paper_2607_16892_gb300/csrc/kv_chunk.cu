@@ -18,7 +18,8 @@
 // Bound by the tensor cores where contexts are long.  A block of both halves takes about 3000 cycles: 16 S products of 70 cycles
 // and 16 PV products of 81 by themselves (64 at peak), 90 to 100 each beside the copies into shared memory and the weights' traffic
 // in tensor memory.  Measured (bf16, 32 heads of 128 over 8 key heads): 4096 tokens at the end of 32768, 2.06 TFLOP in
-// 1390 us = 1.48 PFLOP/s, 0.79 of the measured 1.89 (1551 us in a loop that heats the GPU); 512 tokens over 4099 45 us,
+// 1370 us over ten calls = 1.50 PFLOP/s, 1500 over 400 calls, which heat the GPU = 1.37 (0.80 and 0.73 of the measured 1.89 of
+// a burst; 0.81 of the sustained 1.69); 512 tokens over 4099 45 us,
 // of which 4 are the search of the line, 6 the join and 3 the launch.
 #include "kv_device.cuh"
 
