@@ -33,7 +33,6 @@ constexpr int kHalfRows = 128, kRows = 2 * kHalfRows, kKeys = 128;
 constexpr int kThreads = 384;
 constexpr int kNotes = 16;  // blocks that the copies are ahead of the weights, at most (a power of two)
 constexpr int kOver = 2;   // a tile's fixed cost, in blocks (1 / 2 / 3: mixed batch 148 / 132 / 132 us, capped prompts 95 / 96.5 / 99)
-constexpr float kRaise = 8.f;
 
 template <int D>
 struct Shape {
@@ -373,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * mul;
                     // Raise the maximum that the weights refer to, and rescale what is summed: rarely.
-                    const bool raise = top > m + kRaise || (m == -INFINITY && top > m);
+                    const bool raise = raises<H>(top, m);
                     if (__any_sync(~0u, raise)) {
                         const float to = raise ? top : m, keep = raise ? exp2_fast(m - to) : 1.f;
                         m = to;

@@ -28,7 +28,6 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16, kSlice = 32, k
 constexpr int kMostCtas = 4;  // per SM
 constexpr int kOver = 2;      // a tile's fixed cost, in blocks (0 / 1 / 2: window case 41.3 / 40.3 / 39.6 us)
 constexpr int kAtOnce = 8;    // pieces read at a time
-constexpr float kRaise = 8.f;
 
 template <int D, int NR>
 struct Ring {  // a stage: K or V of a slice
@@ -270,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR>::kCtas)
 #pragma unroll
             for (int n = 0; n < NR; n++)
 #pragma unroll
-                for (int i = 0; i < 2; i++) raise |= top[n][i] > m[n][i] + kRaise || (m[n][i] == -INFINITY && top[n][i] > m[n][i]);
+                for (int i = 0; i < 2; i++) raise |= raises<H>(top[n][i], m[n][i]);
             if (__any_sync(~0u, raise)) {
 #pragma unroll
                 for (int n = 0; n < NR; n++)

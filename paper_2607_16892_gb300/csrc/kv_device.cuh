@@ -29,9 +29,17 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
 }
 // Weights are 2^(s - m + kLift), and so are their sums.  FP16 has no weights below 2^-25, and 32768 of them may be a result's
 // whole component: 2^7 moves that to 2^-32 of the row's largest, while the largest stays at or below 2^15 (m is raised
-// when a row's maximum passes it by 2^8).  BF16 has FP32's exponents.
+// when a row's maximum passes it by more than kRaise).  BF16 has FP32's exponents.
 template <bool H>
 constexpr float kLift = H ? 7.f : 0.f;
+constexpr float kRaise = 8.f;
+// Whether a maximum asks for m to be raised to it.  With FP16 every greater one does where scores are spaced by 1/8 and more: rounded
+// differences of 8 may be 9, and 2^16 is an infinity.
+template <bool H>
+__device__ __forceinline__ bool raises(float top, float m) {
+    const float slack = H && fabsf(top) > 0x1p20f ? 0.f : kRaise;
+    return top > m + slack || (m == -INFINITY && top > m);
+}
 // The log sum of a row (natural), from the m that its sum refers to.
 template <bool H>
 __device__ __forceinline__ float log_sum(float m, float sum) {

@@ -20,6 +20,15 @@ def ctx():
     kvdro.kvdro_destroy(c)
 
 
+def repeat(case, B):
+    """The one request of ``case`` B times, over the same pages."""
+    q = case.lens[0][0]
+    case.lens, case.keys, case.values, case.T = case.lens * B, case.keys * B, case.values * B, B * q
+    case.table, case.kv_len, case.q = case.table.repeat(B, 1), case.kv_len.repeat(B), case.q.repeat(B, 1, 1)
+    case.off = np.arange(B + 1) * q
+    case.q_off = torch.from_numpy(case.off.astype(np.int32)).cuda()
+
+
 @pytest.mark.parametrize("q", [1, 40])
 @pytest.mark.parametrize("first", [0, 30000])
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
@@ -47,13 +56,11 @@ def test_many_small_weights_are_not_lost_where_one_cta_has_the_row(ctx, q, dtype
     k, v = torch.zeros_like(case.keys[0]), torch.zeros_like(case.values[0])
     k[0, :, 0] = 5.0
     v[:, :, 1], v[0, :, 1], v[0, :, 2] = 1.0, 0.0, 1.0
+    case.keys[0], case.values[0] = k, v
     case.set(0, k, v)
     case.q.zero_()
     case.q[..., 0] = 3.5
-    case.lens, case.keys, case.values, case.T = case.lens * B, [k] * B, [v] * B, B * q
-    case.table, case.kv_len, case.q = case.table.repeat(B, 1), case.kv_len.repeat(B), case.q.repeat(B, 1, 1)
-    case.off = np.arange(B + 1) * q
-    case.q_off = torch.from_numpy(case.off.astype(np.int32)).cuda()
+    repeat(case, B)
     out, lse = case.run(ctx, scale=1.0)
     for b in (0, 1, 299, 599):
         assert worst(case, out, lse, b, scale=1.0) <= 1
@@ -67,6 +74,29 @@ def test_split_rows_within_bounds_of_their_weights(ctx, lens, D, Hq, Hkv, page):
     out, lse = case.run(ctx)
     for b in range(len(lens)):
         assert worst(case, out, lse, b) <= 1
+    kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("q", [1, 40])
+@pytest.mark.parametrize("dtype,D", [("fp16", 64), ("fp16", 128), ("bf16", 128)])
+@pytest.mark.parametrize("lead", [1.0, 1.25, 1.5, 1.75, -1.0, -1.5])
+def test_scores_so_large_that_their_spacing_matters(ctx, q, dtype, D, lead):
+    """Scores of 2^16 to 2^27 that climb in small steps: FP32 rounds them to multiples of up to 8, so that a row's maximum can
+    pass the one its weights refer to by more than it seems.  Whatever the rounding, a result is a mean of values."""
+    B, kv = 600, 2000  # so many that a row is not split
+    case = Case([(q, kv)], dtype, D, 4, 1, 16, seed=1)
+    k, v = torch.zeros_like(case.keys[0]), case.values[0]
+    case.q.zero_()
+    repeat(case, B)
+    lo, hi = v.float().amin(0) - 0.01 * v.abs().max(), v.float().amax(0) + 0.01 * v.abs().max()
+    for e in range(16, 27):
+        for step in (0.02, 0.05, 0.011):
+            k[..., 0], k[..., 1] = lead * 2.0 ** (e // 2), (torch.arange(kv, device="cuda") * step).to(case.dt)[:, None]
+            case.set(0, k, v)
+            case.q[..., 0], case.q[..., 1] = 2.0 ** (e - e // 2), 1.0
+            out, lse = case.run(ctx, scale=1.0)
+            assert torch.isfinite(lse).all() and torch.isfinite(out).all(), (e, step)
+            assert ((out >= lo) & (out <= hi)).all(), (e, step)
     kvdro.kvdro_sync(ctx)
 
 
