@@ -37,6 +37,7 @@
 #ifndef KVDRO_H
 #define KVDRO_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -213,6 +214,8 @@ int kvdro_eval_grid_noalloc(int32_t K, const int64_t* offsets, const int32_t* le
  *     kvdro_kv_plan     pages for the requests' lengths and reservations, slots for their new tokens
  *     kvdro_kv_append   the new tokens' keys and values into those slots     (once per layer)
  *     kvdro_kv_attend   the new tokens' attention over their requests' pages (once per layer)
+ * Where requests share a prefix, kvdro_kv_attend_shared stands in the place of the last; kvdro_kv_read gets keys and values back out of
+ * pages.  A cache is of 16 bits (kvdro_kv_open) or of 8 (kvdro_kv_open8); every call takes handles of both.
  * The paper's data plane runs a paged cache of this kind unchanged beneath its decisions (Fig. 1, Sec. 2).
  * All arrays are memory of the context's device (or managed) and every call is asynchronous on `stream` and allocates nothing, so
  * that calls can be captured into a CUDA graph (after one call of the same kind outside a capture,
@@ -238,6 +241,21 @@ typedef enum { KVDRO_BF16 = 0, KVDRO_FP16 = 1 } kvdro_kv_dtype;
  */
 int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
                   int32_t head_dim, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride);
+
+/*
+ * Describe a page cache of 8 bits.  k and v hold e4m3 codes (one byte per element, strides as in kvdro_kv_open but
+ * multiples of 16), k_exp and v_exp a scale byte for every token and key head, at (page * n_kv_heads + head) * page_size + slot:
+ * an element stands for its code times 2^(byte - 127).  Bytes are 1 to 254; 0 stands for zeros.
+ * kvdro_kv_append quantises as it writes: byte - 127 is the least E >= -126 with max |x_d| <= 448 * 2^E over the head's finite
+ * elements, the codes are x_d / 2^E rounded to nearest, ties to even, so that every element is within 2^-4 of itself or 2^(E-10).
+ * Non-finite elements become NaN.  With FP16 rows E = 8 stops at 240 * 2^8 = 61440, for 256 * 2^8 is no FP16 number.
+ *   dtype       the type of the rows that calls on the handle take and give (append, read, q, out): KVDRO_BF16 or
+ *               KVDRO_FP16.  Values beyond FP16's range (written as BF16) are infinities to a handle of KVDRO_FP16.
+ *   k, v, k_exp, v_exp  device memory, 16-byte aligned.  The rest as in kvdro_kv_open.
+ */
+int kvdro_kv_open8(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
+                   int32_t head_dim, void* k, const int64_t* k_stride, uint8_t* k_exp, void* v, const int64_t* v_stride,
+                   uint8_t* v_exp);
 
 /* Free the handle (the arrays stay the caller's).  NULL is accepted. */
 int kvdro_kv_close(kvdro_kv* kv);
@@ -283,6 +301,17 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
                     const int64_t* v_stride, const int32_t* slot, void* stream);
 
 /*
+ * Read keys and values back out of pages: those of the last n = q_off[b+1] - q_off[b] tokens of request b's kv_len[b], so that with
+ * the arrays of a step it gives what kvdro_kv_append wrote in it, and with n = kv_len[b] whole requests.
+ *   q_off, kv_len, table, B, T, max_pages   as in kvdro_kv_attend.
+ *   k, v       results, element (t, head, d) at t * stride[0] + head * stride[1] + d (NULL: contiguous [T][n_kv_heads]
+ *              [head_dim]), of the handle's dtype, rounded to it once (8 bits); 16-byte aligned, strides multiples of 8.  Tokens of no
+ *              request, in front of position 0 and on pages that are none get zeros.
+ */
+int kvdro_kv_read(kvdro_kv* kv, int32_t B, int32_t T, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                  int32_t max_pages, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride, void* stream);
+
+/*
  * Attention of the new tokens over their requests' cached ones, their own included (append first).  Token i
  * of request b's n = q_off[b+1] - q_off[b] stands at position p = kv_len[b] - n + i; its query head h reads key/value
  * head h / (n_heads / n_kv_heads):
@@ -307,6 +336,28 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
                     const int64_t* q_stride, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
                     int32_t max_pages, double scale, int causal, int32_t window, double softcap, void* out,
                     const int64_t* out_stride, float* lse, void* stream);
+
+/*
+ * Attention of requests that share prefixes: requests share_off[g] .. share_off[g+1] - 1 stand behind the same prefix_len[g]
+ * tokens, which live once in the pages prefix_table[g]; kv_len and table are about a request's own tokens alone (as kvdro_kv_plan gives
+ * them).  A token sees what kvdro_kv_attend lets it see of its own tokens, and the whole prefix: the softmax runs over both.
+ * Each prefix is read once for all of its requests' tokens, whose rows it makes one long request of.  Tokens of requests with
+ * kv_len 0 get out = 0 and lse = -infinity, prefix or not.  There is no sliding window.
+ *   G            prefixes, 1 <= G <= B;  share_off: int32[G+1], ascending within [0, B]: requests in front of the first and
+ *                behind the last have no prefix.
+ *   prefix_len   int32[G], 0: none;  prefix_table: int32[G][prefix_pages], prefix_pages * page_size <= 2^30.
+ *   work         device memory of the bytes that kvdro_kv_shared_bytes gives for these sizes, 16-byte aligned: scratch of this call until
+ *                its work is done on the device, to be used by any other call after it.
+ * The other arguments are those of kvdro_kv_attend, max_q the most new tokens of one request.
+ */
+int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,
+                           const int64_t* q_stride, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                           int32_t max_pages, int32_t G, const int32_t* share_off, const int32_t* prefix_len,
+                           const int32_t* prefix_table, int32_t prefix_pages, double scale, int causal, double softcap, void* out,
+                           const int64_t* out_stride, float* lse, void* work, size_t work_bytes, void* stream);
+
+/* Bytes of `work` for T tokens.  KVDRO_EINVAL outside the limits of kvdro_kv_attend. */
+int kvdro_kv_shared_bytes(int32_t T, int32_t n_heads, int32_t head_dim, size_t* bytes);
 
 /* Wait for the context's device work -- the streams of its last call outside the page cache and of its last page cache
  * call, and its last kvdro_kv_attend -- and report any asynchronous CUDA error, kernel timeout or value out

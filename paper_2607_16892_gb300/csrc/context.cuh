@@ -77,6 +77,7 @@ struct kvdro_kv {
     bool half = false;  // FP16, else BF16
     int32_t n_pages = 0, page_size = 0, page_shift = 0, heads = 0, head_dim = 0;
     void *k = nullptr, *v = nullptr;
+    uint8_t *k_exp = nullptr, *v_exp = nullptr;  // 8 bits: scale bytes [page][head][slot]; null: 16 bits
     int64_t k_stride[3] = {}, v_stride[3] = {};  // page, slot, head; in elements
     kvdro::KvMaps maps;
 };

@@ -37,7 +37,35 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 
-// Tensor maps of a cache (d, slot, head, page) for boxes of 64 elements of d by a page's slots, and by 32 at most.
+// Quantises as it copies: strides of the rows in 16-byte units, of the cache in 8-byte ones.
+struct Append8Args {
+    const uint4 *k, *v;
+    uint2 *kc, *vc;
+    uint8_t *k_exp, *v_exp;
+    int64_t k_tok, k_head, v_tok, v_head;
+    int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+    const int32_t* slot;
+    int32_t T, n_slots, page_shift, heads, vec_shift;  // vectors of 8 elements of a head: 1 << vec_shift
+    bool half;
+    int32_t* err;
+};
+cudaError_t launch_kv_append8(const Append8Args& a, cudaStream_t s);
+
+struct ReadArgs {
+    const char *kc, *vc;
+    const uint8_t *k_exp, *v_exp;  // null: 16 bits
+    uint4 *k, *v;                  // results
+    int64_t k_tok, k_head, v_tok, v_head;                            // in 16-byte units
+    int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;  // in bytes
+    const int32_t *q_off, *kv_len, *table;
+    int32_t B, T, n_pages, page_shift, max_pages, heads, vec_shift;
+    bool half;
+    int32_t* err;
+};
+cudaError_t launch_kv_read(const ReadArgs& a, cudaStream_t s);
+
+// Tensor maps of a cache (d, slot, head, page) for boxes of a page's slots by 64 elements of d, and of 32 slots at most.  8 bits: all
+// of d in a box.
 struct KvMaps {
     CUtensorMap k, v, k_slice, v_slice;
 };
@@ -48,8 +76,11 @@ struct Join {
     int32_t last;  // the last CTA with a piece; -1: no tile
 };
 
+enum class Part : int32_t { kWhole, kLeave, kJoin };
+
 struct AttendArgs {
-    const uint16_t *q, *v;
+    const uint16_t* q;
+    const void* v;
     uint16_t* out;
     float* lse;
     int64_t q_tok, q_head, out_tok, out_head, v_page, v_slot, v_head;  // in elements
@@ -63,6 +94,14 @@ struct AttendArgs {
     float* pieces;       // sums of tiles that several CTAs share
     unsigned* tickets;   // by CTA: arrivals at the tile that its stretch ends in, zero between calls
     Join* joins;         // by CTA
+    const uint8_t *k_exp, *v_exp;  // 8 bits: a byte E + 127 per page, head and slot, in this order; null: 16 bits
+    // Prefixes: a launch over them takes request g's tokens from those of requests share_off[g] .. share_off[g + 1] - 1 of
+    // the caller's `share_n`, and leaves its sums; one over the requests' own pages joins those with its own.
+    const int32_t* share_off;
+    int32_t share_n;
+    Part part;
+    float* sums;         // [T][heads][head_dim]
+    float2* sum_ml;      // [T][heads]: maximum (in log2) and sum of weights
     unsigned long long wait_ns;  // bound of a wait
     int32_t skip;        // test hook: each CTA leaves this copy out, so that the wait for it runs out; -1: none
     int32_t* err;
@@ -71,6 +110,8 @@ size_t kv_decode_piece_bytes(int sms);
 int kv_decode_ctas(int sms);
 cudaError_t kv_decode_prepare();
 // `eight`: at most eight rows share a key head (else sixteen; more are right, but slow).
+cudaError_t kv_decode8_prepare();
+cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s);
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 cudaError_t kv_chunk_prepare();

@@ -77,20 +77,20 @@ bool overlap(const Extent& x, const Extent& y) {
     return a < b + 4 * (uintptr_t)y.n && b < a + 4 * (uintptr_t)x.n && x.n > 0 && y.n > 0;
 }
 
-// Strides of rows of 16-byte vectors: `n` of them into `out`, from the caller's or the contiguous ones.
-int rows(kvdro_ctx* ctx, const char* name, const void* p, const int64_t* stride, int n, const int64_t* dense, int64_t* out) {
+// Strides of rows of 16-byte vectors of `vec` elements: `n` of them into `out`, from the caller's or the contiguous ones.
+int rows(kvdro_ctx* ctx, const char* name, const void* p, const int64_t* stride, int n, const int64_t* dense, int64_t* out, int vec = 8) {
     if (reinterpret_cast<uintptr_t>(p) % 16) return fail(ctx, KVDRO_EINVAL, "%s is not 16-byte aligned", name);
     for (int i = 0; i < n; i++) {
         out[i] = stride ? stride[i] : dense[i];
-        if (out[i] < 1 || out[i] >= kMaxStride || out[i] % 8)
-            return fail(ctx, KVDRO_EINVAL, "%s: stride %lld is not a positive multiple of 8 elements below 2^39", name,
-                        (long long)out[i]);
+        if (out[i] < 1 || out[i] >= kMaxStride || out[i] % vec)
+            return fail(ctx, KVDRO_EINVAL, "%s: stride %lld is not a positive multiple of %d elements below 2^39", name,
+                        (long long)out[i], vec);
     }
     return KVDRO_OK;
 }
 
 // A tensor map of k or v for boxes of 64 elements by `slots` slots of one head and page, rows of 128 bytes permuted
-// (128-byte swizzle) so that matrix loads meet no bank conflict.
+// (128-byte swizzle) so that matrix loads meet no bank conflict.  8 bits: boxes of whole rows of 64 or 128 bytes.
 int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const int64_t* stride, int slots) {
     static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
         void* f = nullptr;
@@ -102,11 +102,14 @@ int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const i
     }();
     if (!fn) return fail(ctx, KVDRO_ECUDA, "the driver has no cuTensorMapEncodeTiled");
     const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages};
-    const cuuint64_t bytes[3] = {(cuuint64_t)stride[1] * 2, (cuuint64_t)stride[2] * 2, (cuuint64_t)stride[0] * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
-    const CUresult r = fn(map, c.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, p, dims, bytes, box, one,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const bool codes = c.k_exp != nullptr;
+    const cuuint64_t size = codes ? 1 : 2;
+    const cuuint64_t bytes[3] = {(cuuint64_t)stride[1] * size, (cuuint64_t)stride[2] * size, (cuuint64_t)stride[0] * size};
+    const cuuint32_t box[4] = {codes ? (cuuint32_t)c.head_dim : 64, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = fn(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : c.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                          4, p, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          codes && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(ctx, KVDRO_EINVAL, "these sizes and strides make no tensor map (driver error %d)", (int)r);
     return KVDRO_OK;
 }
@@ -124,6 +127,7 @@ int clear(kvdro_ctx* ctx, void* p, size_t bytes) {
 int prepare_attend(kvdro_ctx* ctx) {
     if (ctx->kv_ready) return KVDRO_OK;
     KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
+    KV_CUDA(kvdro::kv_decode8_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_chunk_prepare(), "preparing the attention kernels");
     if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
     const size_t pieces = kvdro::kv_decode_piece_bytes(ctx->sms) + kvdro::kv_chunk_piece_bytes(ctx->sms);
@@ -145,13 +149,9 @@ int error_word(kvdro_ctx* ctx) {
     return KVDRO_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
-                  int32_t head_dim, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride) {
-    NvtxRange nvtx_("kvdro_kv_open");
+// What a handle of either kind is made of.
+int open_cache(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim, void* k,
+               const int64_t* k_stride, uint8_t* k_exp, void* v, const int64_t* v_stride, uint8_t* v_exp, bool codes) {
     if (out) *out = nullptr;
     if (!ctx) return KVDRO_EINVAL;
     ctx->err.clear();
@@ -164,10 +164,15 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
     if (int rc = check_device(ctx, {{"k", k}, {"v", v}})) return rc;
+    if (codes) {
+        if (int rc = check_device(ctx, {{"k_exp", k_exp}, {"v_exp", v_exp}})) return rc;
+        if (reinterpret_cast<uintptr_t>(k_exp) % 16) return fail(ctx, KVDRO_EINVAL, "k_exp is not 16-byte aligned");
+        if (reinterpret_cast<uintptr_t>(v_exp) % 16) return fail(ctx, KVDRO_EINVAL, "v_exp is not 16-byte aligned");
+    }
     const int64_t row = (int64_t)n_kv_heads * head_dim, dense[3] = {page_size * row, row, head_dim};
     kvdro_kv c;
-    if (int rc = rows(ctx, "k", k, k_stride, 3, dense, c.k_stride)) return rc;
-    if (int rc = rows(ctx, "v", v, v_stride, 3, dense, c.v_stride)) return rc;
+    if (int rc = rows(ctx, "k", k, k_stride, 3, dense, c.k_stride, codes ? 16 : 8)) return rc;
+    if (int rc = rows(ctx, "v", v, v_stride, 3, dense, c.v_stride, codes ? 16 : 8)) return rc;
     if (int rc = error_word(ctx)) return rc;
     if (int rc = prepare_attend(ctx)) return rc;
     c.ctx = ctx;
@@ -179,6 +184,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     c.head_dim = head_dim;
     c.k = k;
     c.v = v;
+    c.k_exp = k_exp;
+    c.v_exp = v_exp;
     if (int rc = encode(ctx, &c.maps.k_slice, c, k, c.k_stride, std::min(page_size, 32))) return rc;
     if (int rc = encode(ctx, &c.maps.v_slice, c, v, c.v_stride, std::min(page_size, 32))) return rc;
     if (int rc = encode(ctx, &c.maps.k, c, k, c.k_stride, page_size)) return rc;
@@ -190,6 +197,149 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
     ctx->caches = kv;
     *out = kv;
     return KVDRO_OK;
+}
+
+// What both kinds of attention calls refuse.
+int check_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, int32_t max_pages, double scale, int causal, double softcap) {
+    kvdro_ctx* ctx = kv->ctx;
+    if (int rc = check_requests(ctx, B, T, max_pages, kv->page_size)) return rc;
+    if (n_heads < 1 || n_heads > kMaxHeads || n_heads % kv->heads)
+        return fail(ctx, KVDRO_EINVAL, "n_heads = %d is not a multiple of n_kv_heads = %d up to %d", n_heads, kv->heads, kMaxHeads);
+    if (max_q < 0) return fail(ctx, KVDRO_EINVAL, "max_q = %d is negative", max_q);
+    if (!std::isfinite((float)scale)) return fail(ctx, KVDRO_EINVAL, "scale = %g is not finite", scale);
+    if (!(softcap == 0.0 || (softcap >= 0x1p-20 && softcap <= 1000.0)))
+        return fail(ctx, KVDRO_EINVAL, "softcap = %g is neither 0 nor in [2^-20, 1000]", softcap);
+    if (causal != 0 && causal != 1) return fail(ctx, KVDRO_EINVAL, "causal must be 0 or 1");
+    return KVDRO_OK;
+}
+
+// The kernels' arguments for a call's rows; with a device of the context current.
+int attend_args(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, const void* q, const int64_t* q_stride, const int32_t* q_off,
+                const int32_t* kv_len, const int32_t* table, int32_t max_pages, double scale, int causal, int32_t window, double softcap,
+                void* out, const int64_t* out_stride, float* lse, kvdro::AttendArgs& a) {
+    kvdro_ctx* ctx = kv->ctx;
+    if ((int64_t)T * n_heads > kMaxRows) return fail(ctx, KVDRO_EINVAL, "T * n_heads = %lld passes 2^30", (long long)T * n_heads);
+    if (int rc = check_device(ctx, {{"q", q}, {"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"out", out}})) return rc;
+    if (lse)
+        if (int rc = check_device(ctx, {{"lse", lse}})) return rc;
+    const int64_t dense[2] = {(int64_t)n_heads * kv->head_dim, kv->head_dim};
+    int64_t qs[2] = {}, os[2] = {};
+    if (int rc = rows(ctx, "q", q, q_stride, 2, dense, qs)) return rc;
+    if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
+    a.q = static_cast<const uint16_t*>(q);
+    a.v = kv->v;
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    a.q_tok = qs[0];
+    a.q_head = qs[1];
+    a.out_tok = os[0];
+    a.out_head = os[1];
+    a.v_page = kv->v_stride[0];
+    a.v_slot = kv->v_stride[1];
+    a.v_head = kv->v_stride[2];
+    a.q_off = q_off;
+    a.kv_len = kv_len;
+    a.table = table;
+    a.B = B;
+    a.T = T;
+    a.heads = n_heads;
+    a.kv_heads = kv->heads;
+    a.group = n_heads / kv->heads;
+    // p = 31 + ceil(log2 group), mul = ceil(2^p / group) < 2^32: row * mul >> p is exact for rows below 2^31, since
+    // mul * group exceeds 2^p by less than group <= 2^(p - 31).
+    a.group_shift = 31 + log2_of(a.group);
+    a.group_mul = (uint32_t)((((uint64_t)1 << a.group_shift) + a.group - 1) / a.group);
+    a.min_q = 0;
+    a.max_q = 0x7fffffff;
+    a.head_dim = kv->head_dim;
+    a.n_pages = kv->n_pages;
+    a.page_shift = kv->page_shift;
+    a.max_pages = max_pages;
+    a.window = window;
+    a.half = kv->half;
+    a.causal = causal != 0;
+    a.scale = (float)scale;
+    a.cap = (float)softcap;
+    a.pieces = static_cast<float*>(ctx->kv_pieces.p);
+    a.tickets = static_cast<unsigned*>(ctx->kv_tickets.p);
+    a.joins = static_cast<kvdro::Join*>(ctx->kv_joins.p);
+    a.k_exp = kv->k_exp;
+    a.v_exp = kv->v_exp;
+    a.share_off = nullptr;
+    a.share_n = 0;
+    a.part = kvdro::Part::kWhole;
+    a.sums = nullptr;
+    a.sum_ml = nullptr;
+    a.wait_ns = ctx->skip_chunk >= 0 ? kTestWaitNs : kWaitNs;
+    a.skip = ctx->skip_chunk;
+    a.err = static_cast<int32_t*>(ctx->kv_err.p);
+    return KVDRO_OK;
+}
+
+// The launches of one pass over pages: `most` new tokens of a request at most, as far as is known; `uniform`: every request has
+// as many.
+int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, cudaStream_t s) {
+    const auto decode = a.k_exp ? kvdro::launch_kv_decode8 : kvdro::launch_kv_decode;
+    // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
+    // both runs on both, each request on its own.
+    const bool eight = a.group <= 8 && most * a.group <= 8;
+    if (most * a.group <= kFewRows || a.k_exp) {
+        KV_CUDA(decode(a, maps, eight, ctx->sms, s), "attention kernel");
+        return KVDRO_OK;
+    }
+    const int32_t few = (a.group <= 8 ? 8 : kFewRows) / a.group;
+    const bool both = few > 0 && !uniform;
+    if (both) {
+        a.max_q = few;
+        KV_CUDA(decode(a, maps, a.group <= 8, ctx->sms, s), "attention kernel");
+        a.min_q = few;
+        a.max_q = 0x7fffffff;
+        a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
+    }
+    KV_CUDA(kvdro::launch_kv_chunk(a, maps, both, ctx->sms, s), "attention kernel");
+    return KVDRO_OK;
+}
+
+// Calls share the scratch: one on another stream than the last waits for that one.  (By the streams' numbers: a new stream
+// may have an old one's handle.  Waiting in every case cost a small call 2 us.)
+struct ScratchTurn {
+    bool captured = false;
+    unsigned long long number = 0;
+    int begin(kvdro_ctx* ctx, cudaStream_t s) {
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
+        captured = capture != cudaStreamCaptureStatusNone;
+        if (!captured) KV_CUDA(cudaStreamGetId(s, &number), "asking for the stream's number");
+        if (!captured && ctx->kv_used && ctx->kv_stream != number) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
+        return KVDRO_OK;
+    }
+    int end(kvdro_ctx* ctx, cudaStream_t s) const {
+        if (captured) return KVDRO_OK;
+        KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
+        ctx->kv_stream = number;
+        ctx->kv_used = true;
+        return KVDRO_OK;
+    }
+};
+
+// New tokens of a request at most, as far as is known.
+int64_t most_tokens(int32_t max_q, int32_t B, int32_t T) { return max_q > 0 ? max_q : T > B ? T : 1; }
+
+}  // namespace
+
+extern "C" {
+
+int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
+                  int32_t head_dim, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride) {
+    NvtxRange nvtx_("kvdro_kv_open");
+    return open_cache(ctx, out, dtype, n_pages, page_size, n_kv_heads, head_dim, k, k_stride, nullptr, v, v_stride, nullptr, false);
+}
+
+int kvdro_kv_open8(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
+                   int32_t head_dim, void* k, const int64_t* k_stride, uint8_t* k_exp, void* v, const int64_t* v_stride,
+                   uint8_t* v_exp) {
+    NvtxRange nvtx_("kvdro_kv_open8");
+    return open_cache(ctx, out, dtype, n_pages, page_size, n_kv_heads, head_dim, k, k_stride, k_exp, v, v_stride, v_exp, true);
 }
 
 int kvdro_kv_close(kvdro_kv* kv) {
@@ -260,6 +410,37 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
     int64_t ks[2] = {}, vs[2] = {};
     if (int rc = rows(ctx, "k", k, k_stride, 2, dense, ks)) return rc;
     if (int rc = rows(ctx, "v", v, v_stride, 2, dense, vs)) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (kv->k_exp) {
+        kvdro::Append8Args a;
+        a.k = static_cast<const uint4*>(k);
+        a.v = static_cast<const uint4*>(v);
+        a.kc = static_cast<uint2*>(kv->k);
+        a.vc = static_cast<uint2*>(kv->v);
+        a.k_exp = kv->k_exp;
+        a.v_exp = kv->v_exp;
+        a.k_tok = ks[0] / 8;
+        a.k_head = ks[1] / 8;
+        a.v_tok = vs[0] / 8;
+        a.v_head = vs[1] / 8;
+        a.kc_page = kv->k_stride[0] / 8;
+        a.kc_slot = kv->k_stride[1] / 8;
+        a.kc_head = kv->k_stride[2] / 8;
+        a.vc_page = kv->v_stride[0] / 8;
+        a.vc_slot = kv->v_stride[1] / 8;
+        a.vc_head = kv->v_stride[2] / 8;
+        a.slot = slot;
+        a.T = T;
+        a.n_slots = kv->n_pages << kv->page_shift;
+        a.page_shift = kv->page_shift;
+        a.heads = kv->heads;
+        a.vec_shift = log2_of(kv->head_dim / 8);
+        a.half = kv->half;
+        a.err = static_cast<int32_t*>(ctx->kv_err.p);
+        ctx->kv_last = s;
+        KV_CUDA(kvdro::launch_kv_append8(a, s), "append kernel");
+        return KVDRO_OK;
+    }
     kvdro::AppendArgs a;
     a.k = static_cast<const uint4*>(k);
     a.v = static_cast<const uint4*>(v);
@@ -282,9 +463,59 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
     a.heads = kv->heads;
     a.vec_shift = log2_of(kv->head_dim / 8);
     a.err = static_cast<int32_t*>(ctx->kv_err.p);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->kv_last = s;
     KV_CUDA(kvdro::launch_kv_append(a, s), "append kernel");
+    return KVDRO_OK;
+}
+
+int kvdro_kv_read(kvdro_kv* kv, int32_t B, int32_t T, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                  int32_t max_pages, void* k, const int64_t* k_stride, void* v, const int64_t* v_stride, void* stream) {
+    NvtxRange nvtx_("kvdro_kv_read");
+    if (!kv) return KVDRO_EINVAL;
+    kvdro_ctx* ctx = kv->ctx;
+    ctx->err.clear();
+    if (int rc = check_requests(ctx, B, T, max_pages, kv->page_size)) return rc;
+    if (T == 0) return KVDRO_OK;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    if (int rc = check_device(ctx, {{"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"k", k}, {"v", v}})) return rc;
+    const int64_t dense[2] = {(int64_t)kv->heads * kv->head_dim, kv->head_dim};
+    int64_t ks[2] = {}, vs[2] = {};
+    if (int rc = rows(ctx, "k", k, k_stride, 2, dense, ks)) return rc;
+    if (int rc = rows(ctx, "v", v, v_stride, 2, dense, vs)) return rc;
+    const int64_t size = kv->k_exp ? 1 : 2;
+    kvdro::ReadArgs a;
+    a.kc = static_cast<const char*>(kv->k);
+    a.vc = static_cast<const char*>(kv->v);
+    a.k_exp = kv->k_exp;
+    a.v_exp = kv->v_exp;
+    a.k = static_cast<uint4*>(k);
+    a.v = static_cast<uint4*>(v);
+    a.k_tok = ks[0] / 8;
+    a.k_head = ks[1] / 8;
+    a.v_tok = vs[0] / 8;
+    a.v_head = vs[1] / 8;
+    a.kc_page = kv->k_stride[0] * size;
+    a.kc_slot = kv->k_stride[1] * size;
+    a.kc_head = kv->k_stride[2] * size;
+    a.vc_page = kv->v_stride[0] * size;
+    a.vc_slot = kv->v_stride[1] * size;
+    a.vc_head = kv->v_stride[2] * size;
+    a.q_off = q_off;
+    a.kv_len = kv_len;
+    a.table = table;
+    a.B = B;
+    a.T = T;
+    a.n_pages = kv->n_pages;
+    a.page_shift = kv->page_shift;
+    a.max_pages = max_pages;
+    a.heads = kv->heads;
+    a.vec_shift = log2_of(kv->head_dim / 8);
+    a.half = kv->half;
+    a.err = static_cast<int32_t*>(ctx->kv_err.p);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ctx->kv_last = s;
+    KV_CUDA(kvdro::launch_kv_read(a, s), "read kernel");
     return KVDRO_OK;
 }
 
@@ -296,101 +527,74 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     if (!kv) return KVDRO_EINVAL;
     kvdro_ctx* ctx = kv->ctx;
     ctx->err.clear();
-    if (int rc = check_requests(ctx, B, T, max_pages, kv->page_size)) return rc;
-    if (n_heads < 1 || n_heads > kMaxHeads || n_heads % kv->heads)
-        return fail(ctx, KVDRO_EINVAL, "n_heads = %d is not a multiple of n_kv_heads = %d up to %d", n_heads, kv->heads, kMaxHeads);
-    if (max_q < 0) return fail(ctx, KVDRO_EINVAL, "max_q = %d is negative", max_q);
-    if (!std::isfinite((float)scale)) return fail(ctx, KVDRO_EINVAL, "scale = %g is not finite", scale);
-    if (!(softcap == 0.0 || (softcap >= 0x1p-20 && softcap <= 1000.0)))
-        return fail(ctx, KVDRO_EINVAL, "softcap = %g is neither 0 nor in [2^-20, 1000]", softcap);
-    if (causal != 0 && causal != 1) return fail(ctx, KVDRO_EINVAL, "causal must be 0 or 1");
+    if (int rc = check_attend(kv, B, T, n_heads, max_q, max_pages, scale, causal, softcap)) return rc;
     if (window < 0 || (window > 0 && !causal)) return fail(ctx, KVDRO_EINVAL, "window = %d: not negative, and with causal only", window);
     if (T == 0) return KVDRO_OK;
-    if ((int64_t)T * n_heads > kMaxRows) return fail(ctx, KVDRO_EINVAL, "T * n_heads = %lld passes 2^30", (long long)T * n_heads);
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
-    if (int rc = check_device(ctx, {{"q", q}, {"q_off", q_off}, {"kv_len", kv_len}, {"table", table}, {"out", out}})) return rc;
-    if (lse)
-        if (int rc = check_device(ctx, {{"lse", lse}})) return rc;
-    const int64_t dense[2] = {(int64_t)n_heads * kv->head_dim, kv->head_dim};
-    int64_t qs[2] = {}, os[2] = {};
-    if (int rc = rows(ctx, "q", q, q_stride, 2, dense, qs)) return rc;
-    if (int rc = rows(ctx, "out", out, out_stride, 2, dense, os)) return rc;
     kvdro::AttendArgs a;
-    a.q = static_cast<const uint16_t*>(q);
-    a.v = static_cast<const uint16_t*>(kv->v);
-    a.out = static_cast<uint16_t*>(out);
-    a.lse = lse;
-    a.q_tok = qs[0];
-    a.q_head = qs[1];
-    a.out_tok = os[0];
-    a.out_head = os[1];
-    a.v_page = kv->v_stride[0];
-    a.v_slot = kv->v_stride[1];
-    a.v_head = kv->v_stride[2];
-    a.q_off = q_off;
-    a.kv_len = kv_len;
-    a.table = table;
-    a.B = B;
-    a.T = T;
-    a.heads = n_heads;
-    a.kv_heads = kv->heads;
-    a.group = n_heads / kv->heads;
-    // p = 31 + ceil(log2 group), mul = ceil(2^p / group) < 2^32: row * mul >> p is exact for rows below 2^31, since
-    // mul * group exceeds 2^p by less than group <= 2^(p - 31).
-    a.group_shift = 31 + log2_of(a.group);
-    a.group_mul = (uint32_t)((((uint64_t)1 << a.group_shift) + a.group - 1) / a.group);
-    a.min_q = 0;
-    a.max_q = 0x7fffffff;
-    a.head_dim = kv->head_dim;
-    a.n_pages = kv->n_pages;
-    a.page_shift = kv->page_shift;
-    a.max_pages = max_pages;
-    a.window = window;
-    a.half = kv->half;
-    a.causal = causal != 0;
-    a.scale = (float)scale;
-    a.cap = (float)softcap;
-    a.pieces = static_cast<float*>(ctx->kv_pieces.p);
-    a.tickets = static_cast<unsigned*>(ctx->kv_tickets.p);
-    a.joins = static_cast<kvdro::Join*>(ctx->kv_joins.p);
-    a.wait_ns = ctx->skip_chunk >= 0 ? kTestWaitNs : kWaitNs;
-    a.skip = ctx->skip_chunk;
-    a.err = static_cast<int32_t*>(ctx->kv_err.p);
+    if (int rc = attend_args(kv, B, T, n_heads, q, q_stride, q_off, kv_len, table, max_pages, scale, causal, window, softcap, out, out_stride, lse, a))
+        return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     ctx->kv_last = s;
-    // Calls share the scratch: one on another stream than the last waits for that one.  (By the streams' numbers: a new stream
-    // may have an old one's handle.  Waiting in every case cost a small call 2 us.)
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    KV_CUDA(cudaStreamIsCapturing(s, &capture), "asking for the stream's state");
-    const bool captured = capture != cudaStreamCaptureStatusNone;
-    unsigned long long number = 0;
-    if (!captured) KV_CUDA(cudaStreamGetId(s, &number), "asking for the stream's number");
-    if (!captured && ctx->kv_used && ctx->kv_stream != number) KV_CUDA(cudaStreamWaitEvent(s, ctx->kv_done, 0), "ordering streams");
-    // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
-    // both runs on both, each request on its own.
-    const int64_t most = max_q > 0 ? max_q : T > B ? T : 1;  // new tokens of a request, as far as is known
-    const bool eight = a.group <= 8 && most * a.group <= 8;
-    if (most * a.group <= kFewRows) {
-        KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, eight, ctx->sms, s), "attention kernel");
-    } else {
-        const int32_t few = (a.group <= 8 ? 8 : kFewRows) / a.group;
-        const bool both = few > 0 && (max_q == 0 || (int64_t)max_q * B != T);
-        if (both) {
-            a.max_q = few;
-            KV_CUDA(kvdro::launch_kv_decode(a, kv->maps, a.group <= 8, ctx->sms, s), "attention kernel");
-            a.min_q = few;
-            a.max_q = 0x7fffffff;
-            a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
-        }
-        KV_CUDA(kvdro::launch_kv_chunk(a, kv->maps, both, ctx->sms, s), "attention kernel");
-    }
-    if (!captured) {
-        KV_CUDA(cudaEventRecord(ctx->kv_done, s), "recording an event");
-        ctx->kv_stream = number;
-        ctx->kv_used = true;
-    }
+    ScratchTurn turn;
+    if (int rc = turn.begin(ctx, s)) return rc;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, s)) return rc;
+    return turn.end(ctx, s);
+}
+
+int kvdro_kv_shared_bytes(int32_t T, int32_t n_heads, int32_t head_dim, size_t* bytes) {
+    if (!bytes || T < 0 || T > kMaxTokens || n_heads < 1 || n_heads > kMaxHeads || (head_dim != 64 && head_dim != 128) ||
+        (int64_t)T * n_heads > kMaxRows)
+        return KVDRO_EINVAL;
+    *bytes = (size_t)T * n_heads * (head_dim + 2) * sizeof(float);
     return KVDRO_OK;
+}
+
+int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t max_q, const void* q,
+                           const int64_t* q_stride, const int32_t* q_off, const int32_t* kv_len, const int32_t* table,
+                           int32_t max_pages, int32_t G, const int32_t* share_off, const int32_t* prefix_len,
+                           const int32_t* prefix_table, int32_t prefix_pages, double scale, int causal, double softcap, void* out,
+                           const int64_t* out_stride, float* lse, void* work, size_t work_bytes, void* stream) {
+    NvtxRange nvtx_("kvdro_kv_attend_shared");
+    if (!kv) return KVDRO_EINVAL;
+    kvdro_ctx* ctx = kv->ctx;
+    ctx->err.clear();
+    if (int rc = check_attend(kv, B, T, n_heads, max_q, max_pages, scale, causal, softcap)) return rc;
+    if (G < 1 || G > B) return fail(ctx, KVDRO_EINVAL, "G = %d outside [1, B]", G);
+    if (prefix_pages < 1 || (int64_t)prefix_pages * kv->page_size > kMaxPositions)
+        return fail(ctx, KVDRO_EINVAL, "prefix_pages = %d: prefix_pages * page_size outside [page_size, 2^30]", prefix_pages);
+    if (T == 0) return KVDRO_OK;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail(ctx, KVDRO_ECUDA, "cannot select device %d", ctx->device);
+    kvdro::AttendArgs a;
+    if (int rc = attend_args(kv, B, T, n_heads, q, q_stride, q_off, kv_len, table, max_pages, scale, causal, 0, softcap, out, out_stride, lse, a))
+        return rc;
+    if (int rc = check_device(ctx, {{"share_off", share_off}, {"prefix_len", prefix_len}, {"prefix_table", prefix_table}, {"work", work}})) return rc;
+    size_t need = 0;
+    kvdro_kv_shared_bytes(T, n_heads, kv->head_dim, &need);
+    if (work_bytes < need) return fail(ctx, KVDRO_EINVAL, "work has %zu bytes; the call needs %zu", work_bytes, need);
+    if (reinterpret_cast<uintptr_t>(work) % 16) return fail(ctx, KVDRO_EINVAL, "work is not 16-byte aligned");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ctx->kv_last = s;
+    ScratchTurn turn;
+    if (int rc = turn.begin(ctx, s)) return rc;
+    a.sums = static_cast<float*>(work);
+    a.sum_ml = reinterpret_cast<float2*>(a.sums + (int64_t)T * n_heads * kv->head_dim);
+    // The prefixes, each a request of all its requests' tokens, every one of which sees all of it.
+    kvdro::AttendArgs p = a;
+    p.part = kvdro::Part::kLeave;
+    p.share_off = share_off;
+    p.share_n = B;
+    p.B = G;
+    p.kv_len = prefix_len;
+    p.table = prefix_table;
+    p.max_pages = prefix_pages;
+    p.causal = false;
+    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, s)) return rc;
+    a.part = kvdro::Part::kJoin;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, s)) return rc;
+    return turn.end(ctx, s);
 }
 
 }  // extern "C"

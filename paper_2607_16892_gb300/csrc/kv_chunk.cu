@@ -447,6 +447,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int cta = blockIdx.x, g = row - tok * a.group, h = cur.at.h * a.group + g;
                 const int64_t t = cur.at.r.q0 + tok;
                 const bool whole = cur.whole(sh.part), begins = cur.begins(sh.part);
+                const bool join = a.part == Part::kJoin && whole && valid;
+                float2 by = make_float2(1.f, 0.f);
+                if (join) by = join_max<H>(a, t * a.heads + h, m, l);
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 float* const piece = a.pieces + (int64_t)(2 * cta + begins) * Sh::kPieceFloats;
                 const int prow = half * kHalfRows + row_in;
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int j = max(see.x, cur.at.t.lo + odd.x * kKeys); j < j1; j++) {
                             const int page = a.table[(int64_t)cur.at.b * a.max_pages + (j >> a.page_shift)];
                             if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-                            const uint16_t* v = a.v + page * a.v_page + (j & ((1 << a.page_shift) - 1)) * a.v_slot + cur.at.h * a.v_head + c;
+                            const uint16_t* v = static_cast<const uint16_t*>(a.v) + page * a.v_page + (j & ((1 << a.page_shift) - 1)) * a.v_slot + cur.at.h * a.v_head + c;
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) {
                                 const uint32_t x = *reinterpret_cast<const uint32_t*>(v + i);
@@ -484,7 +487,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                     }
-                    if (valid && whole) {
+                    if (valid && whole && a.part == Part::kLeave) {
+                        float* const to = a.sums + (t * a.heads + h) * D + c;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    } else if (valid && whole) {
+                        if (join) join_sums<D, 32>(a, t * a.heads + h, c, by, reinterpret_cast<float*>(o));
                         uint32_t x[16];
 #pragma unroll
                         for (int i = 0; i < 16; i++) x[i] = pack2<H>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
@@ -497,7 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (valid) {
                     if (whole) {
-                        if (a.lse) a.lse[t * a.heads + h] = log_sum<H>(m, l);
+                        if (a.part == Part::kLeave) leave_max<H>(a, t * a.heads + h, m, l);
+                        else if (a.lse) a.lse[t * a.heads + h] = log_sum<H>(m, l);
                     } else {
                         reinterpret_cast<float2*>(piece + kRows * D)[prow] = make_float2(m, l);
                     }
@@ -773,10 +782,21 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
                 o[i] = make_float4(fmaf(x[k][i].x, f, o[i].x), fmaf(x[k][i].y, f, o[i].y), fmaf(x[k][i].z, f, o[i].z), fmaf(x[k][i].w, f, o[i].w));
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
     const ChunkLine line(a);
     const int row = j.row0 + row_in, tok = line.token(row), h = j.h * a.group + row - tok * a.group;
     const int64_t t = j.q0 + tok;
+    if (a.part == Part::kLeave) {
+        float4* const to = reinterpret_cast<float4*>(a.sums + (t * a.heads + h) * D + part * (4 * N));
+#pragma unroll
+        for (int i = 0; i < N; i++) to[i] = o[i];
+        if (part == 0) leave_max<H>(a, t * a.heads + h, m, l);
+        return;
+    }
+    if (a.part == Part::kJoin) {
+        const float2 by = join_max<H>(a, t * a.heads + h, m, l);
+        join_sums<D, 4 * N>(a, t * a.heads + h, part * (4 * N), by, reinterpret_cast<float*>(o));
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + part * (4 * N));
 #pragma unroll
     for (int i = 0; i < N; i++) out[i] = make_uint2(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv));

@@ -1,0 +1,12 @@
+// The kernel for few rows on caches of 8 bits.
+#include "kv_decode.cuh"
+
+namespace kvdro {
+
+cudaError_t kv_decode8_prepare() { return prepare_all<true>(); }
+
+cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
+    return launch_any<true>(a, maps, eight, sms, s);
+}
+
+}  // namespace kvdro

@@ -53,6 +53,17 @@ __device__ __forceinline__ bool any_nonfinite(uint32_t w) {
     return ((w & exponent) + one) & 0x80008000u;
 }
 
+// 8 bits: a scale byte as the power of two that it stands for (0: none, the rows are zeros), and its exponent.
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+// Whether one of four codes is NaN: e4m3 has no infinities.
+__device__ __forceinline__ bool any_nan8(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Two codes as FP16, exactly.
+__device__ __forceinline__ uint32_t half2_of(uint16_t codes) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
+    return r;
+}
+
 // 2^x.  Relative error 2^-22; 0 at -infinity.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -80,6 +91,12 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 }
 __device__ __forceinline__ void fence_mbar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// One row of the caller's bytes, 16 at least, both ends 16-byte aligned.
+__device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -147,8 +164,18 @@ struct Line {
     __device__ __forceinline__ int token(int row) const { return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift); }
     __device__ __forceinline__ Request request(int b) {
         Request r;
-        r.q0 = a.q_off[b];
-        const int q1 = a.q_off[b + 1];
+        int b0 = b, b1 = b + 1;
+        if (a.share_off) {
+            b0 = a.share_off[b];
+            b1 = a.share_off[b + 1];
+            if (b0 < 0 || b1 < b0 || b1 > a.share_n) {
+                bad = true;
+                r.q0 = r.n = r.rows = r.kv = 0;
+                return r;
+            }
+        }
+        r.q0 = a.q_off[b0];
+        const int q1 = a.q_off[b1];
         r.kv = a.kv_len[b];
         if (r.q0 < 0 || q1 < r.q0) {
             bad = true;
@@ -372,10 +399,61 @@ struct Walk {
     }
 };
 
+// A row's sums of a launch over prefixes, as launches over the requests' own pages find them: H, the type of the weights, says
+// how far these are lifted, and what is left refers to weights that are not.
+template <bool H>
+__device__ __forceinline__ void leave_max(const AttendArgs& a, int64_t row, float m, float l) {
+    a.sum_ml[row] = make_float2(m - kLift<H>, l);
+}
+// Joins that row's maximum and sum with its own; what multiplies its own sums, and what those left (0: none were).
+template <bool H>
+__device__ __forceinline__ float2 join_max(const AttendArgs& a, int64_t row, float& m, float& l) {
+    float2 ml = __ldcg(a.sum_ml + row);
+    ml.x += kLift<H>;
+    const float to = fmaxf(m, ml.x), shift = to == -INFINITY ? 0.f : to, f = exp2_fast(m - shift), g = ml.y == 0.f ? 0.f : exp2_fast(ml.x - shift);
+    m = to;
+    l = l * f + ml.y * g;
+    return make_float2(f, g);
+}
+// Its sums of N columns from c on.
+template <int D, int N>
+__device__ __forceinline__ void join_sums(const AttendArgs& a, int64_t row, int c, float2 by, float* x) {
+    const float* const from = a.sums + row * D + c;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        float2 y = make_float2(0.f, 0.f);
+        if (by.y != 0.f) y = __ldcg(reinterpret_cast<const float2*>(from + i));  // else nothing may have been written there
+        x[i] = x[i] * by.x + y.x * by.y;
+        x[i + 1] = x[i + 1] * by.x + y.y * by.y;
+    }
+}
+
+// Tokens of no prefix: no sums.  The search is for bounds that ascend; where they do not, that is reported, and what it finds is a
+// prefix whose tokens have sums.
+template <int kThreads, class L>
+__device__ __forceinline__ void clear_parts(L& line) {
+    const AttendArgs& a = line.a;
+    for (int t = blockIdx.x * kThreads + threadIdx.x; t < a.T; t += gridDim.x * kThreads) {
+        int lo = 0, hi = a.B;  // the first prefix whose tokens end behind t
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const Request r = line.request(mid);
+            if (r.q0 + r.n > t) hi = mid;
+            else lo = mid + 1;
+        }
+        if (lo < a.B) {
+            const Request r = line.request(lo);
+            if (r.q0 <= t && t < r.q0 + r.n && r.kv > 0) continue;
+        }
+        for (int h = 0; h < a.heads; h++) a.sum_ml[(int64_t)t * a.heads + h] = make_float2(-INFINITY, 0.f);
+    }
+}
+
 // Tokens of no request, and of requests without positions: out = 0.
 template <int D, int kThreads, class L>
 __device__ __forceinline__ void clear_rest(L& line) {
     const AttendArgs& a = line.a;
+    if (a.part == Part::kLeave) return clear_parts<kThreads>(line);
     auto clear = [&](int t0, int t1, int from, int step) {
         const int64_t vecs = (int64_t)(t1 - t0) * a.heads * (D / 8);
         for (int64_t i = (int64_t)from * kThreads + threadIdx.x; i < vecs; i += (int64_t)step * kThreads) {

@@ -1,5 +1,7 @@
 // Pages for requests (kvdro_kv_plan) and the write into them (kvdro_kv_append).
-#include "kv.cuh"
+#include "kv_device.cuh"
+
+#include <type_traits>
 
 namespace kvdro {
 
@@ -302,6 +304,178 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(AppendArgs a, int 
     }
 }
 
+// Eight elements of a row as codes, the row's other vectors in the neighbouring lanes of `mask`: the scale is the least power of two
+// 2^E, E >= -126, with max |x| <= 448 2^E over the row's finite elements, and each element is rounded once, to the nearest code.
+// A power of two costs no precision (codes are floating-point numbers of three bits whatever their scale) and multiplies
+// exactly.  Non-finite elements become NaN.  FP16 cannot hold 256 * 2^8, which its largest numbers would round to: 240 * 2^8.
+// `e`: E + 127.
+template <bool H>
+__device__ __forceinline__ uint2 quantise(const uint4& x, unsigned mask, int lanes, uint32_t& e) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float f[8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float2 y = kv::unpack2<H>(w[i]);
+        f[2 * i] = y.x;
+        f[2 * i + 1] = y.y;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float y = fabsf(f[i]);
+        top = fmaxf(top, y < INFINITY ? y : 0.f);
+    }
+    for (int o = 1; o < lanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(mask, top, o));
+    const uint32_t u = __float_as_uint(top);
+    e = (uint32_t)max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 1);  // 448 = 1.75 * 2^8
+    const float down = __uint_as_float((254 - e) << 23), most = H && e == 135 ? 240.f : 448.f;
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        float y[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const float z = f[2 * i + k];
+            y[k] = fabsf(z) < INFINITY ? fminf(fmaxf(z * down, -most), most) : __uint_as_float(0x7fffffffu);
+        }
+        uint16_t r;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y[1]), "f"(y[0]));
+        c[i] = r;
+    }
+    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+}
+
+// As the copy above, and bound by the same; lanes that share a head's row find its largest element by shuffles.
+constexpr int kAppend8Deep = 2;
+
+template <bool H>
+__global__ void __launch_bounds__(kAppendThreads) k_kv_append8(Append8Args a, int lanes_shift) {
+    const int64_t id = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x, t = id >> lanes_shift;
+    const int lanes = 1 << lanes_shift;
+    if (t >= a.T) return;
+    const int32_t slot = a.slot[t];
+    if (slot < 0 || slot >= a.n_slots) {
+        if (slot != -1) atomicOr(a.err, kKvErrRange);
+        return;
+    }
+    const int64_t page = slot >> a.page_shift, in = slot & ((1 << a.page_shift) - 1);
+    const uint4 *k = a.k + t * a.k_tok, *v = a.v + t * a.v_tok;
+    uint2 *kc = a.kc + page * a.kc_page + in * a.kc_slot, *vc = a.vc + page * a.vc_page + in * a.vc_slot;
+    const int vecs = a.heads << a.vec_shift, row = 1 << a.vec_shift;
+    const unsigned mask = ((1u << row) - 1u) << (threadIdx.x & 31 & ~(row - 1));  // 8 or 16 lanes, all of one token
+    for (int i0 = (int)id & (lanes - 1); i0 < vecs; i0 += kAppend8Deep * lanes) {
+        uint4 x[kAppend8Deep], y[kAppend8Deep];
+#pragma unroll
+        for (int u = 0; u < kAppend8Deep; u++) {
+            const int i = i0 + u * lanes;
+            if (i < vecs) {
+                x[u] = k[(i >> a.vec_shift) * a.k_head + (i & (row - 1))];
+                y[u] = v[(i >> a.vec_shift) * a.v_head + (i & (row - 1))];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAppend8Deep; u++) {
+            const int i = i0 + u * lanes, h = i >> a.vec_shift, c = i & (row - 1);
+            if (i < vecs) {
+                uint32_t ke, ve;
+                kc[h * a.kc_head + c] = quantise<H>(x[u], mask, row, ke);
+                vc[h * a.vc_head + c] = quantise<H>(y[u], mask, row, ve);
+                if (c == 0) {
+                    const int64_t at = ((page * a.heads + h) << a.page_shift) + in;
+                    a.k_exp[at] = (uint8_t)ke;
+                    a.v_exp[at] = (uint8_t)ve;
+                }
+            }
+        }
+    }
+}
+
+// Rows out of pages: a copy with two lookups, the request of a token and its page.  A token's row is dealt to lanes as above, eight
+// elements each at a time.
+constexpr int kReadDeep = 2;
+
+template <bool H, bool Q>
+__global__ void __launch_bounds__(kAppendThreads) k_kv_read(ReadArgs a, int lanes_shift) {
+    const int64_t id = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x, t64 = id >> lanes_shift;
+    const int lanes = 1 << lanes_shift;
+    if (t64 >= a.T) return;
+    const int t = (int)t64;
+    int lo = 0, hi = a.B;  // the first request that ends behind t
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.q_off[mid + 1] > t) hi = mid;
+        else lo = mid + 1;
+    }
+    int32_t page = -1, in = 0;
+    bool bad = false;
+    if (lo < a.B) {
+        const int32_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], n = a.kv_len[lo];
+        if (q0 < 0 || n < 0 || (int64_t)n > ((int64_t)a.max_pages << a.page_shift)) {
+            bad = true;
+        } else if (t >= q0 && n - (q1 - t) >= 0) {
+            const int32_t p = n - (q1 - t);
+            page = a.table[(int64_t)lo * a.max_pages + (p >> a.page_shift)];
+            in = p & ((1 << a.page_shift) - 1);
+            if ((uint32_t)page >= (uint32_t)a.n_pages) {
+                bad = true;
+                page = -1;
+            }
+        }
+    }
+    if (bad) atomicOr(a.err, kKvErrRange);
+    uint4 *k = a.k + (int64_t)t * a.k_tok, *v = a.v + (int64_t)t * a.v_tok;
+    const int64_t from = max(page, 0);
+    const char *kc = a.kc + from * a.kc_page + in * a.kc_slot, *vc = a.vc + from * a.vc_page + in * a.vc_slot;
+    const int vecs = a.heads << a.vec_shift, mask = (1 << a.vec_shift) - 1;
+    using Vec = typename std::conditional<Q, uint2, uint4>::type;  // eight elements as they are stored
+    for (int i0 = (int)id & (lanes - 1); i0 < vecs; i0 += kReadDeep * lanes) {
+        Vec x[kReadDeep] = {}, y[kReadDeep] = {};
+        uint32_t ke[kReadDeep] = {}, ve[kReadDeep] = {};
+#pragma unroll
+        for (int u = 0; u < kReadDeep; u++) {
+            const int i = i0 + u * lanes, h = i >> a.vec_shift, c = i & mask;
+            if (i < vecs && page >= 0) {
+                x[u] = *reinterpret_cast<const Vec*>(kc + h * a.kc_head + c * (int)sizeof(Vec));
+                y[u] = *reinterpret_cast<const Vec*>(vc + h * a.vc_head + c * (int)sizeof(Vec));
+                if constexpr (Q) {
+                    const int64_t at = ((from * a.heads + h) << a.page_shift) + in;
+                    ke[u] = a.k_exp[at];
+                    ve[u] = a.v_exp[at];
+                }
+            }
+        }
+        auto value = [](const Vec& w, uint32_t e) {
+            if constexpr (Q) {
+                const float s = kv::scale_of(e);
+                uint32_t r[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 f = kv::unpack2<true>(kv::half2_of((uint16_t)((i < 2 ? w.x : w.y) >> (i & 1 ? 16 : 0))));
+                    r[i] = kv::pack2<H>(f.x * s, f.y * s);
+                }
+                return make_uint4(r[0], r[1], r[2], r[3]);
+            } else {
+                return w;
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < kReadDeep; u++) {
+            const int i = i0 + u * lanes, h = i >> a.vec_shift, c = i & mask;
+            if (i < vecs) {
+                k[h * a.k_head + c] = value(x[u], ke[u]);
+                v[h * a.v_head + c] = value(y[u], ve[u]);
+            }
+        }
+    }
+}
+
+// Lanes that a token's row is dealt to, as a power of two, and the CTAs of a launch.
+int lanes_of(int vecs) {
+    int shift = 0;
+    while (shift < 5 && (1 << shift) < vecs) shift++;
+    return shift;
+}
+unsigned ctas_of(int64_t T, int lanes_shift) { return (unsigned)(((T << lanes_shift) + kAppendThreads - 1) / kAppendThreads); }
+
 __global__ void k_kv_take(int32_t* err) { err[1] = atomicExch(err, 0); }
 
 }  // namespace
@@ -324,11 +498,24 @@ cudaError_t launch_kv_plan(const PlanArgs& a, int sms, cudaStream_t s) {
 }
 
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s) {
-    const int vecs = a.heads << a.vec_shift;
-    int shift = 0;
-    while (shift < 5 && (1 << shift) < vecs) shift++;
-    const int64_t threads = (int64_t)a.T << shift;
-    k_kv_append<<<(unsigned)((threads + kAppendThreads - 1) / kAppendThreads), kAppendThreads, 0, s>>>(a, shift);
+    const int shift = lanes_of(a.heads << a.vec_shift);
+    k_kv_append<<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_kv_append8(const Append8Args& a, cudaStream_t s) {
+    const int shift = lanes_of(a.heads << a.vec_shift);
+    if (a.half) k_kv_append8<true><<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
+    else k_kv_append8<false><<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_kv_read(const ReadArgs& a, cudaStream_t s) {
+    const int shift = lanes_of(a.heads << a.vec_shift);
+    const unsigned ctas = ctas_of(a.T, shift);
+    if (!a.k_exp) k_kv_read<true, false><<<ctas, kAppendThreads, 0, s>>>(a, shift);
+    else if (a.half) k_kv_read<true, true><<<ctas, kAppendThreads, 0, s>>>(a, shift);
+    else k_kv_read<false, true><<<ctas, kAppendThreads, 0, s>>>(a, shift);
     return cudaGetLastError();
 }
 

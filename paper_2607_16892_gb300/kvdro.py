@@ -45,7 +45,8 @@ _STATUS = {0: "KVDRO_OK", -1: "KVDRO_EINVAL", -2: "KVDRO_ENOMEM", -3: "KVDRO_ECU
 # Every entry point declared in include/kvdro.h.
 SYMBOLS = ("kvdro_create", "kvdro_load_samples", "kvdro_quantiles", "kvdro_eval_grid", "kvdro_sorted_samples",
            "kvdro_eval_dual", "kvdro_last_grid_ms", "kvdro_eval_grid_noalloc", "kvdro_kv_open", "kvdro_kv_close",
-           "kvdro_kv_plan", "kvdro_kv_append", "kvdro_kv_attend", "kvdro_sync", "kvdro_last_error", "kvdro_destroy")
+           "kvdro_kv_plan", "kvdro_kv_append", "kvdro_kv_attend", "kvdro_kv_open8", "kvdro_kv_read", "kvdro_kv_attend_shared",
+           "kvdro_kv_shared_bytes", "kvdro_sync", "kvdro_last_error", "kvdro_destroy")
 
 _lock = threading.Lock()
 _lib = None
@@ -104,6 +105,15 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.kvdro_kv_append.argtypes = [P, i32, P, P, P, P, P, P]
         lib.kvdro_kv_attend.restype = ctypes.c_int
         lib.kvdro_kv_attend.argtypes = [P, i32, i32, i32, i32, P, P, P, P, P, i32, f64, ctypes.c_int, i32, f64, P, P, P, P]
+        lib.kvdro_kv_open8.restype = ctypes.c_int
+        lib.kvdro_kv_open8.argtypes = [P, ctypes.POINTER(P), ctypes.c_int, i32, i32, i32, i32, P, P, P, P, P, P]
+        lib.kvdro_kv_read.restype = ctypes.c_int
+        lib.kvdro_kv_read.argtypes = [P, i32, i32, P, P, P, i32, P, P, P, P, P]
+        lib.kvdro_kv_attend_shared.restype = ctypes.c_int
+        lib.kvdro_kv_attend_shared.argtypes = [P, i32, i32, i32, i32, P, P, P, P, P, i32, i32, P, P, P, i32, f64, ctypes.c_int, f64, P, P, P, P,
+                                               ctypes.c_size_t, P]
+        lib.kvdro_kv_shared_bytes.restype = ctypes.c_int
+        lib.kvdro_kv_shared_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
         lib.kvdro_sync.restype = ctypes.c_int
         lib.kvdro_sync.argtypes = [P]
         lib.kvdro_last_error.restype = ctypes.c_char_p
@@ -345,9 +355,9 @@ def kvdro_eval_grid_noalloc(K: int, offsets, lengths, L_max, L_in, R: int, r, NL
 # ------------------------------------------------------------------ page cache
 
 class KvdroKv:
-    """A handle of ``kvdro_kv_open`` and the tensors it describes, which it keeps alive."""
+    """A handle of ``kvdro_kv_open`` or ``kvdro_kv_open8`` and the tensors it describes, which it keeps alive."""
 
-    __slots__ = ("handle", "ctx", "owner", "k", "v", "dtype", "heads", "head_dim", "__weakref__")
+    __slots__ = ("handle", "ctx", "owner", "k", "v", "exps", "dtype", "heads", "head_dim", "__weakref__")
 
     def __del__(self):
         try:
@@ -444,16 +454,51 @@ def kvdro_kv_open(ctx, k, v) -> KvdroKv:
             raise ValueError(f"{name} must be [n_pages][page_size][n_kv_heads][head_dim] with a contiguous last dimension")
     if k.shape != v.shape or k.dtype is not v.dtype:
         raise ValueError("k and v differ in shape or dtype")
+    return _open(ctx, k, v, k.dtype, None)
+
+
+def kvdro_kv_open8(ctx, k, v, k_exp, v_exp, dtype) -> KvdroKv:
+    """Describe a page cache of 8 bits: ``k`` and ``v`` are CUDA tensors [n_pages][page_size][n_kv_heads][head_dim] of
+    float8_e4m3fn, ``k_exp`` and ``v_exp`` contiguous ones [n_pages][n_kv_heads][page_size] of uint8 or float8_e8m0fnu; rows that
+    calls on the handle take and give are of ``dtype``, bfloat16 or float16."""
+    import torch
+
+    _kv_setup()
+    for name, a in (("k", k), ("v", v), ("k_exp", k_exp), ("v_exp", v_exp)):
+        _on_device(name, a)
+    for name, a in (("k", k), ("v", v)):
+        if a.dtype is not torch.float8_e4m3fn:
+            raise TypeError(f"{name}: expected float8_e4m3fn, got {a.dtype}")
+        if a.dim() != 4 or (a.shape[3] > 1 and a.stride(3) != 1):
+            raise ValueError(f"{name} must be [n_pages][page_size][n_kv_heads][head_dim] with a contiguous last dimension")
+    if k.shape != v.shape:
+        raise ValueError("k and v differ in shape")
+    n, page, heads, _ = k.shape
+    for name, a in (("k_exp", k_exp), ("v_exp", v_exp)):
+        if a.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            raise TypeError(f"{name}: expected uint8 or float8_e8m0fnu, got {a.dtype}")
+        if a.shape != (n, heads, page) or not a.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor [n_pages][n_kv_heads][page_size]")
+    if dtype not in _kv_types:
+        raise TypeError(f"dtype must be bfloat16 or float16, got {dtype}")
+    return _open(ctx, k, v, dtype, (k_exp, v_exp))
+
+
+def _open(ctx, k, v, dtype, exps) -> KvdroKv:
     n, page, heads, d = k.shape
-    strides = [_I3(*(t.stride(i) if t.shape[i] > 1 else 8 for i in range(3))) for t in (k, v)]
-    h = ctypes.c_void_p()
+    strides = [_I3(*(t.stride(i) if t.shape[i] > 1 else 16 for i in range(3))) for t in (k, v)]
+    lib, h = load_library(), ctypes.c_void_p()
     with _kv_lock:
-        _check(ctx, load_library().kvdro_kv_open(ctx, ctypes.byref(h), _kv_types[k.dtype], n, page, heads, d, k.data_ptr(),
-                                                 strides[0], v.data_ptr(), strides[1]))
+        if exps is None:
+            _check(ctx, lib.kvdro_kv_open(ctx, ctypes.byref(h), _kv_types[dtype], n, page, heads, d, k.data_ptr(), strides[0], v.data_ptr(),
+                                          strides[1]))
+        else:
+            _check(ctx, lib.kvdro_kv_open8(ctx, ctypes.byref(h), _kv_types[dtype], n, page, heads, d, k.data_ptr(), strides[0],
+                                           exps[0].data_ptr(), v.data_ptr(), strides[1], exps[1].data_ptr()))
         c = KvdroKv()
         c.owner = _owners.setdefault(getattr(ctx, "value", ctx), _Owner())
         c.owner.handles.add(h.value)
-        c.handle, c.ctx, c.k, c.v, c.dtype, c.heads, c.head_dim = h, ctx, k, v, k.dtype, heads, d
+        c.handle, c.ctx, c.k, c.v, c.exps, c.dtype, c.heads, c.head_dim = h, ctx, k, v, exps, dtype, heads, d
         c.owner.caches.add(c)
     return c
 
@@ -462,7 +507,7 @@ def kvdro_kv_close(cache: KvdroKv) -> None:
     with _kv_lock:
         handle, cache.handle = cache.handle, None
         if handle:
-            cache.k = cache.v = None
+            cache.k = cache.v = cache.exps = None
             if handle.value in cache.owner.handles:  # else freed with its context
                 cache.owner.handles.remove(handle.value)
                 load_library().kvdro_kv_close(handle)
@@ -486,11 +531,11 @@ def kvdro_kv_plan(ctx, page_size: int, cached, new_len, held, table, ring, pool,
         _check(ctx, st)
 
 
-def _table(table):
+def _table(table, name="table", rows="B", pages="max_pages"):
     try:
         B, max_pages = table.shape
     except (AttributeError, ValueError):
-        raise ValueError("table must be [B][max_pages]") from None
+        raise ValueError(f"{name} must be [{rows}][{pages}]") from None
     return B, max_pages
 
 
@@ -526,6 +571,64 @@ def kvdro_kv_attend(cache: KvdroKv, q, q_off, kv_len, table, out, lse=None, scal
         _current_stream(q.get_device()) if stream is None else _stream(stream))
     if st:
         _check(cache.ctx, st)
+
+
+def kvdro_kv_read(cache: KvdroKv, q_off, kv_len, table, k, v, stream=None) -> None:
+    """Keys and values of the requests' last tokens (as many as ``q_off`` says) out of their pages into ``k`` and ``v``,
+    [T][n_kv_heads][head_dim] of the cache's dtype (last dimension contiguous)."""
+    lib = _lib_kv or _kv_setup()
+    kp, ks, T, heads = _heads(cache, "k", k, None, cache.heads)
+    vp, vs, T, heads = _heads(cache, "v", v, T, heads)
+    B, max_pages = _table(table)
+    st = lib.kvdro_kv_read(
+        _open_handle(cache), B, T, _dev("q_off", q_off, _i32, B + 1), _dev("kv_len", kv_len, _i32, B), _dev("table", table, _i32), max_pages,
+        kp, ks, vp, vs, _current_stream(k.get_device()) if stream is None else _stream(stream))
+    if st:
+        _check(cache.ctx, st)
+
+
+def kvdro_kv_shared_bytes(T: int, n_heads: int, head_dim: int) -> int:
+    """Bytes of workspace that ``kvdro_kv_attend_shared`` needs for T tokens."""
+    n = ctypes.c_size_t()
+    st = (_lib_kv or _kv_setup()).kvdro_kv_shared_bytes(T, n_heads, head_dim, ctypes.byref(n))
+    if st:
+        raise KvdroError(st, f"no workspace for T = {T}, n_heads = {n_heads}, head_dim = {head_dim}")
+    return n.value
+
+
+def kvdro_kv_attend_shared(cache: KvdroKv, q, q_off, kv_len, table, share_off, prefix_len, prefix_table, out, lse=None, scale=None,
+                           causal: bool = True, softcap: float = 0.0, max_q: int = 0, work=None, stream=None) -> None:
+    """``kvdro_kv_attend`` where requests share_off[g] .. share_off[g + 1] - 1 stand behind the prefix_len[g] tokens of the pages
+    ``prefix_table`` [G][prefix_pages]; ``work`` is a CUDA tensor of at least ``kvdro_kv_shared_bytes`` bytes (None: one of torch's allocator,
+    on the call's stream)."""
+    lib = _lib_kv or _kv_setup()
+    qp, qs, T, heads = _heads(cache, "q", q)
+    op, os_, _, _ = _heads(cache, "out", out, T, heads)
+    B, max_pages = _table(table)
+    G, prefix_pages = _table(prefix_table, "prefix_table", "G", "prefix_pages")
+    at = _current_stream(q.get_device()) if stream is None else _stream(stream)
+    if work is None:
+        work = _workspace(kvdro_kv_shared_bytes(T, heads, cache.head_dim), q.device, at)
+    elif not (getattr(work, "is_cuda", False) and work.is_contiguous()):
+        raise ValueError("work must be a contiguous CUDA tensor")
+    st = lib.kvdro_kv_attend_shared(
+        _open_handle(cache), B, T, heads, max_q, qp, qs, _dev("q_off", q_off, _i32, B + 1), _dev("kv_len", kv_len, _i32, B),
+        _dev("table", table, _i32), max_pages, G, _dev("share_off", share_off, _i32, G + 1), _dev("prefix_len", prefix_len, _i32, G),
+        _dev("prefix_table", prefix_table, _i32), prefix_pages, cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, softcap,
+        op, os_, None if lse is None else _dev("lse", lse, _f32, T * heads), work.data_ptr(), work.numel() * work.element_size(), at)
+    if st:
+        _check(cache.ctx, st)
+
+
+def _workspace(n: int, device, stream: int):
+    """Bytes of torch's allocator that are the stream's until it is done with them."""
+    import torch
+
+    with torch.cuda.device(device):
+        if stream == _current_stream(device.index):
+            return torch.empty(n, dtype=torch.uint8, device=device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+            return torch.empty(n, dtype=torch.uint8, device=device)
 
 
 def kvdro_sync(ctx) -> None:
