@@ -65,7 +65,7 @@ struct ReadArgs {
 cudaError_t launch_kv_read(const ReadArgs& a, cudaStream_t s);
 
 // Tensor maps of a cache (d, slot, head, page) for boxes of a page's slots by 64 elements of d, and of 32 slots at most.  8 bits: all
-// of d in a box.
+// of d in a box, the former not permuted.
 struct KvMaps {
     CUtensorMap k, v, k_slice, v_slice;
 };
@@ -115,6 +115,8 @@ cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, bool eigh
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 cudaError_t kv_chunk_prepare();
+cudaError_t kv_chunk8_prepare();
+cudaError_t launch_kv_chunk8(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s);
 // `after_few`: beside a launch of kv_decode for the requests of few rows, directly before it, on other scratch.
 cudaError_t launch_kv_chunk(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s);
 

@@ -90,8 +90,9 @@ int rows(kvdro_ctx* ctx, const char* name, const void* p, const int64_t* stride,
 }
 
 // A tensor map of k or v for boxes of 64 elements by `slots` slots of one head and page, rows of 128 bytes permuted
-// (128-byte swizzle) so that matrix loads meet no bank conflict.  8 bits: boxes of whole rows of 64 or 128 bytes.
-int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const int64_t* stride, int slots) {
+// (128-byte swizzle) so that matrix loads meet no bank conflict.  8 bits: boxes of whole rows of 64 or 128 bytes, `plain` ones not
+// permuted.
+int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const int64_t* stride, int slots, bool plain = false) {
     static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult found;
@@ -108,7 +109,7 @@ int encode(kvdro_ctx* ctx, CUtensorMap* map, const kvdro_kv& c, void* p, const i
     const cuuint32_t box[4] = {codes ? (cuuint32_t)c.head_dim : 64, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
     const CUresult r = fn(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : c.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                           4, p, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          codes && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                          plain ? CU_TENSOR_MAP_SWIZZLE_NONE : codes && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(ctx, KVDRO_EINVAL, "these sizes and strides make no tensor map (driver error %d)", (int)r);
     return KVDRO_OK;
@@ -129,6 +130,7 @@ int prepare_attend(kvdro_ctx* ctx) {
     KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_decode8_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_chunk_prepare(), "preparing the attention kernels");
+    KV_CUDA(kvdro::kv_chunk8_prepare(), "preparing the attention kernels");
     if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
     const size_t pieces = kvdro::kv_decode_piece_bytes(ctx->sms) + kvdro::kv_chunk_piece_bytes(ctx->sms);
     if (int rc = ensure(ctx, ctx->kv_pieces, pieces)) return rc;
@@ -188,8 +190,8 @@ int open_cache(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32
     c.v_exp = v_exp;
     if (int rc = encode(ctx, &c.maps.k_slice, c, k, c.k_stride, std::min(page_size, 32))) return rc;
     if (int rc = encode(ctx, &c.maps.v_slice, c, v, c.v_stride, std::min(page_size, 32))) return rc;
-    if (int rc = encode(ctx, &c.maps.k, c, k, c.k_stride, page_size)) return rc;
-    if (int rc = encode(ctx, &c.maps.v, c, v, c.v_stride, page_size)) return rc;
+    if (int rc = encode(ctx, &c.maps.k, c, k, c.k_stride, page_size, codes)) return rc;
+    if (int rc = encode(ctx, &c.maps.v, c, v, c.v_stride, page_size, codes)) return rc;
     kvdro_kv* kv = new (std::nothrow) kvdro_kv(c);
     if (!kv) return fail(ctx, KVDRO_ENOMEM, "no memory for the handle");
     kv->next = ctx->caches;
@@ -280,10 +282,11 @@ int attend_args(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, const void*
 // as many.
 int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, cudaStream_t s) {
     const auto decode = a.k_exp ? kvdro::launch_kv_decode8 : kvdro::launch_kv_decode;
+    const auto chunk = a.k_exp ? kvdro::launch_kv_chunk8 : kvdro::launch_kv_chunk;
     // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
     // both runs on both, each request on its own.
     const bool eight = a.group <= 8 && most * a.group <= 8;
-    if (most * a.group <= kFewRows || a.k_exp) {
+    if (most * a.group <= kFewRows) {
         KV_CUDA(decode(a, maps, eight, ctx->sms, s), "attention kernel");
         return KVDRO_OK;
     }
@@ -296,7 +299,7 @@ int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps
         a.max_q = 0x7fffffff;
         a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
     }
-    KV_CUDA(kvdro::launch_kv_chunk(a, maps, both, ctx->sms, s), "attention kernel");
+    KV_CUDA(chunk(a, maps, both, ctx->sms, s), "attention kernel");
     return KVDRO_OK;
 }
 
