@@ -65,7 +65,7 @@ struct ReadArgs {
 cudaError_t launch_kv_read(const ReadArgs& a, cudaStream_t s);
 
 // Tensor maps of a cache (d, slot, head, page) for boxes of a page's slots by 64 elements of d, and of 32 slots at most.  8 bits: all
-// of d in a box, the former not permuted.
+// of d in a box, the former not permuted, the latter of 64 slots where heads are of 64.
 struct KvMaps {
     CUtensorMap k, v, k_slice, v_slice;
 };
@@ -95,6 +95,7 @@ struct AttendArgs {
     unsigned* tickets;   // by CTA: arrivals at the tile that its stretch ends in, zero between calls
     Join* joins;         // by CTA
     const uint8_t *k_exp, *v_exp;  // 8 bits: a byte E + 127 per page, head and slot, in this order; null: 16 bits
+    int32_t head_shift;  // 8 bits, eight rows: a tile of the kernel for few rows is of 2^head_shift key heads
     // Prefixes: a launch over them takes request g's tokens from those of requests share_off[g] .. share_off[g + 1] - 1 of
     // the caller's `share_n`, and leaves its sums; one over the requests' own pages joins those with its own.
     const int32_t* share_off;

@@ -30,22 +30,25 @@ namespace {
 
 using namespace kv;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16, kSlice = 32, kKeys = kSlice * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16;
 constexpr int kMostCtas = 4;  // per SM
 constexpr int kOver = 2;      // a tile's fixed cost, in blocks (0 / 1 / 2: window case 41.3 / 40.3 / 39.6 us)
 constexpr int kAtOnce = 8;    // pieces read at a time
 
 template <int D, int NR, bool Q>
-struct Ring {  // a stage: K or V of a slice
+struct Ring {  // a stage: K or V of a slice; 8 bits: both
     // What fits the registers and the shared memory.  Eight rows, D 128: 3 CTAs of 2 stages 95 us (64 requests), 2 of 3 stages 99;
     // D 64: 4 of 3 stages 41 us (window case), 3 of 4 stages 44, 2 of 6 stages 52.
-    static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? 4 : 2);  // per SM
-    static constexpr int kBytes = kSlice * D * (Q ? 1 : 2), kStages = (D == 128 ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6)) * (Q ? 2 : 1);
-    static constexpr int kScales = Q ? kWarps * kStages * kSlice : 0;  // a byte per position, behind the ring
+    // 8 bits: keys and values of a slice together; of heads of 64, 64 positions (four requests of 131071: 215 us, 253 with 32).
+    static constexpr int kSlice = Q && D == 64 ? 64 : 32;
+    static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? (Q ? 3 : 4) : 2);  // per SM
+    static constexpr int kBytes = kSlice * D * 2;
+    static constexpr int kStages = D == 128 || Q ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6);
+    static constexpr int kScales = Q ? kWarps * kStages * 2 * kSlice : 0;  // a byte per key and value, behind the ring
     static constexpr int kSmem = kWarps * kStages * kBytes + kScales + 1024;
     static_assert(Stretch<kThreads>::kScratch <= kSmem, "the ring is scratch first");
 };
-// A piece in global memory: rows of D sums, then their maxima and sums of weights.
+// A piece in global memory: rows (8 bits: of two heads, if of eight) of D sums, then their maxima and sums of weights.
 template <int D>
 constexpr int kPieceFloats = kMostRows * (D + 2);
 
@@ -83,7 +86,8 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 template <int D, bool Q>
 __device__ __forceinline__ uint32_t chunk_at(int key, int c) {
     if constexpr (Q && D == 64) return (uint32_t)(key * 64 + ((c ^ (key >> 1 & 3)) << 4));
-    return (uint32_t)((c >> 3) * (kSlice * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4));
+    if constexpr (Q) return (uint32_t)(key * 128 + ((c ^ (key & 7)) << 4));
+    return (uint32_t)((c >> 3) * (32 * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4));
 }
 __device__ __forceinline__ uint32_t load_u8(uint32_t at) {
     uint32_t x;
@@ -96,12 +100,12 @@ template <bool H, int D, int NR, bool Q>
 __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ __align__(16) char s_raw[];  // 64-bit words of the search first
+    constexpr int kSlice = Ring<D, NR, Q>::kSlice, kKeys = kSlice * kWarps;
     constexpr int kStages = Ring<D, NR, Q>::kStages, kStage = Ring<D, NR, Q>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
-    using DecodeLine = Line<kRows, kKeys, kSlice, kOver>;
+    using DecodeLine = Line<kRows, kKeys, kSlice, kOver, Q && NR == 1>;
     constexpr bool F16 = H || Q;  // the type of the products
-    // Where column c of row r of the sums stands in shared memory, without bank conflicts: rows of D + 4 floats, or of D that
-    // a stage of 8 bits has room for, permuted by the row.
+    // Where column c of row r of the sums stands in shared memory, without bank conflicts.
     auto sum_at = [](int r, int c) { return Q ? r * D + (c ^ (r >> 1 & 3) << 3) : r * (D + 4) + c; };
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
     __shared__ Stretch<kThreads> s_part;
@@ -110,7 +114,10 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(s_raw), ring = ((raw + 1023) & ~1023u) + warp * kStages * kStage;
     char* const ring_ptr = s_raw + (ring - raw);
-    const uint32_t scales = ((raw + 1023) & ~1023u) + kWarps * kStages * kStage + warp * kStages * kSlice;
+    // A tile's heads, of which this warp has one, and its warps with the others of that head a block's slices.
+    const int hs = Q && NR == 1 ? a.head_shift : 0, of_head = kWarps >> hs, my_head = warp / of_head, my_slice = (warp & (of_head - 1)) * kSlice;
+    const uint32_t flip = (D == 128 ? lane & 7 : lane >> 1 & 3) << 4;  // 8 bits: how chunks of row lane & 15 of sixteen are permuted
+    const uint32_t scales = ((raw + 1023) & ~1023u) + kWarps * kStages * kStage + warp * kStages * 2 * kSlice;
     DecodeLine line(a);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // a launch for many rows may fill SMs that this one leaves
 
@@ -126,37 +133,90 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
         return;
     }
 
-    // Units in the order K, V of a slice, K, V of the next.
+    // Units in the order K, V of a slice, K, V of the next; 8 bits: a unit is both.
     Walk<DecodeLine> in(line, s_part), w = in;  // of the copies, and of the sums
     int in_blk = in.p0;
     bool in_v = false;
     int fetched = 0;
 
-    // Page numbers of this warp's slices of 32 blocks, one per lane; a slice has two pages if they have 16 slots.
+    // Page numbers of this warp's slices of 32 blocks, one per lane; a slice has several pages if they have fewer slots.
+    constexpr int NP = kSlice / 16;
     const int slots = min(kSlice, 1 << a.page_shift);
-    int pg[2] = {-1, -1}, pg_b = -1, pg_rt = -1, pg_blk = -1;
+    int pg[NP], pg_b = -1, pg_rt = -1, pg_blk = -1;
+#pragma unroll
+    for (int i = 0; i < NP; i++) pg[i] = -1;
     bool range = false;
     uint32_t filled = 0, phase = 0;  // by stage: holds a slice; the parity to wait for
-    uint32_t gaps = 0;               // by stage, two bits: 16 positions whose page number is none
+    uint32_t gaps = 0;               // by stage, a bit for each 16 positions whose page number is none
+    constexpr uint32_t kAllGaps = (1u << NP) - 1;
+    // The page numbers of the slices around the next one, unless they are there.
+    auto look_up = [&] {
+        if (in.at.b == pg_b && in.at.rt == pg_rt && (in_blk >> 5) == pg_blk) return;
+        pg_b = in.at.b;
+        pg_rt = in.at.rt;
+        pg_blk = in_blk >> 5;
+        const int j = in.at.t.lo + ((in_blk & ~31) + lane) * line.keys() + my_slice;
+        const int seen_lo = line.seen(in.at.r, line.token(in.at.rt * kRows)).x;
+#pragma unroll
+        for (int i = 0; i < NP; i++) {
+            pg[i] = -1;
+            if (j + 16 * i < in.at.t.hi && ((j + 16 * i) | (slots - 1)) >= seen_lo) {  // else no row's business
+                const int page = a.table[(int64_t)in.at.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
+                if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
+                else range = true;
+            }
+        }
+    };
+    // 8 bits: the next slice's keys, values and scales.
+    auto fetch8 = [&](int stage) {
+        filled &= ~(1u << stage);
+        if (!in.more) return;
+        look_up();
+        int p[NP];
+        uint32_t gap = 0;
+#pragma unroll
+        for (int i = 0; i < NP; i++) {
+            p[i] = __shfl_sync(~0u, pg[i], in_blk & 31);
+            gap |= (p[i] < 0 ? 1u : 0u) << i;
+        }
+        gaps = (gaps & ~(kAllGaps << NP * stage)) | gap << NP * stage;
+        if (gap != kAllGaps) {
+            const int slot = __shfl_sync(~0u, (in.at.t.lo + in_blk * line.keys() + my_slice) & ((1 << a.page_shift) - 1), 0);
+            const int head = __shfl_sync(~0u, (in.at.h << hs) + my_head, 0);
+            const uint32_t bar = __shfl_sync(~0u, smem_u32(&s_bar[warp][stage]), 0), to = __shfl_sync(~0u, ring + stage * kStage, 0);
+            const uint32_t scale_to = __shfl_sync(~0u, scales + stage * 2 * kSlice, 0);
+            if (fetched != a.skip && elect_one()) {  // (left out: a test's wait runs out)
+                mbar_expect(bar, kStage + 2 * kSlice);
+                auto copy = [&](int at, int page) {  // a page that is none reads as zeros, with any page's scales
+                    const int box_page = page >= 0 ? page : a.n_pages;
+                    const int64_t e = (((int64_t)max(page, 0) * a.kv_heads + head) << a.page_shift) + slot;
+                    load_box(to + at * D, &kmap, 0, slot, head, box_page, bar);
+                    load_box(to + (kSlice + at) * D, &vmap, 0, slot, head, box_page, bar);
+                    load_bytes(scale_to + at, a.k_exp + e, slots, bar);
+                    load_bytes(scale_to + kSlice + at, a.v_exp + e, slots, bar);
+                };
+                if (slots == kSlice) {
+                    copy(0, p[0]);
+                } else if (slots == 16) {
+#pragma unroll
+                    for (int i = 0; i < NP; i++) copy(16 * i, p[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NP; i += 2) copy(16 * i, p[i]);
+                }
+            }
+            filled |= 1u << stage;
+        }
+        fetched++;
+        if (++in_blk == in.p1) {
+            in.next();
+            in_blk = 0;
+        }
+    };
     auto fetch = [&](int stage) {
         filled &= ~(1u << stage);
         if (!in.more) return;
-        if (in.at.b != pg_b || in.at.rt != pg_rt || (in_blk >> 5) != pg_blk) {
-            pg_b = in.at.b;
-            pg_rt = in.at.rt;
-            pg_blk = in_blk >> 5;
-            const int j = in.at.t.lo + ((in_blk & ~31) + lane) * kKeys + warp * kSlice;
-            const int seen_lo = line.seen(in.at.r, line.token(in.at.rt * kRows)).x;
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                pg[i] = -1;
-                if (j + 16 * i < in.at.t.hi && ((j + 16 * i) | (slots - 1)) >= seen_lo) {  // else no row's business
-                    const int page = a.table[(int64_t)in.at.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
-                    if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
-                    else range = true;
-                }
-            }
-        }
+        look_up();
         const int p0 = __shfl_sync(~0u, pg[0], in_blk & 31), p1 = __shfl_sync(~0u, pg[1], in_blk & 31);
         gaps = (gaps & ~(3u << 2 * stage)) | ((p0 < 0 ? 1u : 0u) | (p1 < 0 ? 2u : 0u)) << 2 * stage;
         if (p0 >= 0 || p1 >= 0) {
@@ -165,18 +225,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             const uint32_t bar = __shfl_sync(~0u, smem_u32(&s_bar[warp][stage]), 0), to = __shfl_sync(~0u, ring + stage * kStage, 0);
             if (fetched != a.skip && elect_one()) {  // (left out: a test's wait runs out)
                 const CUtensorMap* const map = in_v ? &vmap : &kmap;
-                mbar_expect(bar, kStage + (Q ? kSlice : 0));
+                mbar_expect(bar, kStage);
 #pragma unroll
-                for (int d = 0; d < (Q ? 1 : D / 64); d++) {  // a page that is none reads as zeros
+                for (int d = 0; d < D / 64; d++) {  // a page that is none reads as zeros
                     load_box(to + d * (kSlice * 128), map, d * 64, slot, head, p0 >= 0 ? p0 : a.n_pages, bar);
-                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + kStage / (Q ? 2 : 2 * (D / 64)), map, d * 64, slot, head, p1 >= 0 ? p1 : a.n_pages, bar);
-                }
-                if constexpr (Q) {  // (of any page, if it is none)
-                    const uint8_t* const e = in_v ? a.v_exp : a.k_exp;
-                    auto from = [&](int page) { return e + ((((int64_t)max(page, 0) * a.kv_heads + head) << a.page_shift) + slot); };
-                    const uint32_t at = scales + stage * kSlice;
-                    load_bytes(at, from(p0), slots, bar);
-                    if (slots < kSlice) load_bytes(at + 16, from(p1), 16, bar);
+                    if (slots < kSlice) load_box(to + d * (kSlice * 128) + 16 * 128, map, d * 64, slot, head, p1 >= 0 ? p1 : a.n_pages, bar);
                 }
             }
             filled |= 1u << stage;
@@ -190,7 +243,10 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
         }
     };
 #pragma unroll
-    for (int s = 0; s < kStages; s++) fetch(s);
+    for (int s = 0; s < kStages; s++) {
+        if constexpr (Q) fetch8(s);
+        else fetch(s);
+    }
 
     const float mul = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : kLog2e * a.scale, cap2 = a.cap * kLog2e;
     uint32_t qf[NR][KS][2];
@@ -211,7 +267,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
         return !dead;
     };
     auto advance = [&] {
-        if (!dead) fetch(stage);
+        if constexpr (Q) {
+            if (!dead) fetch8(stage);
+        } else {
+            if (!dead) fetch(stage);
+        }
         stage = stage + 1 == kStages ? 0 : stage + 1;
     };
 
@@ -223,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             for (int n = 0; n < NR; n++) {
                 {
                     const int r = first + min(8 * n + (lane >> 2), rows - 1), tok = line.token(r), g = r - tok * a.group;
-                    const uint16_t* const q = a.q + (int64_t)(at.r.q0 + tok) * a.q_tok + (int64_t)(at.h * a.group + g) * a.q_head + (Q ? 4 : 2) * (lane & 3);
+                    const uint16_t* const q = a.q + (int64_t)(at.r.q0 + tok) * a.q_tok + (int64_t)(((at.h << hs) + my_head) * a.group + g) * a.q_head + (Q ? 4 : 2) * (lane & 3);
 #pragma unroll
                     for (int k = 0; k < KS; k++) {
                         if constexpr (Q) {  // a register of codes holds four neighbours: theirs
@@ -279,12 +339,171 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             any_see = make_int2(s0.x, s1.y);
         }
         for (int blk = w.p0; blk < w.p1; blk++) {
-        const int j0 = at.t.lo + blk * kKeys + warp * kSlice;
+        const int j0 = at.t.lo + blk * line.keys() + my_slice;
+        if constexpr (Q) {
+            const uint32_t gap = gaps >> NP * stage & kAllGaps;
+            const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || gap;
+            if (ready()) {
+                const uint32_t kt = ring + stage * kStage, vt = kt + kSlice * D, ke = scales + stage * 2 * kSlice + (lane >> 2), ve = ke + kSlice;
+                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y; };
+                bool odd = false;  // a value that some rows see and others do not is NaN
+                if (edge && (any_see.x != all_see.x || any_see.y != all_see.y)) {
+#pragma unroll 1
+                    for (int c = lane; c < kSlice * D / 16; c += 32) {
+                        uint32_t w[4];
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                     : "r"(vt + c * 16));
+                        odd |= (any_nan8(w[0]) || any_nan8(w[1]) || any_nan8(w[2]) || any_nan8(w[3])) && seen(j0 + c / (D / 16));
+                    }
+                    odd = __any_sync(~0u, odd);
+                }
+                // Sixteen positions at a time in a rolled loop: unrolled, what 64 or 32 of them take left the instruction cache.
+#pragma unroll 1
+                for (int t = 0; t < MT; t++) {
+                    float s[NR][4];  // scores, then weights: position 16 t + (lane >> 2) + 8 (i >> 1), row 8 n + 2 (lane & 3) + (i & 1)
+#pragma unroll
+                    for (int n = 0; n < NR; n++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) s[n][i] = 0.f;
+                    const uint32_t krow = kt + (16 * t + (lane & 15)) * D;
+#pragma unroll
+                    for (int k = 0; k < KS; k += 2) {
+                        uint32_t x[4];
+                        ldsm4(x, krow + ((k + (lane >> 4)) << 4 ^ flip));
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            const uint32_t kf[4] = {half2_of(x[2 * i]), half2_of(x[2 * i + 1]), half2_of(x[2 * i] >> 16), half2_of(x[2 * i + 1] >> 16)};
+#pragma unroll
+                            for (int n = 0; n < NR; n++) mma<true>(s[n], kf, qf[n][k + i][0], qf[n][k + i][1]);
+                        }
+                    }
+                    float ks[2], vs[2];  // scales of the keys, exponents of the values'
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        ks[i] = scale_of(load_u8(ke + 16 * t + 8 * i));
+                        vs[i] = (float)((int)load_u8(ve + 16 * t + 8 * i) - 127);
+                    }
+                    float top[NR][2], topo[NR][2];
+#pragma unroll
+                    for (int n = 0; n < NR; n++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) s[n][i] *= ks[i >> 1];
+                    bool raise = false;
+#pragma unroll
+                    for (int n = 0; n < NR; n++) {
+#pragma unroll
+                        for (int i = 0; i < 4; i++) s[n][i] = score(s[n][i], qmul[n][i & 1], cap2);
+                        if (edge) {
+                            const int j = j0 + 16 * t + (lane >> 2);
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                if (j + 8 * (i >> 1) < see[n][i & 1].x || j + 8 * (i >> 1) >= see[n][i & 1].y || (gap >> t & 1)) s[n][i] = -INFINITY;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            top[n][i] = fmaxf(s[n][i], s[n][i + 2]);
+                            topo[n][i] = fmaxf(s[n][i] + vs[0], s[n][i + 2] + vs[1]);
+                            raise |= raises<true>(top[n][i], m[n][i]) || raises<true>(topo[n][i], mo[n][i]);
+                        }
+                    }
+                    if (__any_sync(~0u, raise)) {
+#pragma unroll
+                        for (int n = 0; n < NR; n++)
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                float to = top[n][i], too = topo[n][i];
+#pragma unroll
+                                for (int x = 4; x < 32; x <<= 1) {
+                                    to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
+                                    too = fmaxf(too, __shfl_xor_sync(~0u, too, x));
+                                }
+                                to = fmaxf(to, m[n][i]);
+                                too = fmaxf(too, mo[n][i]);
+                                l[n][i] *= m[n][i] == -INFINITY ? 0.f : exp2_fast(m[n][i] - to);
+                                const float keep = mo[n][i] == -INFINITY ? 0.f : exp2_fast(mo[n][i] - too);
+                                m[n][i] = to;
+                                mo[n][i] = too;
+#pragma unroll
+                                for (int d = 0; d < DT; d++) {
+                                    o[n][d][i] *= keep;
+                                    o[n][d][i + 2] *= keep;
+                                }
+                            }
+                    }
+                    uint32_t pf[NR][2];
+#pragma unroll
+                    for (int n = 0; n < NR; n++) {
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            const float shift = (m[n][i] == -INFINITY ? 0.f : m[n][i]) - kLift<true>, shifto = (mo[n][i] == -INFINITY ? 0.f : mo[n][i]) - kLift<true>;
+                            l[n][i] += exp2_fast(s[n][i] - shift) + exp2_fast(s[n][i + 2] - shift);
+                            s[n][i] = exp2_fast(s[n][i] + vs[0] - shifto);
+                            s[n][i + 2] = exp2_fast(s[n][i + 2] + vs[1] - shifto);
+                        }
+                        pf[n][0] = transpose8(pack2<true>(s[n][0], s[n][1]));
+                        pf[n][1] = transpose8(pack2<true>(s[n][2], s[n][3]));
+                    }
+                    if (!odd) {
+                        uint32_t keep[2] = {~0u, ~0u};  // values of positions that no row sees are taken as zero, whatever is stored there
+                        if (edge) {
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                const int j = j0 + 16 * t + 8 * i + 2 * (lane & 3);
+                                keep[i] = (seen(j) ? 0xffffu : 0u) | (seen(j + 1) ? 0xffff0000u : 0u);
+                            }
+                        }
+                        const uint32_t vrow = vt + (16 * t + (lane & 15)) * D;
+#pragma unroll
+                        for (int d = 0; d < DT; d += 2) {
+                            // Transposed in pairs of columns: a register holds two columns of two positions.
+                            uint32_t x[4];
+                            ldsm4t(x, vrow + ((d + (lane >> 4)) << 4 ^ flip));
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                const uint32_t y = __byte_perm(x[2 * i], 0, 0x3120), z = __byte_perm(x[2 * i + 1], 0, 0x3120);
+                                const uint32_t vf[4] = {half2_of(y) & keep[0], half2_of(y >> 16) & keep[0], half2_of(z) & keep[1], half2_of(z >> 16) & keep[1]};
+#pragma unroll
+                                for (int n = 0; n < NR; n++) mma<true>(o[n][d + i], vf, pf[n][0], pf[n][1]);
+                            }
+                        }
+                    } else {  // row by row, over what each sees
+#pragma unroll 1
+                        for (int k = 0; k < 16; k++) {
+                            const int from = (k & 7) * 4 + (lane & 3), j = j0 + 16 * t + k;
+#pragma unroll
+                            for (int n = 0; n < NR; n++) {
+                                float w[2];
+                                bool see_k[2];
+#pragma unroll
+                                for (int i = 0; i < 2; i++) {
+                                    w[i] = __shfl_sync(~0u, k & 8 ? s[n][2 + i] : s[n][i], from);
+                                    see_k[i] = j >= see[n][i].x && j < see[n][i].y && !(gap >> t & 1);
+                                }
+#pragma unroll
+                                for (int d = 0; d < 2 * DT; d++) {
+                                    const uint32_t at = vt + chunk_at<D, Q>(16 * t + k, d >> 1) + 2 * (lane >> 2) + (d & 1);
+                                    const float v = unpack2<true>(half2_of((uint16_t)load_u8(at))).x;
+#pragma unroll
+                                    for (int i = 0; i < 2; i++) {
+                                        float& y = o[n][d >> 1][2 * (d & 1) + i];
+                                        if (see_k[i]) y = fmaf(w[i], v, y);
+                                    }
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+            if (blk + 1 < w.p1) {
+                __syncwarp();
+                advance();
+            }
+        } else {
         const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || (gaps >> 2 * stage & 3);
         const uint32_t gap = gaps >> 2 * stage & 3;
         float s[NR][MT][4];  // scores, then weights: position 16 t + (lane >> 2) + 8 (i >> 1), row 8 n + 2 (lane & 3) + (i & 1)
         const bool some = ready();
-        float ks[MT][2];  // 8 bits: scales of the keys of positions 16 t + (lane >> 2) + 8 i
         if (some) {
             const uint32_t st = ring + stage * kStage;
 #pragma unroll
@@ -293,71 +512,43 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                 for (int t = 0; t < MT; t++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) s[n][t][i] = 0.f;
-            if constexpr (Q) {
 #pragma unroll
-                for (int t = 0; t < MT; t++)
+            for (int k = 0; k < KS; k++)
 #pragma unroll
-                    for (int i = 0; i < 2; i++) ks[t][i] = scale_of(load_u8(scales + stage * kSlice + 16 * t + 8 * i + (lane >> 2)));
+                for (int t = 0; t < MT; t++) {
+                    uint32_t kf[4];
+                    ldsm4(kf, st + chunk_at<D, Q>(16 * t + (lane & 15), 2 * k + (lane >> 4)));
 #pragma unroll
-                for (int k = 0; k < KS; k += 2)
-#pragma unroll
-                    for (int t = 0; t < MT; t++) {
-                        uint32_t x[4];
-                        ldsm4(x, st + chunk_at<D, Q>(16 * t + (lane & 15), k + (lane >> 4)));
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint32_t kf[4] = {half2_of(x[2 * i]), half2_of(x[2 * i + 1]), half2_of(x[2 * i] >> 16), half2_of(x[2 * i + 1] >> 16)};
-#pragma unroll
-                            for (int n = 0; n < NR; n++) mma<true>(s[n][t], kf, qf[n][k + i][0], qf[n][k + i][1]);
-                        }
-                    }
-            } else {
-#pragma unroll
-                for (int k = 0; k < KS; k++)
-#pragma unroll
-                    for (int t = 0; t < MT; t++) {
-                        uint32_t kf[4];
-                        ldsm4(kf, st + chunk_at<D, Q>(16 * t + (lane & 15), 2 * k + (lane >> 4)));
-#pragma unroll
-                        for (int n = 0; n < NR; n++) mma<H>(s[n][t], kf, qf[n][k][0], qf[n][k][1]);
-                    }
-            }
+                    for (int n = 0; n < NR; n++) mma<H>(s[n][t], kf, qf[n][k][0], qf[n][k][1]);
+                }
         }
         __syncwarp();
         advance();
         const bool have = ready();
         const uint32_t st = ring + stage * kStage;
         if (some && have) {
-            float top[NR][2], topo[NR][2];
-            float ve[MT][2];  // 8 bits: exponents of the values' scales
-            if constexpr (Q) {
-#pragma unroll
-                for (int t = 0; t < MT; t++)
-#pragma unroll
-                    for (int i = 0; i < 2; i++) ve[t][i] = (float)((int)load_u8(scales + stage * kSlice + 16 * t + 8 * i + (lane >> 2)) - 127);
-            }
+            float top[NR][2];
 #pragma unroll
             for (int n = 0; n < NR; n++) {
-                top[n][0] = top[n][1] = topo[n][0] = topo[n][1] = -INFINITY;
+                top[n][0] = top[n][1] = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < MT; t++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         float& x = s[n][t][i];
-                        x = Q ? score(x * ks[t][i >> 1], qmul[n][i & 1], cap2) : score(x, mul, cap2);
+                        x = score(x, mul, cap2);
                         if (edge) {
                             const int j = j0 + 16 * t + (lane >> 2) + 8 * (i >> 1);
                             if (j < see[n][i & 1].x || j >= see[n][i & 1].y || (gap >> t & 1)) x = -INFINITY;
                         }
                         top[n][i & 1] = fmaxf(top[n][i & 1], x);
-                        if (Q) topo[n][i & 1] = fmaxf(topo[n][i & 1], x + ve[t][i >> 1]);
                     }
             }
             bool raise = false;
 #pragma unroll
             for (int n = 0; n < NR; n++)
 #pragma unroll
-                for (int i = 0; i < 2; i++) raise |= raises<F16>(top[n][i], m[n][i]) || (Q && raises<F16>(topo[n][i], mo[n][i]));
+                for (int i = 0; i < 2; i++) raise |= raises<H>(top[n][i], m[n][i]);
             if (__any_sync(~0u, raise)) {
 #pragma unroll
                 for (int n = 0; n < NR; n++)
@@ -367,17 +558,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
                         to = fmaxf(to, m[n][i]);
-                        float keep = m[n][i] == -INFINITY ? 0.f : exp2_fast(m[n][i] - to);
+                        const float keep = m[n][i] == -INFINITY ? 0.f : exp2_fast(m[n][i] - to);
                         m[n][i] = to;
                         l[n][i] *= keep;
-                        if constexpr (Q) {
-                            to = topo[n][i];
-#pragma unroll
-                            for (int x = 4; x < 32; x <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
-                            to = fmaxf(to, mo[n][i]);
-                            keep = mo[n][i] == -INFINITY ? 0.f : exp2_fast(mo[n][i] - to);
-                            mo[n][i] = to;
-                        }
 #pragma unroll
                         for (int d = 0; d < DT; d++) {
                             o[n][d][i] *= keep;
@@ -390,16 +573,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             for (int n = 0; n < NR; n++)
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
-                    const float shift[2] = {(m[n][0] == -INFINITY ? 0.f : m[n][0]) - kLift<F16>, (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kLift<F16>};
-                    const float shifto[2] = {(mo[n][0] == -INFINITY ? 0.f : mo[n][0]) - kLift<F16>, (mo[n][1] == -INFINITY ? 0.f : mo[n][1]) - kLift<F16>};
+                    const float shift[2] = {(m[n][0] == -INFINITY ? 0.f : m[n][0]) - kLift<H>, (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kLift<H>};
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const float x = s[n][t][i], p = exp2_fast(x - shift[i & 1]);
-                        s[n][t][i] = Q ? exp2_fast(x + ve[t][i >> 1] - shifto[i & 1]) : p;
-                        l[n][i & 1] += p;
+                        s[n][t][i] = exp2_fast(s[n][t][i] - shift[i & 1]);
+                        l[n][i & 1] += s[n][t][i];
                     }
-                    pf[n][t][0] = transpose8(pack2<F16>(s[n][t][0], s[n][t][1]));
-                    pf[n][t][1] = transpose8(pack2<F16>(s[n][t][2], s[n][t][3]));
+                    pf[n][t][0] = transpose8(pack2<H>(s[n][t][0], s[n][t][1]));
+                    pf[n][t][1] = transpose8(pack2<H>(s[n][t][2], s[n][t][3]));
                 }
             // Values of positions that no row sees are taken as zero, whatever is stored there.
             uint32_t keep[MT][2];
@@ -415,41 +596,19 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     }
                 if (any_see.x != all_see.x || any_see.y != all_see.y) {  // a value that some rows see must be finite for the others
 #pragma unroll 1
-                    for (int c = lane; c < kStage / 16; c += 32) {
+                    for (int c = lane; c < kSlice * D / 8; c += 32) {
                         uint32_t w[4];
                         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                                      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
                                      : "r"(st + c * 16));
                         bool x = false;
-                        for (int i = 0; i < 4; i++) x |= Q ? any_nan8(w[i]) : any_nonfinite<H>(w[i]);
-                        odd |= x && seen(j0 + (c >> (Q && D == 64 ? 2 : 3)) % kSlice);
+                        for (int i = 0; i < 4; i++) x |= any_nonfinite<H>(w[i]);
+                        odd |= x && seen(j0 + (c >> 3) % kSlice);
                     }
                     odd = __any_sync(~0u, odd);
                 }
             }
-            if (Q && !odd) {
-#pragma unroll
-                for (int d = 0; d < DT; d += 2)
-#pragma unroll
-                    for (int t = 0; t < MT; t++) {
-                        // Transposed in pairs of columns: a register holds two columns of two positions.
-                        uint32_t x[4];
-                        ldsm4t(x, st + chunk_at<D, Q>(16 * t + (lane & 15), d + (lane >> 4)));
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint32_t y = __byte_perm(x[2 * i], 0, 0x3120), z = __byte_perm(x[2 * i + 1], 0, 0x3120);
-                            uint32_t vf[4] = {half2_of(y), half2_of(y >> 16), half2_of(z), half2_of(z >> 16)};
-                            if (edge) {
-                                vf[0] &= keep[t][0];
-                                vf[1] &= keep[t][0];
-                                vf[2] &= keep[t][1];
-                                vf[3] &= keep[t][1];
-                            }
-#pragma unroll
-                            for (int n = 0; n < NR; n++) mma<true>(o[n][d + i], vf, pf[n][t][0], pf[n][t][1]);
-                        }
-                    }
-            } else if (!odd) {
+            if (!odd) {
 #pragma unroll
                 for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -481,14 +640,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         }
 #pragma unroll
                         for (int d = 0; d < 2 * DT; d++) {
-                            float v;
-                            if constexpr (Q) {
-                                v = unpack2<true>(half2_of((uint16_t)load_u8(st + chunk_at<D, Q>(k, d >> 1) + 2 * (lane >> 2) + (d & 1)))).x;
-                            } else {
-                                uint16_t x;
-                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(st + chunk_at<D, Q>(k, d) + 2 * (lane >> 2)));
-                                v = unpack2<H>(x).x;
-                            }
+                            uint16_t x;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(st + chunk_at<D, Q>(k, d) + 2 * (lane >> 2)));
+                            const float v = unpack2<H>(x).x;
 #pragma unroll
                             for (int i = 0; i < 2; i++) {
                                 float& y = o[n][d >> 1][2 * (d & 1) + i];
@@ -503,6 +657,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
         if (blk + 1 < w.p1) {
             __syncwarp();
             advance();
+        }
         }
         }
         {  // the end of a tile, or of this CTA's piece of it
@@ -521,12 +676,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             __syncthreads();
             const bool whole = w.whole(s_part);
             float* const piece = a.pieces + (int64_t)(2 * blockIdx.x + w.begins(s_part)) * kPieceFloats<D>;
-            // N columns of a row, whole.
-            auto row_out = [&](int r, int c, auto& x, float to, float sum) {
+            // N columns of a row of the tile's head `of`, whole.
+            auto row_out = [&](int of, int r, int c, auto& x, float to, float sum) {
                 constexpr int N = sizeof(x) / sizeof(float);
                 const int tok = line.token(first + r), g = first + r - tok * a.group;
                 const int64_t t = at.r.q0 + tok;
-                const int h = at.h * a.group + g;
+                const int h = ((at.h << hs) + of) * a.group + g;
                 const int64_t row = t * a.heads + h;
                 if (a.part == Part::kLeave) {
                     for (int i = 0; i < N; i += 2) *reinterpret_cast<float2*>(a.sums + row * D + c + i) = make_float2(x[i], x[i + 1]);
@@ -554,8 +709,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     const int r = 2 * (lane & 3) + i;
-                    float to = s_m[0][8 * n + r];
-                    for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][8 * n + r]);
+                    float to = s_m[my_head * of_head][8 * n + r];
+                    for (int w = 1; w < of_head; w++) to = fmaxf(to, s_m[my_head * of_head + w][8 * n + r]);
                     const float f = exp2_fast((Q ? mo[n][i] : m[n][i]) - (to == -INFINITY ? 0.f : to));
 #pragma unroll
                     for (int d = 0; d < DT; d++) {
@@ -568,12 +723,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     }
                 }
                 __syncthreads();
-                for (int i = tid; i < min(8, rows - 8 * n) * kQuads; i += kThreads) {
-                    const int r8 = i / kQuads, c = 4 * (i % kQuads), r = 8 * n + r8;
-                    float to = s_m[0][r], sum = 0.f;
-                    for (int w = 1; w < kWarps; w++) to = fmaxf(to, s_m[w][r]);
+                for (int i = tid; i < (min(8, rows - 8 * n) << hs) * kQuads; i += kThreads) {
+                    const int all = i / kQuads, r8 = all >> hs, of = all - (r8 << hs), c = 4 * (i % kQuads), r = 8 * n + r8, w0 = of * of_head, w1 = w0 + of_head;
+                    float to = s_m[w0][r], sum = 0.f;
+                    for (int w = w0 + 1; w < w1; w++) to = fmaxf(to, s_m[w][r]);
                     float x[4] = {};
-                    for (int w = 0; w < kWarps; w++) {
+                    for (int w = w0; w < w1; w++) {
                         const float4 y = *reinterpret_cast<const float4*>(ring_ptr + (w - warp) * kStages * kStage + stage * kStage + 4 * sum_at(r8, c));
                         x[0] += y.x;
                         x[1] += y.y;
@@ -582,10 +737,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
                     }
                     if (whole) {
-                        row_out(r, c, x, to, sum);
+                        row_out(of, r, c, x, to, sum);
                     } else {
-                        *reinterpret_cast<float4*>(piece + r * D + c) = make_float4(x[0], x[1], x[2], x[3]);
-                        if (c == 0) *reinterpret_cast<float2*>(piece + kMostRows * D + 2 * r) = make_float2(to, sum);
+                        const int pr = (r << hs) + of;
+                        *reinterpret_cast<float4*>(piece + pr * D + c) = make_float4(x[0], x[1], x[2], x[3]);
+                        if (c == 0) *reinterpret_cast<float2*>(piece + kMostRows * D + 2 * pr) = make_float2(to, sum);
                     }
                 }
             }
@@ -609,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     // A warp to a row: the factors of 32 pieces at once, a piece per lane, then their sums, loads of several in
                     // flight.
                     constexpr int V = D / 32;
-                    for (int r = warp; r < rows; r += kWarps) {
+                    for (int r = warp; r < rows << hs; r += kWarps) {
                         float to = -INFINITY, sum = 0.f, x[V] = {};
                         for (int64_t p0 = c0; p0 <= c1; p0 += 32) {
                             const int n = (int)min((int64_t)32, c1 - p0 + 1);
@@ -640,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                                 }
                             }
                         }
-                        row_out(r, V * lane, x, to, sum);
+                        row_out(r & ((1 << hs) - 1), r >> hs, V * lane, x, to, sum);
                     }
                 }
             }

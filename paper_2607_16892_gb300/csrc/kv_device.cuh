@@ -153,7 +153,8 @@ struct Tile {
     int lo, hi, blocks;  // positions [lo, hi), lo aligned
 };
 
-template <int kRowsOf, int kKeysOf, int kAlign, int kOverOf>
+// kHeads: a tile may be of 2^a.head_shift key heads, whose blocks then have that much fewer positions.
+template <int kRowsOf, int kKeysOf, int kAlign, int kOverOf, bool kHeads = false>
 struct Line {
     static constexpr int kRows = kRowsOf, kKeys = kKeysOf, kOver = kOverOf;
     const AttendArgs& a;
@@ -161,6 +162,12 @@ struct Line {
 
     __device__ __forceinline__ explicit Line(const AttendArgs& args) : a(args) {}
 
+    __device__ __forceinline__ int keys() const { return kHeads ? kKeys >> a.head_shift : kKeys; }
+    __device__ __forceinline__ int head_tiles() const { return kHeads ? a.kv_heads >> a.head_shift : a.kv_heads; }
+    __device__ __forceinline__ int blocks(int positions) const {
+        if constexpr (kHeads) return (positions + keys() - 1) >> (__ffs(kKeys) - 1 - a.head_shift);
+        else return (positions + kKeys - 1) / kKeys;
+    }
     __device__ __forceinline__ int token(int row) const { return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift); }
     __device__ __forceinline__ Request request(int b) {
         Request r;
@@ -202,7 +209,7 @@ struct Line {
         Tile t;
         t.hi = seen(r, token(last)).y;
         t.lo = min(seen(r, token(first)).x, t.hi) & ~(kAlign - 1);
-        t.blocks = max(1, (t.hi - t.lo + kKeys - 1) / kKeys);
+        t.blocks = max(1, blocks(t.hi - t.lo));
         return t;
     }
     __device__ __forceinline__ int row_tiles(const Request& r) const { return (r.rows + kRows - 1) / kRows; }
@@ -210,7 +217,7 @@ struct Line {
     __device__ __forceinline__ int64_t cost(const Request& r, int first = 0, int step = 1) const {
         int64_t c = 0;
         for (int rt = first, n = row_tiles(r); rt < n; rt += step) c += tile(r, rt).blocks + kOver;
-        return c * a.kv_heads;
+        return c * head_tiles();
     }
 };
 
@@ -244,7 +251,7 @@ struct Cursor {
         }
         for (rt = 0;; rt += 32) {  // 32 row tiles at a time
             const bool there = rt + lane < line.row_tiles(r);
-            const int64_t mine = there ? (int64_t)(line.tile(r, rt + lane).blocks + L::kOver) * line.a.kv_heads : 0;
+            const int64_t mine = there ? (int64_t)(line.tile(r, rt + lane).blocks + L::kOver) * line.head_tiles() : 0;
             int64_t incl = mine;
             for (int o = 1; o < 32; o <<= 1) {
                 const int64_t x = __shfl_up_sync(~0u, incl, o);
@@ -268,7 +275,7 @@ struct Cursor {
     template <class L>
     __device__ __forceinline__ void next(L& line) {
         start += t.blocks + L::kOver;
-        if (++h < line.a.kv_heads) return;
+        if (++h < line.head_tiles()) return;
         h = 0;
         if (++rt >= line.row_tiles(r)) {
             rt = 0;
