@@ -37,15 +37,15 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 
-// Quantises as it copies: strides of the rows in 16-byte units, of the cache in 8-byte ones.
+// Quantises as it copies: all strides in 16-byte units.
 struct Append8Args {
     const uint4 *k, *v;
-    uint2 *kc, *vc;
+    uint4 *kc, *vc;
     uint8_t *k_exp, *v_exp;
     int64_t k_tok, k_head, v_tok, v_head;
     int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
     const int32_t* slot;
-    int32_t T, n_slots, page_shift, heads, vec_shift;  // vectors of 8 elements of a head: 1 << vec_shift
+    int32_t T, n_slots, page_shift, heads, part_shift;  // parts of 16 elements of a head: 1 << part_shift
     bool half;
     int32_t* err;
 };

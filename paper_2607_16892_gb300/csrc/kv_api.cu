@@ -422,26 +422,26 @@ int kvdro_kv_append(kvdro_kv* kv, int32_t T, const void* k, const int64_t* k_str
         kvdro::Append8Args a;
         a.k = static_cast<const uint4*>(k);
         a.v = static_cast<const uint4*>(v);
-        a.kc = static_cast<uint2*>(kv->k);
-        a.vc = static_cast<uint2*>(kv->v);
+        a.kc = static_cast<uint4*>(kv->k);
+        a.vc = static_cast<uint4*>(kv->v);
         a.k_exp = kv->k_exp;
         a.v_exp = kv->v_exp;
         a.k_tok = ks[0] / 8;
         a.k_head = ks[1] / 8;
         a.v_tok = vs[0] / 8;
         a.v_head = vs[1] / 8;
-        a.kc_page = kv->k_stride[0] / 8;
-        a.kc_slot = kv->k_stride[1] / 8;
-        a.kc_head = kv->k_stride[2] / 8;
-        a.vc_page = kv->v_stride[0] / 8;
-        a.vc_slot = kv->v_stride[1] / 8;
-        a.vc_head = kv->v_stride[2] / 8;
+        a.kc_page = kv->k_stride[0] / 16;
+        a.kc_slot = kv->k_stride[1] / 16;
+        a.kc_head = kv->k_stride[2] / 16;
+        a.vc_page = kv->v_stride[0] / 16;
+        a.vc_slot = kv->v_stride[1] / 16;
+        a.vc_head = kv->v_stride[2] / 16;
         a.slot = slot;
         a.T = T;
         a.n_slots = kv->n_pages << kv->page_shift;
         a.page_shift = kv->page_shift;
         a.heads = kv->heads;
-        a.vec_shift = log2_of(kv->head_dim / 8);
+        a.part_shift = log2_of(kv->head_dim / 16);
         a.half = kv->half;
         a.err = static_cast<int32_t*>(ctx->kv_err.p);
         ctx->kv_last = s;

@@ -304,52 +304,67 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append(AppendArgs a, int 
     }
 }
 
-// Eight elements of a row as codes, the row's other vectors in the neighbouring lanes of `mask`: the scale is the least power of two
+// Sixteen elements of a row as codes, the row's others in the neighbouring `lanes` of `mask`: the scale is the least power of two
 // 2^E, E >= -126, with max |x| <= 448 2^E over the row's finite elements, and each element is rounded once, to the nearest code.
 // A power of two costs no precision (codes are floating-point numbers of three bits whatever their scale) and multiplies
 // exactly.  Non-finite elements become NaN.  FP16 cannot hold 256 * 2^8, which its largest numbers would round to: 240 * 2^8.
 // `e`: E + 127.
 template <bool H>
-__device__ __forceinline__ uint2 quantise(const uint4& x, unsigned mask, int lanes, uint32_t& e) {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    float f[8], top = 0.f;
+__device__ __forceinline__ uint4 quantise(const uint4 (&x)[2], unsigned mask, int lanes, uint32_t& e) {
+    constexpr uint32_t kInf = H ? 0x7c00u : 0x7f80u;
+    const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+    uint32_t top2 = 0;  // magnitudes of 16-bit numbers are ordered as whole numbers, two at a time
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const float2 y = kv::unpack2<H>(w[i]);
-        f[2 * i] = y.x;
-        f[2 * i + 1] = y.y;
+    for (int i = 0; i < 8; i++) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
+    for (int o = 1; o < lanes; o <<= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(mask, top2, o));
+    uint32_t top16 = max(top2 & 0xffffu, top2 >> 16);
+    const bool odd = top16 >= kInf;
+    if (odd) {  // the largest of the finite ones
+        top2 = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t y = w[i] & 0x7fff7fffu;
+            top2 = __vmaxu2(top2, ((y & 0xffffu) < kInf ? y & 0xffffu : 0u) | (y >> 16 < kInf ? y & 0xffff0000u : 0u));
+        }
+        for (int o = 1; o < lanes; o <<= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(mask, top2, o));
+        top16 = max(top2 & 0xffffu, top2 >> 16);
     }
+    const uint32_t u = __float_as_uint(kv::unpack2<H>(top16).x);
+    e = (uint32_t)max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 1);  // 448 = 1.75 * 2^8
+    const float down = __uint_as_float((254 - e) << 23);
+    float2 y[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        const float y = fabsf(f[i]);
-        top = fmaxf(top, y < INFINITY ? y : 0.f);
+        y[i] = kv::unpack2<H>(w[i]);
+        y[i].x *= down;
+        y[i].y *= down;
     }
-    for (int o = 1; o < lanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(mask, top, o));
-    const uint32_t u = __float_as_uint(top);
-    e = (uint32_t)max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 1);  // 448 = 1.75 * 2^8
-    const float down = __uint_as_float((254 - e) << 23), most = H && e == 135 ? 240.f : 448.f;
+    if (odd || (H && e == 135)) {
+        const float most = H && e == 135 ? 240.f : 448.f, nan = __uint_as_float(0x7fffffffu);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            y[i] = make_float2(fminf(fmaxf(y[i].x, -most), most), fminf(fmaxf(y[i].y, -most), most));
+            if ((w[i] & 0x7fffu) >= kInf) y[i].x = nan;
+            if ((w[i] >> 16 & 0x7fffu) >= kInf) y[i].y = nan;
+        }
+    }
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        float y[2];
+        uint16_t r[2];
 #pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const float z = f[2 * i + k];
-            y[k] = fabsf(z) < INFINITY ? fminf(fmaxf(z * down, -most), most) : __uint_as_float(0x7fffffffu);
-        }
-        uint16_t r;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y[1]), "f"(y[0]));
-        c[i] = r;
+        for (int k = 0; k < 2; k++) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r[k]) : "f"(y[2 * i + k].y), "f"(y[2 * i + k].x));
+        c[i] = __byte_perm(r[0], r[1], 0x5410);
     }
-    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    return make_uint4(c[0], c[1], c[2], c[3]);
 }
 
-// As the copy above, and bound by the same; lanes that share a head's row find its largest element by shuffles.
-constexpr int kAppend8Deep = 2;
+// As the copy above, with sixteen elements to a lane: what is done once for a row weighs less.  XX
+constexpr int kAppend8Deep = 1, kAppend8Threads = 128, kAppend8Ctas = 10;
 
 template <bool H>
-__global__ void __launch_bounds__(kAppendThreads) k_kv_append8(Append8Args a, int lanes_shift) {
-    const int64_t id = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x, t = id >> lanes_shift;
+__global__ void __launch_bounds__(kAppend8Threads, kAppend8Ctas) k_kv_append8(Append8Args a, int lanes_shift) {
+    const int64_t id = (int64_t)blockIdx.x * kAppend8Threads + threadIdx.x, t = id >> lanes_shift;
     const int lanes = 1 << lanes_shift;
     if (t >= a.T) return;
     const int32_t slot = a.slot[t];
@@ -358,44 +373,53 @@ __global__ void __launch_bounds__(kAppendThreads) k_kv_append8(Append8Args a, in
         return;
     }
     const int64_t page = slot >> a.page_shift, in = slot & ((1 << a.page_shift) - 1);
-    const uint4 *k = a.k + t * a.k_tok, *v = a.v + t * a.v_tok;
-    uint2 *kc = a.kc + page * a.kc_page + in * a.kc_slot, *vc = a.vc + page * a.vc_page + in * a.vc_slot;
-    const int vecs = a.heads << a.vec_shift, row = 1 << a.vec_shift;
-    const unsigned mask = ((1u << row) - 1u) << (threadIdx.x & 31 & ~(row - 1));  // 8 or 16 lanes, all of one token
-    for (int i0 = (int)id & (lanes - 1); i0 < vecs; i0 += kAppend8Deep * lanes) {
-        uint4 x[kAppend8Deep], y[kAppend8Deep];
+    // A lane has the same part of every head that it comes to: its addresses advance by the same steps.
+    const int row = 1 << a.part_shift, c = (int)id & (row - 1), by = lanes >> a.part_shift;
+    int h = ((int)id & (lanes - 1)) >> a.part_shift;
+    const uint4 *k = a.k + t * a.k_tok + h * a.k_head + 2 * c, *v = a.v + t * a.v_tok + h * a.v_head + 2 * c;
+    uint4 *kc = a.kc + page * a.kc_page + in * a.kc_slot + h * a.kc_head + c, *vc = a.vc + page * a.vc_page + in * a.vc_slot + h * a.vc_head + c;
+    const int64_t k_by = by * a.k_head, v_by = by * a.v_head, kc_by = by * a.kc_head, vc_by = by * a.vc_head;
+    int64_t at = ((page * a.heads + h) << a.page_shift) + in;
+    const int64_t at_by = (int64_t)by << a.page_shift;
+    const unsigned mask = ((1u << row) - 1u) << (threadIdx.x & 31 & ~(row - 1));  // 4 or 8 lanes, all of one token
+    for (; h < a.heads; h += kAppend8Deep * by) {
+        uint4 x[kAppend8Deep][2], y[kAppend8Deep][2];
 #pragma unroll
         for (int u = 0; u < kAppend8Deep; u++) {
-            const int i = i0 + u * lanes;
-            if (i < vecs) {
-                x[u] = k[(i >> a.vec_shift) * a.k_head + (i & (row - 1))];
-                y[u] = v[(i >> a.vec_shift) * a.v_head + (i & (row - 1))];
+            if (h + u * by < a.heads) {
+                x[u][0] = k[0];
+                x[u][1] = k[1];
+                y[u][0] = v[0];
+                y[u][1] = v[1];
             }
+            k += k_by;
+            v += v_by;
         }
 #pragma unroll
         for (int u = 0; u < kAppend8Deep; u++) {
-            const int i = i0 + u * lanes, h = i >> a.vec_shift, c = i & (row - 1);
-            if (i < vecs) {
+            if (h + u * by < a.heads) {
                 uint32_t ke, ve;
-                kc[h * a.kc_head + c] = quantise<H>(x[u], mask, row, ke);
-                vc[h * a.vc_head + c] = quantise<H>(y[u], mask, row, ve);
+                *kc = quantise<H>(x[u], mask, row, ke);
+                *vc = quantise<H>(y[u], mask, row, ve);
                 if (c == 0) {
-                    const int64_t at = ((page * a.heads + h) << a.page_shift) + in;
                     a.k_exp[at] = (uint8_t)ke;
                     a.v_exp[at] = (uint8_t)ve;
                 }
             }
+            kc += kc_by;
+            vc += vc_by;
+            at += at_by;
         }
     }
 }
 
 // Rows out of pages: a copy with two lookups, the request of a token and its page.  A token's row is dealt to lanes as above, eight
 // elements each at a time.
-constexpr int kReadDeep = 2;
+constexpr int kReadDeep = 2, kReadThreads = 128;
 
 template <bool H, bool Q>
-__global__ void __launch_bounds__(kAppendThreads) k_kv_read(ReadArgs a, int lanes_shift) {
-    const int64_t id = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x, t64 = id >> lanes_shift;
+__global__ void __launch_bounds__(kReadThreads) k_kv_read(ReadArgs a, int lanes_shift) {
+    const int64_t id = (int64_t)blockIdx.x * kReadThreads + threadIdx.x, t64 = id >> lanes_shift;
     const int lanes = 1 << lanes_shift;
     if (t64 >= a.T) return;
     const int t = (int)t64;
@@ -474,7 +498,7 @@ int lanes_of(int vecs) {
     while (shift < 5 && (1 << shift) < vecs) shift++;
     return shift;
 }
-unsigned ctas_of(int64_t T, int lanes_shift) { return (unsigned)(((T << lanes_shift) + kAppendThreads - 1) / kAppendThreads); }
+unsigned ctas_of(int64_t T, int lanes_shift, int threads) { return (unsigned)(((T << lanes_shift) + threads - 1) / threads); }
 
 __global__ void k_kv_take(int32_t* err) { err[1] = atomicExch(err, 0); }
 
@@ -499,23 +523,23 @@ cudaError_t launch_kv_plan(const PlanArgs& a, int sms, cudaStream_t s) {
 
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s) {
     const int shift = lanes_of(a.heads << a.vec_shift);
-    k_kv_append<<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
+    k_kv_append<<<ctas_of(a.T, shift, kAppendThreads), kAppendThreads, 0, s>>>(a, shift);
     return cudaGetLastError();
 }
 
 cudaError_t launch_kv_append8(const Append8Args& a, cudaStream_t s) {
-    const int shift = lanes_of(a.heads << a.vec_shift);
-    if (a.half) k_kv_append8<true><<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
-    else k_kv_append8<false><<<ctas_of(a.T, shift), kAppendThreads, 0, s>>>(a, shift);
+    const int shift = lanes_of(a.heads << a.part_shift);
+    if (a.half) k_kv_append8<true><<<ctas_of(a.T, shift, kAppend8Threads), kAppend8Threads, 0, s>>>(a, shift);
+    else k_kv_append8<false><<<ctas_of(a.T, shift, kAppend8Threads), kAppend8Threads, 0, s>>>(a, shift);
     return cudaGetLastError();
 }
 
 cudaError_t launch_kv_read(const ReadArgs& a, cudaStream_t s) {
     const int shift = lanes_of(a.heads << a.vec_shift);
-    const unsigned ctas = ctas_of(a.T, shift);
-    if (!a.k_exp) k_kv_read<true, false><<<ctas, kAppendThreads, 0, s>>>(a, shift);
-    else if (a.half) k_kv_read<true, true><<<ctas, kAppendThreads, 0, s>>>(a, shift);
-    else k_kv_read<false, true><<<ctas, kAppendThreads, 0, s>>>(a, shift);
+    const unsigned ctas = ctas_of(a.T, shift, kReadThreads);
+    if (!a.k_exp) k_kv_read<true, false><<<ctas, kReadThreads, 0, s>>>(a, shift);
+    else if (a.half) k_kv_read<true, true><<<ctas, kReadThreads, 0, s>>>(a, shift);
+    else k_kv_read<false, true><<<ctas, kReadThreads, 0, s>>>(a, shift);
     return cudaGetLastError();
 }
 
