@@ -30,6 +30,8 @@
 
 #include "kv_device.cuh"
 
+#include <type_traits>
+
 namespace kvdro {
 
 namespace {
@@ -266,16 +268,16 @@ __device__ __forceinline__ void cap_pair(uint32_t& x0, uint32_t& x1, float mul, 
     x1 = __float_as_uint(y.y);
 }
 
-// Sixteen codes and their scale byte as two chunks of eight 16-bit elements.  FP16: products of FP16 where the scale is one (2^-24
-// to 2^15), rounded once; else, and for BF16, through FP32, exact but for what FP16 cannot hold.
-template <bool H>
-__device__ __forceinline__ void widen(const uint4& codes, uint32_t e, bool in_half, uint4 (&out)[2]) {
+// Sixteen codes and their scale byte as two chunks of eight 16-bit elements.  kInHalf: products of FP16, whose scale is one (2^-24 to
+// 2^15), rounded once; else through FP32, exact but for what FP16 cannot hold.
+template <bool H, bool kInHalf>
+__device__ __forceinline__ void widen(const uint4& codes, uint32_t e, uint4 (&out)[2]) {
     const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
     uint32_t x[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) x[i] = half2_of((uint16_t)(w[i >> 1] >> (i & 1 ? 16 : 0)));
     const float s = scale_of(e);
-    if (H && in_half) {
+    if constexpr (kInHalf) {
         const __half2 s2 = __float2half2_rn(s);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -285,8 +287,8 @@ __device__ __forceinline__ void widen(const uint4& codes, uint32_t e, bool in_ha
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float2 y = unpack2<true>(x[i]);
-            x[i] = pack2<H>(y.x * s, y.y * s);
+            const float2 y = fma2(unpack2<true>(x[i]), make_float2(s, s), make_float2(-0.f, -0.f));
+            x[i] = pack2<H>(y.x, y.y);
         }
     }
     out[0] = make_uint4(x[0], x[1], x[2], x[3]);
@@ -755,6 +757,7 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                 const int part = warp - 10;
                 constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes, kRowsOf = kKeys / 4;  // lanes of a row; rows at a time, and of a warp
                 const int c = lane % kLanes;
+                const bool swap = D == 128 && c >= kLanes / 2;
                 int raw = 0;
                 uint32_t raw_round = 0, turns = 0;
                 while (w.more) {
@@ -767,39 +770,65 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                             if (turns++ >= (uint32_t)kStages) wait(sh.kv_empty[stage], round ^ 1, sh);
                             wait(sh.raw_full[raw], raw_round, sh);
                             __syncwarp();
-                            const bool look = v && w.edge(blk, all);
-                            const int j0 = w.at.t.lo + blk * kKeys;
-                            bool found = false;
-#pragma unroll 4
-                            for (int r = part * kRowsOf + lane / kLanes; r < (part + 1) * kRowsOf; r += kAtOnce) {
-                                uint4 codes, x[2];
-                                uint32_t e;
-                                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                             : "=r"(codes.x), "=r"(codes.y), "=r"(codes.z), "=r"(codes.w)
-                                             : "r"(raw_at + raw * Sh::kCodes + r * D + c * 16));
-                                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(scale_at + raw * kKeys + r));
-                                widen<H>(codes, e, !H || __all_sync(~0u, e >= 103 && e <= 142), x);
-                                if (look) {
+                            // Four rows of a lane at once, so that their loads overlap; what is rare is kept out of this loop, for the
+                            // instruction cache.
+                            auto tile = [&](auto in_half) {
+#pragma unroll 1
+                                for (int r0 = part * kRowsOf + lane / kLanes; r0 < (part + 1) * kRowsOf; r0 += 4 * kAtOnce) {
+                                    uint4 codes[4];
+                                    uint32_t e[4];
 #pragma unroll
-                                    for (int i = 0; i < 8; i++) {
-                                        uint32_t& y = reinterpret_cast<uint32_t*>(x)[i];
-                                        if (!any_nonfinite<H>(y)) continue;
-                                        const float2 f = unpack2<H>(y);
-                                        y &= (isfinite(f.x) ? 0xffffu : 0u) | (isfinite(f.y) ? 0xffff0000u : 0u);
-                                        found |= j0 + r >= seen_lo && j0 + r < w.at.t.hi;
+                                    for (int i = 0; i < 4; i++) {
+                                        const int r = r0 + i * kAtOnce;
+                                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                                     : "=r"(codes[i].x), "=r"(codes[i].y), "=r"(codes[i].z), "=r"(codes[i].w)
+                                                     : "r"(raw_at + raw * Sh::kCodes + r * D + c * 16));
+                                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(scale_at + raw * kKeys + r));
+                                    }
+#pragma unroll
+                                    for (int i = 0; i < 4; i++) {
+                                        const int r = r0 + i * kAtOnce;
+                                        uint4 x[2];
+                                        if (swap) codes[i] = make_uint4(codes[i].z, codes[i].w, codes[i].x, codes[i].y);
+                                        widen<H, decltype(in_half)::value>(codes[i], e[i], x);
+                                        // Chunks 2 c and 2 c + 1 of the row; the half of a long row that stands in other lanes the other way
+                                        // round, for the banks.
+#pragma unroll
+                                        for (int k = 0; k < 2; k++) {
+                                            const int at = 2 * c + (swap ? !k : k);
+                                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(kv_at + stage * kTile + (at >> 3) * (kKeys * 128) +
+                                                                                                      r * 128 + (((at & 7) ^ (r & 7)) << 4)),
+                                                         "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w));
+                                        }
                                     }
                                 }
-                                // Chunks 2 c and 2 c + 1 of the row; the half of a long row that stands in other lanes the other way round, for
-                                // the banks.
-#pragma unroll
-                                for (int i = 0; i < 2; i++) {
-                                    const bool second = D == 128 && c >= kLanes / 2 ? !i : i;
-                                    const int k = 2 * c + second;
-                                    const uint4& y = second ? x[1] : x[0];
-                                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(kv_at + stage * kTile + (k >> 3) * (kKeys * 128) + r * 128 +
-                                                                                              (((k & 7) ^ (r & 7)) << 4)),
-                                                 "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w)
-                                                 : "memory");
+                            };
+                            bool in_half = false;
+                            if constexpr (H) {
+                                uint32_t e;
+                                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(scale_at + raw * kKeys + part * kRowsOf + lane));
+                                in_half = __all_sync(~0u, e >= 103 && e <= 142);
+                            }
+                            if (in_half) tile(std::true_type{});
+                            else tile(std::false_type{});
+                            const bool look = v && w.edge(blk, all);
+                            bool found = false;
+                            if (look) {  // elements that are not finite become zeros
+                                __syncwarp();
+                                const int j0 = w.at.t.lo + blk * kKeys;
+#pragma unroll 1
+                                for (int i = lane; i < kRowsOf * D / 8; i += 32) {
+                                    const int r = part * kRowsOf + (i & (kRowsOf - 1)), half = i / kRowsOf / 8;
+                                    uint4* const at = reinterpret_cast<uint4*>(smem_ptr + 2 * kTile + stage * kTile + half * (kKeys * 128) + r * 128) + (i / kRowsOf & 7);
+                                    uint4 x = *at;
+                                    uint32_t* const y = reinterpret_cast<uint32_t*>(&x);
+                                    if (!(any_nonfinite<H>(x.x) || any_nonfinite<H>(x.y) || any_nonfinite<H>(x.z) || any_nonfinite<H>(x.w))) continue;
+                                    found |= j0 + r >= seen_lo && j0 + r < w.at.t.hi;
+                                    for (int k = 0; k < 4; k++) {
+                                        const float2 f = unpack2<H>(y[k]);
+                                        y[k] &= (isfinite(f.x) ? 0xffffu : 0u) | (isfinite(f.y) ? 0xffff0000u : 0u);
+                                    }
+                                    *at = x;
                                 }
                             }
                             if (look && __any_sync(~0u, found)) {
