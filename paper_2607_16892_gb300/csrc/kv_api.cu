@@ -283,27 +283,29 @@ int attend_args(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, const void*
 }
 
 // The launches of one pass over pages: `most` new tokens of a request at most, as far as is known; `uniform`: every request has
-// as many.
-int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, cudaStream_t s) {
+// as many.  `chunked`: whether the last of them was the kernel for chunks; before, in the same call.
+int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, bool& chunked, cudaStream_t s) {
     const auto decode = a.k_exp ? kvdro::launch_kv_decode8 : kvdro::launch_kv_decode;
     const auto chunk = a.k_exp ? kvdro::launch_kv_chunk8 : kvdro::launch_kv_chunk;
     // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
     // both runs on both, each request on its own.
     const bool eight = a.group <= 8 && most * a.group <= 8;
     if (most * a.group <= kFewRows) {
-        KV_CUDA(decode(a, maps, eight, ctx->sms, s), "attention kernel");
+        KV_CUDA(decode(a, maps, eight, chunked, ctx->sms, s), "attention kernel");
+        chunked = false;
         return KVDRO_OK;
     }
     const int32_t few = (a.group <= 8 ? 8 : kFewRows) / a.group;
     const bool both = few > 0 && !uniform;
     if (both) {
         a.max_q = few;
-        KV_CUDA(decode(a, maps, a.group <= 8, ctx->sms, s), "attention kernel");
+        KV_CUDA(decode(a, maps, a.group <= 8, false, ctx->sms, s), "attention kernel");
         a.min_q = few;
         a.max_q = 0x7fffffff;
-        a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
     }
+    a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);  // scratch of its own: launches of the two kernels overlap
     KV_CUDA(chunk(a, maps, both, ctx->sms, s), "attention kernel");
+    chunked = true;
     return KVDRO_OK;
 }
 
@@ -546,7 +548,8 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     ctx->kv_last = s;
     ScratchTurn turn;
     if (int rc = turn.begin(ctx, s)) return rc;
-    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, s)) return rc;
+    bool chunked = false;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, chunked, s)) return rc;
     return turn.end(ctx, s);
 }
 
@@ -598,9 +601,10 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     p.table = prefix_table;
     p.max_pages = prefix_pages;
     p.causal = false;
-    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, s)) return rc;
+    bool chunked = false;
+    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, chunked, s)) return rc;
     a.part = kvdro::Part::kJoin;
-    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, s)) return rc;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, chunked, s)) return rc;
     return turn.end(ctx, s);
 }
 

@@ -908,71 +908,119 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");  // a launch for few rows before this one, which ran beside it, is done
 }
 
-// Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
-// last of CTA c; eight threads a row's sums, lanes along the rows as the pieces are laid out.  Bound by the latency of its
-// dependent reads (what to join, the pieces), so many threads read little each, four pieces at a time.
-constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinAtOnce = 4;
+// Joins the pieces of tiles that cross CTAs.  A few long tiles have many pieces each, many short ones two or three: the tiles to be
+// joined are counted first, and each is given to 8, 16 or 32 CTAs -- 32 rows, and all, half or a quarter of the columns -- as
+// the grid has room for.  A CTA reads the maxima and sums of its rows' pieces together, then each thread sums its columns over
+// the pieces in order, eight loads in flight; lanes along the rows as the pieces are laid out.  Bound by the latency of those
+// reads.
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinGroups = kRows / kJoinRows, kJoinPieces = 64;  // pieces at a time
 
-template <bool H, int D>
-__global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const Join j = a.joins[blockIdx.x];
-    const int row_in = blockIdx.y * kJoinRows + (threadIdx.x & 31), part = threadIdx.x >> 5;
-    if (j.last < 0 || row_in >= j.rows) return;
-    constexpr int kFloats = Shape<D, false>::kPieceFloats, N = D * 8 / kJoinThreads;  // 16-byte vectors of a part
+template <bool H, int D, int N>  // N: 16-byte vectors of a row and thread
+__device__ __forceinline__ void join_rows(const AttendArgs& a, const Join& j, int c0, int group, int part, float2 (*s_ml)[kJoinRows]) {
+    constexpr int kFloats = Shape<D, false>::kPieceFloats, kAhead = 8 / N;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row_in = group * kJoinRows + lane;
+    const int n = j.last - c0 + 1;
+    auto piece = [&](int p) { return a.pieces + (int64_t)(2 * (c0 + p) + (p == 0)) * kFloats; };
+    const bool valid = row_in < j.rows;
+    const int first = (part * (kJoinThreads / 32) + warp) * N;  // its first vector
     float m = -INFINITY, l = 0.f;
-    float4 o[N];
+    float4 o[N], x[kAhead][N];
 #pragma unroll
     for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = blockIdx.x; c0 <= j.last; c0 += kJoinAtOnce) {
-        float2 ml[kJoinAtOnce];
-        float4 x[kJoinAtOnce][N];
+    auto load = [&](int p) {
 #pragma unroll
-        for (int k = 0; k < kJoinAtOnce; k++) {
-            const int c = min(c0 + k, j.last);
-            const float* const piece = a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats;
-            ml[k] = reinterpret_cast<const float2*>(piece + kRows * D)[row_in];
-            if (c0 + k > j.last) ml[k] = make_float2(-INFINITY, 0.f);
+        for (int k = 0; k < kAhead; k++)
 #pragma unroll
-            for (int i = 0; i < N; i++) x[k][i] = reinterpret_cast<const float4*>(piece)[(part * N + i) * kRows + row_in];
-        }
+            for (int i = 0; i < N; i++) x[k][i] = __ldcg(reinterpret_cast<const float4*>(piece(min(p + k, n - 1))) + (first + i) * kRows + row_in);
+    };
+    load(0);
+    for (int p0 = 0; p0 < n; p0 += kJoinPieces) {
+        const int held = min(kJoinPieces, n - p0);
+        __syncthreads();
+#pragma unroll 4
+        for (int p = warp; p < held; p += kJoinThreads / 32) s_ml[p][lane] = __ldcg(reinterpret_cast<const float2*>(piece(p0 + p) + kRows * D) + row_in);
+        __syncthreads();
         float to = m;
-#pragma unroll
-        for (int k = 0; k < kJoinAtOnce; k++) to = fmaxf(to, ml[k].x);
+#pragma unroll 4
+        for (int p = 0; p < held; p++) to = fmaxf(to, s_ml[p][lane].x);
         const float shift = to == -INFINITY ? 0.f : to, keep = exp2_fast(m - shift);
         m = to;
         l *= keep;
 #pragma unroll
         for (int i = 0; i < N; i++) o[i] = make_float4(o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep);
+#pragma unroll 1
+        for (int p = 0; p < held; p += kAhead) {
+            if (p0 + p > 0) load(p0 + p);
 #pragma unroll
-        for (int k = 0; k < kJoinAtOnce; k++) {
-            if (c0 + k > j.last) break;
-            const float f = exp2_fast(ml[k].x - shift);
-            l += ml[k].y * f;
+            for (int k = 0; k < kAhead; k++) {
+                if (p + k < held) {
+                    const float2 ml = s_ml[p + k][lane];
+                    const float f = exp2_fast(ml.x - shift);
+                    l += ml.y * f;
 #pragma unroll
-            for (int i = 0; i < N; i++)
-                o[i] = make_float4(fmaf(x[k][i].x, f, o[i].x), fmaf(x[k][i].y, f, o[i].y), fmaf(x[k][i].z, f, o[i].z), fmaf(x[k][i].w, f, o[i].w));
+                    for (int i = 0; i < N; i++)
+                        o[i] = make_float4(fmaf(x[k][i].x, f, o[i].x), fmaf(x[k][i].y, f, o[i].y), fmaf(x[k][i].z, f, o[i].z), fmaf(x[k][i].w, f, o[i].w));
+                }
+            }
         }
     }
+    if (!valid) return;
     const ChunkLine line(a);
     const int row = j.row0 + row_in, tok = line.token(row), h = j.h * a.group + row - tok * a.group;
     const int64_t t = j.q0 + tok;
     if (a.part == Part::kLeave) {
-        float4* const to = reinterpret_cast<float4*>(a.sums + (t * a.heads + h) * D + part * (4 * N));
+        float4* const to = reinterpret_cast<float4*>(a.sums + (t * a.heads + h) * D) + first;
 #pragma unroll
         for (int i = 0; i < N; i++) to[i] = o[i];
-        if (part == 0) leave_max<H>(a, t * a.heads + h, m, l);
+        if (first == 0) leave_max<H>(a, t * a.heads + h, m, l);
         return;
     }
     if (a.part == Part::kJoin) {
         const float2 by = join_max<H>(a, t * a.heads + h, m, l);
-        join_sums<D, 4 * N>(a, t * a.heads + h, part * (4 * N), by, reinterpret_cast<float*>(o));
+        join_sums<D, 4 * N>(a, t * a.heads + h, 4 * first, by, reinterpret_cast<float*>(o));
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + part * (4 * N));
+    uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head) + first;
 #pragma unroll
     for (int i = 0; i < N; i++) out[i] = make_uint2(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv));
-    if (a.lse && part == 0) a.lse[t * a.heads + h] = log_sum<H>(m, l);
+    if (a.lse && first == 0) a.lse[t * a.heads + h] = log_sum<H>(m, l);
+}
+
+template <bool H, int D>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a, int ctas) {
+    __shared__ float2 s_ml[kJoinPieces][kJoinRows];
+    __shared__ int s_count[kJoinThreads / 32], s_tile;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a launch for few rows that waits for the sums itself)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Tiles to be joined, and of them this CTA's: the one of rank blockIdx.x / (CTAs of a tile).
+    constexpr int kMost = D / 4 / (kJoinThreads / 32);  // vectors of a row and thread, with all columns
+    int total = 0;
+    for (int c = tid; c - tid < ctas; c += kJoinThreads) total += __syncthreads_count(c < ctas && a.joins[c].last >= 0);
+    int parts = kMost;  // CTAs that share the columns
+    while (parts > 1 && total * kJoinGroups * parts > (int)gridDim.x) parts >>= 1;
+    const int tile = blockIdx.x / (kJoinGroups * parts), rest = blockIdx.x - tile * (kJoinGroups * parts);
+    if (tile >= total) return;
+    int before = 0;
+    for (int c = tid; c - tid < ctas; c += kJoinThreads) {
+        const bool there = c < ctas && a.joins[c].last >= 0;
+        const unsigned all = __ballot_sync(~0u, there);
+        if (lane == 0) s_count[warp] = __popc(all);
+        __syncthreads();
+        int rank = before + __popc(all & ((1u << lane) - 1u));
+        for (int w = 0; w < kJoinThreads / 32; w++) {
+            if (w < warp) rank += s_count[w];
+            before += s_count[w];
+        }
+        if (there && rank == tile) s_tile = c;
+        __syncthreads();
+    }
+    const Join j = a.joins[s_tile];
+    const int group = rest % kJoinGroups, part = rest / kJoinGroups;
+    if (group * kJoinRows >= j.rows) return;
+    if (parts == kMost) join_rows<H, D, 1>(a, j, s_tile, group, part, s_ml);
+    else if (kMost == 4 && parts == 2) join_rows<H, D, 2>(a, j, s_tile, group, part, s_ml);
+    else join_rows<H, D, kMost>(a, j, s_tile, group, part, s_ml);
 }
 
 template <bool H, int D, bool Q>
@@ -1001,11 +1049,11 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool after_few, int 
     c.numAttrs = after_few ? 1 : 0;
     const cudaError_t e = cudaLaunchKernelEx(&c, a.cap > 0.f ? k_kv_chunk<H, D, true, Q> : k_kv_chunk<H, D, false, Q>, a, maps.k, maps.v);
     if (e != cudaSuccess) return e;
-    c.gridDim = dim3(sms, kRows / kJoinRows);
+    c.gridDim = dim3(sms * kJoinGroups);
     c.blockDim = dim3(kJoinThreads);
     c.dynamicSmemBytes = 0;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a);
+    return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a, sms);
 }
 template <bool Q>
 cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s) {

@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     __syncthreads();
     if (s_part.empty()) {
         if (line.bad && tid == 0) atomicOr(a.err, kKvErrRange);
+        if (a.part == Part::kJoin) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
 
@@ -275,6 +276,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
         stage = stage + 1 == kStages ? 0 : stage + 1;
     };
 
+    bool waited = a.part != Part::kJoin;  // for the sums of the launch before, beside which this one may have started
     while (w.more) {
         Cursor& at = w.at;
         {  // a tile begins here, or this CTA's piece of it
@@ -674,6 +676,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     }
                 }
             __syncthreads();
+            if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+            waited = true;
             const bool whole = w.whole(s_part);
             float* const piece = a.pieces + (int64_t)(2 * blockIdx.x + w.begins(s_part)) * kPieceFloats<D>;
             // N columns of a row of the tile's head `of`, whole.
@@ -829,15 +833,23 @@ cudaError_t prepare_all() {
 }
 
 template <bool H, int D, bool Q>
-cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
-    if (eight) k_kv_decode<H, D, 1, Q><<<sms * Ring<D, 1, Q>::kCtas, kThreads, Ring<D, 1, Q>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
-    else k_kv_decode<H, D, 2, Q><<<sms * Ring<D, 2, Q>::kCtas, kThreads, Ring<D, 2, Q>::kSmem, s>>>(a, maps.k_slice, maps.v_slice);
-    return cudaGetLastError();
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(sms * (eight ? Ring<D, 1, Q>::kCtas : Ring<D, 2, Q>::kCtas));
+    c.blockDim = dim3(kThreads);
+    c.dynamicSmemBytes = eight ? Ring<D, 1, Q>::kSmem : Ring<D, 2, Q>::kSmem;
+    c.stream = s;
+    c.attrs = at;
+    c.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&c, eight ? k_kv_decode<H, D, 1, Q> : k_kv_decode<H, D, 2, Q>, a, maps.k_slice, maps.v_slice);
 }
 template <bool Q>
-cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, bool eight, int sms, cudaStream_t s) {
-    if (a.half) return a.head_dim == 128 ? launch<true, 128, Q>(a, maps, eight, sms, s) : launch<true, 64, Q>(a, maps, eight, sms, s);
-    return a.head_dim == 128 ? launch<false, 128, Q>(a, maps, eight, sms, s) : launch<false, 64, Q>(a, maps, eight, sms, s);
+cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
+    if (a.half) return a.head_dim == 128 ? launch<true, 128, Q>(a, maps, eight, early, sms, s) : launch<true, 64, Q>(a, maps, eight, early, sms, s);
+    return a.head_dim == 128 ? launch<false, 128, Q>(a, maps, eight, early, sms, s) : launch<false, 64, Q>(a, maps, eight, early, sms, s);
 }
 
 }  // namespace
