@@ -110,11 +110,11 @@ struct AttendArgs {
 size_t kv_decode_piece_bytes(int sms);
 int kv_decode_ctas(int sms);
 cudaError_t kv_decode_prepare();
-// `eight`: at most eight rows share a key head (else sixteen; more are right, but slow).  `early`: may start while kv_chunk's last
-// launch before it, whose sums it joins, ends.
+// `rows`: that share a key head, at most (more are right, but slow).  `early`: may start while the launch before it, whose sums it
+// joins, ends.
 cudaError_t kv_decode8_prepare();
-cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s);
-cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s);
+cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
+cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 cudaError_t kv_chunk_prepare();
 cudaError_t kv_chunk8_prepare();

@@ -24,7 +24,7 @@ constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
 constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
 // Rows that share a key head, up to which the kernel for single tokens runs.  32 requests of 3000 positions, 8 key heads of 128:
 // 12 rows 77 us there; 20 to 32 rows 140 us there, 85 on the kernel for chunks; 64 rows 249 and 85.
-constexpr int64_t kFewRows = 16;
+constexpr int64_t kFewRows = 16, kFewRows8 = 24;
 
 int log2_of(int32_t v) {
     int s = 0;
@@ -135,7 +135,7 @@ int prepare_attend(kvdro_ctx* ctx) {
     const size_t pieces = kvdro::kv_decode_piece_bytes(ctx->sms) + kvdro::kv_chunk_piece_bytes(ctx->sms);
     if (int rc = ensure(ctx, ctx->kv_pieces, pieces)) return rc;
     if (int rc = ensure(ctx, ctx->kv_joins, sizeof(kvdro::Join) * (size_t)ctx->sms)) return rc;
-    const size_t tickets = 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);
+    const size_t tickets = 2 * 4 * (size_t)kvdro::kv_decode_ctas(ctx->sms);  // of two launches that overlap
     if (int rc = ensure(ctx, ctx->kv_tickets, tickets)) return rc;
     if (int rc = clear(ctx, ctx->kv_tickets.p, tickets)) return rc;
     ctx->kv_ready = true;
@@ -283,29 +283,34 @@ int attend_args(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, const void*
 }
 
 // The launches of one pass over pages: `most` new tokens of a request at most, as far as is known; `uniform`: every request has
-// as many.  `chunked`: whether the last of them was the kernel for chunks; before, in the same call.
-int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, bool& chunked, cudaStream_t s) {
+// as many.  `before`: the kernel of the launch before it in the same call, whose sums it joins; that of its own last one after.
+enum class Last { kNone, kFew, kChunks };
+int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps, int64_t most, bool uniform, Last& before, cudaStream_t s) {
     const auto decode = a.k_exp ? kvdro::launch_kv_decode8 : kvdro::launch_kv_decode;
     const auto chunk = a.k_exp ? kvdro::launch_kv_chunk8 : kvdro::launch_kv_chunk;
+    float* const second = a.pieces + kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
     // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
-    // both runs on both, each request on its own.
-    const bool eight = a.group <= 8 && most * a.group <= 8;
-    if (most * a.group <= kFewRows) {
-        KV_CUDA(decode(a, maps, eight, chunked, ctx->sms, s), "attention kernel");
-        chunked = false;
+    // both runs on both, each request on its own.  What overlaps has scratch of its own.
+    if (most * a.group <= (a.k_exp ? kFewRows8 : kFewRows)) {
+        if (before == Last::kFew) {
+            a.pieces = second;
+            a.tickets += kvdro::kv_decode_ctas(ctx->sms);
+        }
+        KV_CUDA(decode(a, maps, (int)(most * a.group), before != Last::kNone, ctx->sms, s), "attention kernel");
+        before = Last::kFew;
         return KVDRO_OK;
     }
     const int32_t few = (a.group <= 8 ? 8 : kFewRows) / a.group;
     const bool both = few > 0 && !uniform;
     if (both) {
         a.max_q = few;
-        KV_CUDA(decode(a, maps, a.group <= 8, false, ctx->sms, s), "attention kernel");
+        KV_CUDA(decode(a, maps, a.group <= 8 ? 8 : (int)kFewRows, false, ctx->sms, s), "attention kernel");
         a.min_q = few;
         a.max_q = 0x7fffffff;
     }
-    a.pieces += kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);  // scratch of its own: launches of the two kernels overlap
+    a.pieces = second;
     KV_CUDA(chunk(a, maps, both, ctx->sms, s), "attention kernel");
-    chunked = true;
+    before = Last::kChunks;
     return KVDRO_OK;
 }
 
@@ -548,8 +553,8 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
     ctx->kv_last = s;
     ScratchTurn turn;
     if (int rc = turn.begin(ctx, s)) return rc;
-    bool chunked = false;
-    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, chunked, s)) return rc;
+    Last before = Last::kNone;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, before, s)) return rc;
     return turn.end(ctx, s);
 }
 
@@ -601,10 +606,10 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     p.table = prefix_table;
     p.max_pages = prefix_pages;
     p.causal = false;
-    bool chunked = false;
-    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, chunked, s)) return rc;
+    Last before = Last::kNone;
+    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, before, s)) return rc;
     a.part = kvdro::Part::kJoin;
-    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, chunked, s)) return rc;
+    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, before, s)) return rc;
     return turn.end(ctx, s);
 }
 

@@ -8,8 +8,8 @@ int kv_decode_ctas(int sms) { return sms * kMostCtas; }
 
 cudaError_t kv_decode_prepare() { return prepare_all<false>(); }
 
-cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
-    return launch_any<false>(a, maps, eight, early, sms, s);
+cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
+    return launch_any<false>(a, maps, rows, early, sms, s);
 }
 
 }  // namespace kvdro

@@ -1,6 +1,6 @@
 // Attention of few rows over pages: single tokens, drafted tokens.
 //
-// Bound by the bytes of the keys and values, each read once for the (at most 16) rows that share a key head.  The line of
+// Bound by the bytes of the keys and values, each read once for the (at most 16; 8 bits: 24) rows that share a key head.  The line of
 // all blocks of 128 positions is dealt to two to four CTAs per SM (kv_device.cuh); in a block each of a CTA's four warps has 32
 // positions of its own, with its own ring of tensor copies, maxima, sums and weighted sums: nothing in the loop waits
 // for another warp.  The warps are joined through shared memory at the end of a tile, pieces of a tile through
@@ -30,7 +30,7 @@ namespace {
 
 using namespace kv;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 16;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 24;
 constexpr int kMostCtas = 4;  // per SM
 constexpr int kOver = 2;      // a tile's fixed cost, in blocks (0 / 1 / 2: window case 41.3 / 40.3 / 39.6 us)
 constexpr int kAtOnce = 8;    // pieces read at a time
@@ -824,32 +824,46 @@ template <bool H, int D, int NR, bool Q>
 cudaError_t prepare() {
     return cudaFuncSetAttribute(k_kv_decode<H, D, NR, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NR, Q>::kSmem);
 }
+template <bool H, int D, bool Q>
+cudaError_t prepare() {
+    cudaError_t e = prepare<H, D, 1, Q>();
+    if (e == cudaSuccess) e = prepare<H, D, 2, Q>();
+    if constexpr (Q)
+        if (e == cudaSuccess) e = prepare<H, D, 3, Q>();
+    return e;
+}
 template <bool Q>
 cudaError_t prepare_all() {
-    for (cudaError_t e : {prepare<false, 64, 1, Q>(), prepare<false, 64, 2, Q>(), prepare<true, 64, 1, Q>(), prepare<true, 64, 2, Q>(),
-                          prepare<false, 128, 1, Q>(), prepare<false, 128, 2, Q>(), prepare<true, 128, 1, Q>(), prepare<true, 128, 2, Q>()})
+    for (cudaError_t e : {prepare<false, 64, Q>(), prepare<true, 64, Q>(), prepare<false, 128, Q>(), prepare<true, 128, Q>()})
         if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
 
-template <bool H, int D, bool Q>
-cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
+template <bool H, int D, int NR, bool Q>
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool early, int sms, cudaStream_t s) {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(sms * (eight ? Ring<D, 1, Q>::kCtas : Ring<D, 2, Q>::kCtas));
+    c.gridDim = dim3(sms * Ring<D, NR, Q>::kCtas);
     c.blockDim = dim3(kThreads);
-    c.dynamicSmemBytes = eight ? Ring<D, 1, Q>::kSmem : Ring<D, 2, Q>::kSmem;
+    c.dynamicSmemBytes = Ring<D, NR, Q>::kSmem;
     c.stream = s;
     c.attrs = at;
     c.numAttrs = early ? 1 : 0;
-    return cudaLaunchKernelEx(&c, eight ? k_kv_decode<H, D, 1, Q> : k_kv_decode<H, D, 2, Q>, a, maps.k_slice, maps.v_slice);
+    return cudaLaunchKernelEx(&c, k_kv_decode<H, D, NR, Q>, a, maps.k_slice, maps.v_slice);
+}
+template <bool H, int D, bool Q>
+cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
+    if (rows <= 8) return launch<H, D, 1, Q>(a, maps, early, sms, s);
+    if constexpr (Q)
+        if (rows > 16) return launch<H, D, 3, Q>(a, maps, early, sms, s);
+    return launch<H, D, 2, Q>(a, maps, early, sms, s);
 }
 template <bool Q>
-cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
-    if (a.half) return a.head_dim == 128 ? launch<true, 128, Q>(a, maps, eight, early, sms, s) : launch<true, 64, Q>(a, maps, eight, early, sms, s);
-    return a.head_dim == 128 ? launch<false, 128, Q>(a, maps, eight, early, sms, s) : launch<false, 64, Q>(a, maps, eight, early, sms, s);
+cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
+    if (a.half) return a.head_dim == 128 ? launch<true, 128, Q>(a, maps, rows, early, sms, s) : launch<true, 64, Q>(a, maps, rows, early, sms, s);
+    return a.head_dim == 128 ? launch<false, 128, Q>(a, maps, rows, early, sms, s) : launch<false, 64, Q>(a, maps, rows, early, sms, s);
 }
 
 }  // namespace

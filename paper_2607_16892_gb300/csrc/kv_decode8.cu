@@ -5,8 +5,8 @@ namespace kvdro {
 
 cudaError_t kv_decode8_prepare() { return prepare_all<true>(); }
 
-cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, bool eight, bool early, int sms, cudaStream_t s) {
-    return launch_any<true>(a, maps, eight, early, sms, s);
+cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
+    return launch_any<true>(a, maps, rows, early, sms, s);
 }
 
 }  // namespace kvdro
