@@ -45,7 +45,10 @@ struct Ring {  // a stage: K or V of a slice; 8 bits: both
     static constexpr int kBytes = kSlice * D * 2;
     static constexpr int kStages = D == 128 || Q ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6);
     static constexpr int kScales = Q ? kWarps * kStages * 2 * kSlice : 0;  // a byte per key and value, behind the ring
-    static constexpr int kSmem = kWarps * kStages * kBytes + kScales + 1024;
+    // Queries in shared memory where they and the sums do not fit the registers (24 rows of 128, 32 requests of 3000: 78 us in registers, 52 so).
+    static constexpr bool kHoldQ = Q && D == 128 && NR == 3;
+    static constexpr int kQAt = kWarps * kStages * kBytes + kScales, kQueries = kHoldQ ? NR * (D / 16) * 32 * 8 : 0;
+    static constexpr int kSmem = kQAt + kQueries + 1024;
     static_assert(Stretch<kThreads>::kScratch <= kSmem, "the ring is scratch first");
 };
 // A piece in global memory: rows (8 bits: of two heads, if of eight) of D sums, then their maxima and sums of weights.
@@ -118,6 +121,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     const int hs = Q && NR == 1 ? a.head_shift : 0, of_head = kWarps >> hs, my_head = warp / of_head, my_slice = (warp & (of_head - 1)) * kSlice;
     const uint32_t flip = (D == 128 ? lane & 7 : lane >> 1 & 3) << 4;  // 8 bits: how chunks of row lane & 15 of sixteen are permuted
     const uint32_t scales = ((raw + 1023) & ~1023u) + kWarps * kStages * kStage + warp * kStages * 2 * kSlice;
+    constexpr bool kHoldQ = Ring<D, NR, Q>::kHoldQ;
+    uint2* const s_q = reinterpret_cast<uint2*>(s_raw + (((raw + 1023) & ~1023u) - raw) + Ring<D, NR, Q>::kQAt) + lane;
     DecodeLine line(a);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // a launch for many rows may fill SMs that this one leaves
 
@@ -254,6 +259,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     float o[NR][DT][4];  // columns 16 d + (lane >> 2) and 8 more (8 bits: 16 d + 2 (lane >> 2) and 1 more), of the rows
     float m[NR][2], l[NR][2];  // of rows 8 n + 2 (lane & 3) + i
     float mo[NR][2], qmul[NR][2];  // 8 bits: what O refers to, and what turns products into scores
+    float up[NR][2], upo[NR][2];   // 8 bits: m and mo are raised above this
     int2 see[NR][2];
     int2 all_see, any_see;  // positions that every row of the tile sees, and that some row does
     bool dead = false;
@@ -324,11 +330,18 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     } else {
                         qmul[n][0] = qmul[n][1] = mul;
                     }
+                    if constexpr (kHoldQ) {
+                        if (warp == 0) {
+#pragma unroll
+                            for (int k = 0; k < KS; k++) s_q[(n * KS + k) * 32] = make_uint2(qf[n][k][0], qf[n][k][1]);
+                        }
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     see[n][i] = line.seen(at.r, line.token(first + min(8 * n + 2 * (lane & 3) + i, rows - 1)));
-                    m[n][i] = mo[n][i] = -INFINITY;
+                    m[n][i] = mo[n][i] = Q ? 0.f : -INFINITY;
+                    up[n][i] = upo[n][i] = -INFINITY;
                     l[n][i] = 0.f;
                 }
 #pragma unroll
@@ -339,6 +352,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             const int2 s0 = line.seen(at.r, line.token(first)), s1 = line.seen(at.r, line.token(first + rows - 1));
             all_see = make_int2(s1.x, s0.y);
             any_see = make_int2(s0.x, s1.y);
+            if constexpr (kHoldQ) __syncthreads();
         }
         for (int blk = w.p0; blk < w.p1; blk++) {
         const int j0 = at.t.lo + blk * line.keys() + my_slice;
@@ -377,7 +391,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         for (int i = 0; i < 2; i++) {
                             const uint32_t kf[4] = {half2_of(x[2 * i]), half2_of(x[2 * i + 1]), half2_of(x[2 * i] >> 16), half2_of(x[2 * i + 1] >> 16)};
 #pragma unroll
-                            for (int n = 0; n < NR; n++) mma<true>(s[n], kf, qf[n][k + i][0], qf[n][k + i][1]);
+                            for (int n = 0; n < NR; n++) {
+                                uint2 q = make_uint2(qf[n][k + i][0], qf[n][k + i][1]);
+                                if constexpr (kHoldQ)
+                                    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q.x), "=r"(q.y) : "r"(smem_u32(s_q + (n * KS + k + i) * 32)));
+                                mma<true>(s[n], kf, q.x, q.y);
+                            }
                         }
                     }
                     float ks[2], vs[2];  // scales of the keys, exponents of the values'
@@ -406,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         for (int i = 0; i < 2; i++) {
                             top[n][i] = fmaxf(s[n][i], s[n][i + 2]);
                             topo[n][i] = fmaxf(s[n][i] + vs[0], s[n][i + 2] + vs[1]);
-                            raise |= raises<true>(top[n][i], m[n][i]) || raises<true>(topo[n][i], mo[n][i]);
+                            raise |= top[n][i] > up[n][i] || topo[n][i] > upo[n][i];
                         }
                     }
                     if (__any_sync(~0u, raise)) {
@@ -420,10 +439,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                                     to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
                                     too = fmaxf(too, __shfl_xor_sync(~0u, too, x));
                                 }
-                                to = fmaxf(to, m[n][i]);
-                                too = fmaxf(too, mo[n][i]);
-                                l[n][i] *= m[n][i] == -INFINITY ? 0.f : exp2_fast(m[n][i] - to);
-                                const float keep = mo[n][i] == -INFINITY ? 0.f : exp2_fast(mo[n][i] - too);
+                                // Nothing seen so far: 0 stands for the maximum, and sums are 0.  (As raises(), by the maximum itself.)
+                                if (up[n][i] != -INFINITY) to = fmaxf(to, m[n][i]);
+                                if (upo[n][i] != -INFINITY) too = fmaxf(too, mo[n][i]);
+                                up[n][i] = to + (fabsf(to) > 0x1p19f ? 0.f : kRaise);
+                                upo[n][i] = too + (fabsf(too) > 0x1p19f ? 0.f : kRaise);
+                                if (to == -INFINITY) to = too = 0.f;
+                                l[n][i] *= exp2_fast(fminf(m[n][i] - to, 0.f));
+                                const float keep = exp2_fast(fminf(mo[n][i] - too, 0.f));
                                 m[n][i] = to;
                                 mo[n][i] = too;
 #pragma unroll
@@ -438,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     for (int n = 0; n < NR; n++) {
 #pragma unroll
                         for (int i = 0; i < 2; i++) {
-                            const float shift = (m[n][i] == -INFINITY ? 0.f : m[n][i]) - kLift<true>, shifto = (mo[n][i] == -INFINITY ? 0.f : mo[n][i]) - kLift<true>;
+                            const float shift = m[n][i] - kLift<true>, shifto = mo[n][i] - kLift<true>;
                             l[n][i] += exp2_fast(s[n][i] - shift) + exp2_fast(s[n][i + 2] - shift);
                             s[n][i] = exp2_fast(s[n][i] + vs[0] - shifto);
                             s[n][i + 2] = exp2_fast(s[n][i + 2] + vs[1] - shifto);
@@ -463,8 +486,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                             ldsm4t(x, vrow + ((d + (lane >> 4)) << 4 ^ flip));
 #pragma unroll
                             for (int i = 0; i < 2; i++) {
-                                const uint32_t y = __byte_perm(x[2 * i], 0, 0x3120), z = __byte_perm(x[2 * i + 1], 0, 0x3120);
-                                const uint32_t vf[4] = {half2_of(y) & keep[0], half2_of(y >> 16) & keep[0], half2_of(z) & keep[1], half2_of(z >> 16) & keep[1]};
+                                const uint32_t y = __byte_perm(x[2 * i] & keep[0], 0, 0x3120), z = __byte_perm(x[2 * i + 1] & keep[1], 0, 0x3120);
+                                const uint32_t vf[4] = {half2_of(y), half2_of(y >> 16), half2_of(z), half2_of(z >> 16)};
 #pragma unroll
                                 for (int n = 0; n < NR; n++) mma<true>(o[n][d + i], vf, pf[n][0], pf[n][1]);
                             }
@@ -668,6 +691,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             for (int n = 0; n < NR; n++)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
+                    if (Q && up[n][i] == -INFINITY) m[n][i] = mo[n][i] = -INFINITY;
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(~0u, l[n][i], x);
                     if (lane < 4) {
