@@ -908,12 +908,83 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");  // a launch for few rows before this one, which ran beside it, is done
 }
 
-// Joins the pieces of tiles that cross CTAs.  A few long tiles have many pieces each, many short ones two or three: the tiles to be
-// joined are counted first, and each is given to 8, 16 or 32 CTAs -- 32 rows, and all, half or a quarter of the columns -- as
-// the grid has room for.  A CTA reads the maxima and sums of its rows' pieces together, then each thread sums its columns over
+// Joins the pieces of tiles that cross CTAs: block (c, g) the rows 32 g .. 32 g + 31 of the tile whose first piece is the
+// last of CTA c; eight threads a row's sums, lanes along the rows as the pieces are laid out.  Bound by the latency of its
+// dependent reads (what to join, the pieces), so many threads read little each, four pieces at a time.
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinGroups = kRows / kJoinRows, kJoinAtOnce = 4;
+
+template <bool H, int D>
+__global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a launch for few rows that waits for the sums itself)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Join j = a.joins[blockIdx.x];
+    const int row_in = blockIdx.y * kJoinRows + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    if (j.last < 0 || row_in >= j.rows) return;
+    constexpr int kFloats = Shape<D, false>::kPieceFloats, N = D * 8 / kJoinThreads;  // 16-byte vectors of a part
+    float m = -INFINITY, l = 0.f;
+    float4 o[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = blockIdx.x; c0 <= j.last; c0 += kJoinAtOnce) {
+        float2 ml[kJoinAtOnce];
+        float4 x[kJoinAtOnce][N];
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; k++) {
+            const int c = min(c0 + k, j.last);
+            const float* const piece = a.pieces + (int64_t)(2 * c + (c == (int)blockIdx.x)) * kFloats;
+            ml[k] = reinterpret_cast<const float2*>(piece + kRows * D)[row_in];
+            if (c0 + k > j.last) ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[k][i] = reinterpret_cast<const float4*>(piece)[(part * N + i) * kRows + row_in];
+        }
+        float to = m;
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; k++) to = fmaxf(to, ml[k].x);
+        const float shift = to == -INFINITY ? 0.f : to, keep = exp2_fast(m - shift);
+        m = to;
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < N; i++) o[i] = make_float4(o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep);
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; k++) {
+            if (c0 + k > j.last) break;
+            const float f = exp2_fast(ml[k].x - shift);
+            l += ml[k].y * f;
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                o[i] = make_float4(fmaf(x[k][i].x, f, o[i].x), fmaf(x[k][i].y, f, o[i].y), fmaf(x[k][i].z, f, o[i].z), fmaf(x[k][i].w, f, o[i].w));
+        }
+    }
+    const ChunkLine line(a);
+    const int row = j.row0 + row_in, tok = line.token(row), h = j.h * a.group + row - tok * a.group;
+    const int64_t t = j.q0 + tok;
+    if (a.part == Part::kLeave) {
+        float4* const to = reinterpret_cast<float4*>(a.sums + (t * a.heads + h) * D + part * (4 * N));
+#pragma unroll
+        for (int i = 0; i < N; i++) to[i] = o[i];
+        if (part == 0) leave_max<H>(a, t * a.heads + h, m, l);
+        return;
+    }
+    if (a.part == Part::kJoin) {
+        const float2 by = join_max<H>(a, t * a.heads + h, m, l);
+        join_sums<D, 4 * N>(a, t * a.heads + h, part * (4 * N), by, reinterpret_cast<float*>(o));
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint2* const out = reinterpret_cast<uint2*>(a.out + t * a.out_tok + h * a.out_head + part * (4 * N));
+#pragma unroll
+    for (int i = 0; i < N; i++) out[i] = make_uint2(pack2<H>(o[i].x * inv, o[i].y * inv), pack2<H>(o[i].z * inv, o[i].w * inv));
+    if (a.lse && part == 0) a.lse[t * a.heads + h] = log_sum<H>(m, l);
+}
+
+// The same where there are few tiles, long ones of many pieces: each is given to 8, 16 or 32 CTAs -- 32 rows, and all, half or a
+// quarter of the columns -- as many as run at once.  A CTA reads the maxima and sums of its rows' pieces together, then each thread sums its columns over
 // the pieces in order, eight loads in flight; lanes along the rows as the pieces are laid out.  Bound by the latency of those
 // reads.
-constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinGroups = kRows / kJoinRows, kJoinPieces = 64;  // pieces at a time
+constexpr int kJoinCtas = 3, kJoinPieces = 64;  // per SM; pieces at a time
+constexpr int kJoinMost = 1024;                 // CTAs of the launch before, at most
+// Up to this many tiles.  64 requests behind a prefix of 32768, 8 tiles of 19 pieces: 85 us in all, 93 with the other; 512 tokens over
+// 4099, 64 tiles of three: 47.4 us in all, 45.1 with the other.
+constexpr int64_t kFewTiles = 38;
 
 template <bool H, int D, int N>  // N: 16-byte vectors of a row and thread
 __device__ __forceinline__ void join_rows(const AttendArgs& a, const Join& j, int c0, int group, int part, float2 (*s_ml)[kJoinRows]) {
@@ -987,40 +1058,41 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, const Join& j, in
 }
 
 template <bool H, int D>
-__global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a, int ctas) {
+__global__ void __launch_bounds__(kJoinThreads, kJoinCtas) k_kv_join_few(const AttendArgs a, int ctas) {
     __shared__ float2 s_ml[kJoinPieces][kJoinRows];
-    __shared__ int s_count[kJoinThreads / 32], s_tile;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a launch for few rows that waits for the sums itself)
+    __shared__ unsigned s_there[kJoinMost / 32];
+    const int tid = threadIdx.x, lane = tid & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // Tiles to be joined, and of them this CTA's: the one of rank blockIdx.x / (CTAs of a tile).
     constexpr int kMost = D / 4 / (kJoinThreads / 32);  // vectors of a row and thread, with all columns
+    for (int c = tid; c - tid < ctas; c += kJoinThreads) {
+        const unsigned there = __ballot_sync(~0u, c < ctas && a.joins[c].last >= 0);
+        if (lane == 0) s_there[c / 32] = there;
+    }
+    __syncthreads();
+    const int words = (ctas + 31) / 32;
     int total = 0;
-    for (int c = tid; c - tid < ctas; c += kJoinThreads) total += __syncthreads_count(c < ctas && a.joins[c].last >= 0);
-    int parts = kMost;  // CTAs that share the columns
-    while (parts > 1 && total * kJoinGroups * parts > (int)gridDim.x) parts >>= 1;
+    for (int w = 0; w < words; w++) total += __popc(s_there[w]);
+    int parts = kMost;  // CTAs that share the columns: as many as run at once
+    while (parts > 1 && total * kJoinGroups * parts > kJoinCtas * ctas) parts >>= 1;
     const int tile = blockIdx.x / (kJoinGroups * parts), rest = blockIdx.x - tile * (kJoinGroups * parts);
     if (tile >= total) return;
-    int before = 0;
-    for (int c = tid; c - tid < ctas; c += kJoinThreads) {
-        const bool there = c < ctas && a.joins[c].last >= 0;
-        const unsigned all = __ballot_sync(~0u, there);
-        if (lane == 0) s_count[warp] = __popc(all);
-        __syncthreads();
-        int rank = before + __popc(all & ((1u << lane) - 1u));
-        for (int w = 0; w < kJoinThreads / 32; w++) {
-            if (w < warp) rank += s_count[w];
-            before += s_count[w];
+    int c0 = 0;
+    for (int rank = tile;; c0 += 32) {
+        const int n = __popc(s_there[c0 / 32]);
+        if (rank < n) {
+            c0 += __fns(s_there[c0 / 32], 0, rank + 1);
+            break;
         }
-        if (there && rank == tile) s_tile = c;
-        __syncthreads();
+        rank -= n;
     }
-    const Join j = a.joins[s_tile];
+    const Join j = a.joins[c0];
     const int group = rest % kJoinGroups, part = rest / kJoinGroups;
     if (group * kJoinRows >= j.rows) return;
-    if (parts == kMost) join_rows<H, D, 1>(a, j, s_tile, group, part, s_ml);
-    else if (kMost == 4 && parts == 2) join_rows<H, D, 2>(a, j, s_tile, group, part, s_ml);
-    else join_rows<H, D, kMost>(a, j, s_tile, group, part, s_ml);
+    if (parts == kMost) join_rows<H, D, 1>(a, j, c0, group, part, s_ml);
+    else if (kMost == 4 && parts == 2) join_rows<H, D, 2>(a, j, c0, group, part, s_ml);
+    else join_rows<H, D, kMost>(a, j, c0, group, part, s_ml);
 }
 
 template <bool H, int D, bool Q>
@@ -1049,11 +1121,16 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool after_few, int 
     c.numAttrs = after_few ? 1 : 0;
     const cudaError_t e = cudaLaunchKernelEx(&c, a.cap > 0.f ? k_kv_chunk<H, D, true, Q> : k_kv_chunk<H, D, false, Q>, a, maps.k, maps.v);
     if (e != cudaSuccess) return e;
-    c.gridDim = dim3(sms * kJoinGroups);
     c.blockDim = dim3(kJoinThreads);
     c.dynamicSmemBytes = 0;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a, sms);
+    const int64_t tiles = ((int64_t)a.T * a.group / kRows + a.B) * a.kv_heads;  // at most
+    if (tiles <= kFewTiles && sms <= kJoinMost) {
+        c.gridDim = dim3(sms * kJoinCtas);
+        return cudaLaunchKernelEx(&c, k_kv_join_few<H, D>, a, sms);
+    }
+    c.gridDim = dim3(sms, kJoinGroups);
+    return cudaLaunchKernelEx(&c, k_kv_join<H, D>, a);
 }
 template <bool Q>
 cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s) {
