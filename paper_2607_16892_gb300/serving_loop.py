@@ -8,10 +8,12 @@ then is
                       requests give theirs back; a request that finds no pages is refused and tries again
     kvdro_kv_append   the new tokens' keys and values, per layer
     kvdro_kv_attend   whole prompts and single tokens in one batch, per layer
+With ``bits=8`` the caches hold e4m3 codes (kvdro_kv_open8); with ``system`` tokens of instructions in front of every request,
+these are written once, into pages that no request holds, and kvdro_kv_attend_shared takes the place of the last call.
 There is no model here: queries, keys and values are seeded draws of a model's shapes.  The host reads back the
 lengths of a step (which requests were refused) and nothing else.
 
-    python -m paper_2607_16892_gb300.serving_loop --steps 200
+    python -m paper_2607_16892_gb300.serving_loop --steps 200 --bits 8 --system 700
 """
 
 from __future__ import annotations
@@ -42,8 +44,9 @@ def reservations(ctx, rng, rho: float, eps: float, prompts, samples_per_class: i
 
 def run(steps: int = 200, slots: int = 32, pages: int = 1200, page_size: int = 16, layers: int = 2, heads: int = 32,
         kv_heads: int = 8, head_dim: int = 128, prompts=(37, 200, 801), rho: float = 10.0, eps: float = 20.0, arrival: float = 0.3,
-        seed: int = 1, device: int = 0, watch=None) -> dict:
-    """Serve ``steps`` steps; returns counts.  ``watch(step, layer, state)`` sees each layer's tensors after its attention."""
+        seed: int = 1, device: int = 0, watch=None, bits: int = 16, system: int = 0) -> dict:
+    """Serve ``steps`` steps; returns counts.  ``watch(step, layer, state)`` sees each layer's tensors after its attention (step -1:
+    the keys and values of the instructions)."""
     import torch
 
     dev = torch.device("cuda", device)
@@ -55,9 +58,25 @@ def run(steps: int = 200, slots: int = 32, pages: int = 1200, page_size: int = 1
     i32 = dict(dtype=torch.int32, device=dev)
     try:
         reserve_of = reservations(ctx, rng, rho, eps, prompts)
-        shape = (pages, page_size, kv_heads, head_dim)
-        caches = [kv.kvdro_kv_open(ctx, torch.empty(shape, dtype=torch.bfloat16, device=dev),
-                                   torch.empty(shape, dtype=torch.bfloat16, device=dev)) for _ in range(layers)]
+        shared = -(-system // page_size)  # pages of the instructions, behind the requests'
+        shape = (pages + shared, page_size, kv_heads, head_dim)
+
+        def cache():
+            k, v = (torch.empty(shape, dtype=torch.bfloat16 if bits == 16 else torch.float8_e4m3fn, device=dev) for _ in "kv")
+            if bits == 16:
+                return kv.kvdro_kv_open(ctx, k, v)
+            exps = (torch.empty((shape[0], kv_heads, page_size), dtype=torch.uint8, device=dev) for _ in "kv")
+            return kv.kvdro_kv_open8(ctx, k, v, *exps, torch.bfloat16)
+
+        caches = [cache() for _ in range(layers)]
+        if system:
+            share_off, prefix_len = torch.tensor([0, slots], **i32), torch.tensor([system], **i32)
+            prefix_table = torch.arange(pages, pages + shared, **i32)[None]
+            for layer, c in enumerate(caches):
+                k, v = torch.randn((system, 2 * kv_heads, head_dim), generator=gen, device=dev, dtype=torch.bfloat16).chunk(2, dim=1)
+                kv.kvdro_kv_append(c, k, v, torch.arange(pages * page_size, pages * page_size + system, **i32), stream=stream)
+                if watch is not None:
+                    watch(-1, layer, {"k": k, "v": v})
         max_pages = -(-(max(prompts) + L_MAX) // page_size)
         table = torch.full((slots, max_pages), -1, **i32)
         ring = torch.randperm(pages, generator=gen, device=dev).to(torch.int32)
@@ -92,7 +111,11 @@ def run(steps: int = 200, slots: int = 32, pages: int = 1200, page_size: int = 1
                 q, k, v = qkv.split([heads, kv_heads, kv_heads], dim=1)
                 out = torch.empty((T, heads, head_dim), dtype=torch.bfloat16, device=dev)
                 kv.kvdro_kv_append(cache, k, v, slot, stream=stream)
-                kv.kvdro_kv_attend(cache, q, q_off, kv_len, table, out, max_q=int(new.max()), stream=stream)
+                if system:
+                    kv.kvdro_kv_attend_shared(cache, q, q_off, kv_len, table, share_off, prefix_len, prefix_table, out, max_q=int(new.max()),
+                                              stream=stream)
+                else:
+                    kv.kvdro_kv_attend(cache, q, q_off, kv_len, table, out, max_q=int(new.max()), stream=stream)
                 if watch is not None:
                     watch(step, layer, {"q": q, "k": k, "v": v, "out": out, "new": new, "cls": cls.copy(), "kv_len": kv_len, "pos": pos})
             got = kv_len.cpu().numpy()  # 0: refused, done or empty
@@ -124,8 +147,10 @@ def main():
     p.add_argument("--rho", type=float, default=10.0)
     p.add_argument("--eps", type=float, default=20.0)
     p.add_argument("--device", type=int, default=0)
+    p.add_argument("--bits", type=int, choices=(8, 16), default=16)
+    p.add_argument("--system", type=int, default=0)
     a = p.parse_args()
-    print(json.dumps(run(a.steps, a.slots, a.pages, rho=a.rho, eps=a.eps, device=a.device)))
+    print(json.dumps(run(a.steps, a.slots, a.pages, rho=a.rho, eps=a.eps, device=a.device, bits=a.bits, system=a.system)))
 
 
 if __name__ == "__main__":
