@@ -23,8 +23,12 @@ constexpr int32_t kMaxTokens = 1 << 30, kMaxPositions = 1 << 30, kMaxRows = 1 <<
 constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
 constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
 // Rows that share a key head, up to which the kernel for single tokens runs.  32 requests of 3000 positions, 8 key heads of 128:
-// 12 rows 77 us there; 20 to 32 rows 140 us there, 85 on the kernel for chunks; 64 rows 249 and 85.
+// 12 rows 77 us there; 20 to 32 rows 140 us there, 85 on the kernel for chunks; 64 rows 249 and 85.  8 bits, 4 key heads: 21 rows
+// 52 us there, 64 on the kernel for chunks; 28 rows 91 and 64.
 constexpr int64_t kFewRows = 16, kFewRows8 = 24;
+// Rows of a prefix on average, above which all prefixes run on the kernel for chunks.  A launch for those of few rows that finds none
+// costs 2 us (five prefixes behind 84 rows each: 62.8 us, 60.5 without it) to 9 (behind 378: 136 and 127).
+constexpr int64_t kManyRows = 64;
 
 int log2_of(int32_t v) {
     int s = 0;
@@ -607,7 +611,7 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     p.max_pages = prefix_pages;
     p.causal = false;
     Last before = Last::kNone;
-    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1, before, s)) return rc;
+    if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1 || (int64_t)T * a.group > kManyRows * G, before, s)) return rc;
     a.part = kvdro::Part::kJoin;
     if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, before, s)) return rc;
     return turn.end(ctx, s);

@@ -20,6 +20,13 @@
 // Caches of 8 bits (Q): codes become FP16, exactly, two to an instruction, as they leave shared memory, whatever the type of the
 // queries; BF16 queries become FP16 times a power of two per row.  A key's scale multiplies its scores.  A value's scale goes
 // into its weight, 2^(s + E - m_o), so O has a maximum of its own, that of s + E: nothing is lost whatever the scales' range.
+// V is transposed in pairs of columns, as 16-bit elements, and a byte permutation per register parts them.
+// Half the bytes leave half the time for as many positions, and what bounds such a kernel first is its own code: unrolled over 32
+// positions it took 1050 instructions a slice (70 us for the batch below), over 64 1700 and as long, warps waiting for instructions
+// more often than for data; the loop over 16 positions is rolled, 460 instructions with their share of a slice's, and the batch takes 61.  Copies without any
+// products take 57: rows of 128 bytes are the least that DRAM gives, and rows of 64 are read in pairs of heads.
+// Measured (8 bits): 64 requests of lognormal lengths up to 8192, 8 key heads of 128, 281 MB, 61 to 64 us from one GPU to the next = 4.6 to 4.4
+// TB/s; 4 requests of 131071, 16 heads of 64, 1090 MB, 183 to 205 us = 6.0 to 5.3 TB/s; one request of 1000, 12.8 us, all latency.
 #pragma once
 
 #include "kv_device.cuh"
@@ -41,9 +48,10 @@ struct Ring {  // a stage: K or V of a slice; 8 bits: both
     // D 64: 4 of 3 stages 41 us (window case), 3 of 4 stages 44, 2 of 6 stages 52.
     // 8 bits: keys and values of a slice together; of heads of 64, 64 positions (four requests of 131071: 215 us, 253 with 32).
     static constexpr int kSlice = Q && D == 64 ? 64 : 32;
-    static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? (Q ? 3 : 4) : 2);  // per SM
+    // Sixteen rows of 64: 3 CTAs of 2 stages 29.7 us (32 requests of 3000), 2 of 3 stages 31.5; of 128 3 CTAs spill, 47.4 us for 40.5.
+    static constexpr int kCtas = D == 128 ? (NR == 1 ? 3 : 2) : (NR == 1 ? (Q ? 3 : 4) : Q && NR == 2 ? 3 : 2);  // per SM
     static constexpr int kBytes = kSlice * D * 2;
-    static constexpr int kStages = D == 128 || Q ? (NR == 1 ? 2 : 3) : (NR == 1 ? 3 : 6);
+    static constexpr int kStages = D == 128 || Q ? (NR == 1 || (Q && D == 64 && NR == 2) ? 2 : 3) : (NR == 1 ? 3 : 6);
     static constexpr int kScales = Q ? kWarps * kStages * 2 * kSlice : 0;  // a byte per key and value, behind the ring
     // Queries in shared memory where they and the sums do not fit the registers (24 rows of 128, 32 requests of 3000: 78 us in registers, 52 so).
     static constexpr bool kHoldQ = Q && D == 128 && NR == 3;
