@@ -221,8 +221,8 @@ int kvdro_eval_grid_noalloc(int32_t K, const int64_t* offsets, const int32_t* le
  * that calls can be captured into a CUDA graph (after one call of the same kind outside a capture,
  * which loads its kernels).  A value in device memory that is out of range is never followed: the kernels leave
  * out what it stands for and the next kvdro_sync() returns KVDRO_ERANGE.
- * Calls on one context may use several streams: kvdro_kv_attend orders its scratch across
- * them itself, outside of captures (the launches of captured graphs that share a context must be ordered by
+ * Calls on one context may use several streams: kvdro_kv_attend and kvdro_kv_attend_shared order their scratch across
+ * them themselves, outside of captures (the launches of captured graphs that share a context must be ordered by
  * the caller); the caller orders everything else (his arrays) as for any kernel.
  */
 typedef struct kvdro_kv kvdro_kv;
@@ -360,7 +360,7 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
 int kvdro_kv_shared_bytes(int32_t T, int32_t n_heads, int32_t head_dim, size_t* bytes);
 
 /* Wait for the context's device work -- the streams of its last call outside the page cache and of its last page cache
- * call, and its last kvdro_kv_attend -- and report any asynchronous CUDA error, kernel timeout or value out
+ * call, and its last kvdro_kv_attend or kvdro_kv_attend_shared -- and report any asynchronous CUDA error, kernel timeout or value out
  * of range.  (Earlier page cache calls on yet other streams: what their kernels found is reported once they are
  * done.) */
 int kvdro_sync(kvdro_ctx* ctx);
