@@ -24,7 +24,8 @@ constexpr int32_t kMaxHeads = 4096, kMaxKvHeads = 1024;
 constexpr unsigned long long kWaitNs = 2000000000, kTestWaitNs = 1000000;
 // Rows that share a key head, up to which the kernel for single tokens runs.  32 requests of 3000 positions, 8 key heads of 128:
 // 12 rows 77 us there; 20 to 32 rows 140 us there, 85 on the kernel for chunks; 64 rows 249 and 85.  8 bits, 4 key heads: 21 rows
-// 52 us there, 64 on the kernel for chunks; 28 rows 91 and 64.
+// 52 us there, 64 on the kernel for chunks; 28 rows 91 and 64; but prefixes, which are few and long: 20 rows over 2048 in front of short requests
+// 30 us there, 25 on the kernel for chunks, 12 rows 23 and 24.5.
 constexpr int64_t kFewRows = 16, kFewRows8 = 24;
 // Rows of a prefix on average, above which all prefixes run on the kernel for chunks.  A launch for those of few rows that finds none
 // costs 2 us (five prefixes behind 84 rows each: 62.8 us, 60.5 without it) to 9 (behind 378: 136 and 127).
@@ -295,7 +296,7 @@ int launch_attend(kvdro_ctx* ctx, kvdro::AttendArgs a, const kvdro::KvMaps& maps
     float* const second = a.pieces + kvdro::kv_decode_piece_bytes(ctx->sms) / sizeof(float);
     // Few rows that share a key head run on the kernel for single tokens, many on the one for chunks; a batch that may hold
     // both runs on both, each request on its own.  What overlaps has scratch of its own.
-    if (most * a.group <= (a.k_exp ? kFewRows8 : kFewRows)) {
+    if (most * a.group <= (a.k_exp && a.part != kvdro::Part::kLeave ? kFewRows8 : kFewRows)) {
         if (before == Last::kFew) {
             a.pieces = second;
             a.tickets += kvdro::kv_decode_ctas(ctx->sms);
