@@ -341,7 +341,8 @@ int kvdro_kv_attend(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, int32_t
  * Attention of requests that share prefixes: requests share_off[g] .. share_off[g+1] - 1 stand behind the same prefix_len[g]
  * tokens, which live once in the pages prefix_table[g]; kv_len and table are about a request's own tokens alone (as kvdro_kv_plan gives
  * them).  A token sees what kvdro_kv_attend lets it see of its own tokens, and the whole prefix: the softmax runs over both.
- * Each prefix is read once for all of its requests' tokens, whose rows it makes one long request of.  Tokens of requests with
+ * A prefix is read once for all of its requests' tokens, whose rows it makes one long request of; where few requests stand behind short ones
+ * (prefix_pages says how long they may be) each reads its own, which is faster.  Tokens of requests with
  * kv_len 0 get out = 0 and lse = -infinity, prefix or not.  There is no sliding window.
  *   G            prefixes, 1 <= G <= B;  share_off: int32[G+1], ascending within [0, B]: requests in front of the first and
  *                behind the last have no prefix.

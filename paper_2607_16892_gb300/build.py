@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libkvdro.so")
 SOURCES = ["api.cu", "setup.cu", "sort.cu", "grid.cu", "dual.cu", "noalloc.cu",
-           "kv_api.cu", "kv_pages.cu", "kv_decode.cu", "kv_decode8.cu", "kv_chunk.cu", "kv_chunk8.cu"]
+           "kv_api.cu", "kv_pages.cu", "kv_decode.cu", "kv_decode8.cu", "kv_direct.cu",
+           "kv_direct8.cu", "kv_chunk.cu", "kv_chunk8.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -100,6 +100,9 @@ struct AttendArgs {
     // the caller's `share_n`, and leaves its sums; one over the requests' own pages joins those with its own.
     const int32_t* share_off;
     int32_t share_n;
+    // Prefixes read by each of their requests, in front of its own tokens: as the call gives them.
+    const int32_t *pre_off, *pre_len, *pre_table;
+    int32_t pre_n, pre_pages;
     Part part;
     float* sums;         // [T][heads][head_dim]
     float2* sum_ml;      // [T][heads]: maximum (in log2) and sum of weights
@@ -113,6 +116,11 @@ cudaError_t kv_decode_prepare();
 // `rows`: that share a key head, at most (more are right, but slow).  `early`: may start while the launch before it, whose sums it
 // joins, ends.
 cudaError_t kv_decode8_prepare();
+cudaError_t kv_direct_prepare();
+cudaError_t kv_direct8_prepare();
+// The same with a's prefixes in front of the requests' own tokens, up to sixteen rows.
+cudaError_t launch_kv_direct(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
+cudaError_t launch_kv_direct8(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
 cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);

@@ -31,6 +31,11 @@ constexpr int64_t kFewRows = 16, kFewRows8 = 24;
 // costs 2 us (five prefixes behind 84 rows each: 62.8 us, 60.5 without it) to 9 (behind 378: 136 and 127).
 constexpr int64_t kManyRows = 64;
 
+// Elements of keys that a call's requests read of their prefixes, had these all the pages of their table rows, up to which each of few
+// rows reads its own, out of L2, in one launch.  Single tokens with 200 of their own, 8 key heads of 128, one by one and once for all: 6 behind 2048
+// 16.7 and 23.9 us (8 bits: 17.1 and 27.2); 16 behind 2048, this many, 22.9 and 24.6 (23.3 and 27.6); 32 behind 2048 31.3 and 26.2.
+constexpr int64_t kDirectElements = 32 << 20;
+
 int log2_of(int32_t v) {
     int s = 0;
     while ((1 << s) < v) s++;
@@ -134,6 +139,8 @@ int prepare_attend(kvdro_ctx* ctx) {
     if (ctx->kv_ready) return KVDRO_OK;
     KV_CUDA(kvdro::kv_decode_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_decode8_prepare(), "preparing the attention kernels");
+    KV_CUDA(kvdro::kv_direct_prepare(), "preparing the attention kernels");
+    KV_CUDA(kvdro::kv_direct8_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_chunk_prepare(), "preparing the attention kernels");
     KV_CUDA(kvdro::kv_chunk8_prepare(), "preparing the attention kernels");
     if (!ctx->kv_done) KV_CUDA(cudaEventCreateWithFlags(&ctx->kv_done, cudaEventDisableTiming), "creating an event");
@@ -278,6 +285,8 @@ int attend_args(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, const void*
     a.head_shift = kv->k_exp && kv->head_dim == 64 && kv->heads % 2 == 0 ? 1 : 0;
     a.share_off = nullptr;
     a.share_n = 0;
+    a.pre_off = a.pre_len = a.pre_table = nullptr;
+    a.pre_n = a.pre_pages = 0;
     a.part = kvdro::Part::kWhole;
     a.sums = nullptr;
     a.sum_ml = nullptr;
@@ -599,6 +608,17 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     ctx->kv_last = s;
     ScratchTurn turn;
     if (int rc = turn.begin(ctx, s)) return rc;
+    const int64_t most = most_tokens(max_q, B, T);
+    const int64_t each = (int64_t)prefix_pages * kv->page_size;  // positions, below 2^31
+    if (most * a.group <= kFewRows && each <= kDirectElements && B * each * (kv->heads * kv->head_dim) <= kDirectElements) {
+        a.pre_off = share_off;
+        a.pre_len = prefix_len;
+        a.pre_table = prefix_table;
+        a.pre_n = G;
+        a.pre_pages = prefix_pages;
+        KV_CUDA((kv->k_exp ? kvdro::launch_kv_direct8 : kvdro::launch_kv_direct)(a, kv->maps, (int)(most * a.group), ctx->sms, s), "attention kernel");
+        return turn.end(ctx, s);
+    }
     a.sums = static_cast<float*>(work);
     a.sum_ml = reinterpret_cast<float2*>(a.sums + (int64_t)T * n_heads * kv->head_dim);
     // The prefixes, each a request of all its requests' tokens, every one of which sees all of it.
@@ -614,7 +634,7 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     Last before = Last::kNone;
     if (int rc = launch_attend(ctx, p, kv->maps, T, G == 1 || (int64_t)T * a.group > kManyRows * G, before, s)) return rc;
     a.part = kvdro::Part::kJoin;
-    if (int rc = launch_attend(ctx, a, kv->maps, most_tokens(max_q, B, T), max_q > 0 && (int64_t)max_q * B == T, before, s)) return rc;
+    if (int rc = launch_attend(ctx, a, kv->maps, most, max_q > 0 && (int64_t)max_q * B == T, before, s)) return rc;
     return turn.end(ctx, s);
 }
 

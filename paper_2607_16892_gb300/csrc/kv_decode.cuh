@@ -27,6 +27,9 @@
 // products take 57: rows of 128 bytes are the least that DRAM gives, and rows of 64 are read in pairs of heads.
 // Measured (8 bits): 64 requests of lognormal lengths up to 8192, 8 key heads of 128, 281 MB, 61 to 64 us from one GPU to the next = 4.6 to 4.4
 // TB/s; 4 requests of 131071, 16 heads of 64, 1090 MB, 183 to 205 us = 6.0 to 5.3 TB/s; one request of 1000, 12.8 us, all latency.
+//
+// With prefixes in front (S) a request's line of blocks begins with its prefix's, and pages are looked up in the one table or the other:
+// what it costs to read a short prefix once per request out of L2 is less than the launches that read it once for all.
 #pragma once
 
 #include "kv_device.cuh"
@@ -107,14 +110,14 @@ __device__ __forceinline__ uint32_t load_u8(uint32_t at) {
 }
 
 // NR: groups of eight rows of a tile.
-template <bool H, int D, int NR, bool Q>
+template <bool H, int D, int NR, bool Q, bool S>
 __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     k_kv_decode(const AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ __align__(16) char s_raw[];  // 64-bit words of the search first
     constexpr int kSlice = Ring<D, NR, Q>::kSlice, kKeys = kSlice * kWarps;
     constexpr int kStages = Ring<D, NR, Q>::kStages, kStage = Ring<D, NR, Q>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
-    using DecodeLine = Line<kRows, kKeys, kSlice, kOver, Q && NR == 1>;
+    using DecodeLine = Line<kRows, kKeys, kSlice, kOver, Q && NR == 1, S>;
     constexpr bool F16 = H || Q;  // the type of the products
     // Where column c of row r of the sums stands in shared memory, without bank conflicts.
     auto sum_at = [](int r, int c) { return Q ? r * D + (c ^ (r >> 1 & 3) << 3) : r * (D + 4) + c; };
@@ -174,7 +177,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
         for (int i = 0; i < NP; i++) {
             pg[i] = -1;
-            if (j + 16 * i < in.at.t.hi && ((j + 16 * i) | (slots - 1)) >= seen_lo) {  // else no row's business
+            if (S && j < 0) {
+                const int at = j + 16 * i + in.at.r.pad;
+                if (at < in.at.r.pre) {
+                    const int page = a.pre_table[(int64_t)in.at.r.prefix * a.pre_pages + (at >> a.page_shift)];
+                    if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
+                    else range = true;
+                }
+            } else if (j + 16 * i < in.at.t.hi && ((j + 16 * i) | (slots - 1)) >= seen_lo) {  // else no row's business
                 const int page = a.table[(int64_t)in.at.b * a.max_pages + ((j + 16 * i) >> a.page_shift)];
                 if ((uint32_t)page < (uint32_t)a.n_pages) pg[i] = page;
                 else range = true;
@@ -270,6 +280,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     float up[NR][2], upo[NR][2];   // 8 bits: m and mo are raised above this
     int2 see[NR][2];
     int2 all_see, any_see;  // positions that every row of the tile sees, and that some row does
+    int none = 0;           // S: from here to 0 there are no positions
     bool dead = false;
     int stage = 0;
 
@@ -360,16 +371,17 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             const int2 s0 = line.seen(at.r, line.token(first)), s1 = line.seen(at.r, line.token(first + rows - 1));
             all_see = make_int2(s1.x, s0.y);
             any_see = make_int2(s0.x, s1.y);
+            if constexpr (S) none = at.r.pre - at.r.pad;
             if constexpr (kHoldQ) __syncthreads();
         }
         for (int blk = w.p0; blk < w.p1; blk++) {
         const int j0 = at.t.lo + blk * line.keys() + my_slice;
         if constexpr (Q) {
             const uint32_t gap = gaps >> NP * stage & kAllGaps;
-            const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || gap;
+            const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || gap || (S && j0 < 0 && j0 + kSlice > none);
             if (ready()) {
                 const uint32_t kt = ring + stage * kStage, vt = kt + kSlice * D, ke = scales + stage * 2 * kSlice + (lane >> 2), ve = ke + kSlice;
-                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y; };
+                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y && !(S && j >= none && j < 0); };
                 bool odd = false;  // a value that some rows see and others do not is NaN
                 if (edge && (any_see.x != all_see.x || any_see.y != all_see.y)) {
 #pragma unroll 1
@@ -427,7 +439,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                             const int j = j0 + 16 * t + (lane >> 2);
 #pragma unroll
                             for (int i = 0; i < 4; i++)
-                                if (j + 8 * (i >> 1) < see[n][i & 1].x || j + 8 * (i >> 1) >= see[n][i & 1].y || (gap >> t & 1)) s[n][i] = -INFINITY;
+                                if (j + 8 * (i >> 1) < see[n][i & 1].x || j + 8 * (i >> 1) >= see[n][i & 1].y || (gap >> t & 1) ||
+                                    (S && j + 8 * (i >> 1) >= none && j + 8 * (i >> 1) < 0))
+                                    s[n][i] = -INFINITY;
                         }
 #pragma unroll
                         for (int i = 0; i < 2; i++) {
@@ -511,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
                                 for (int i = 0; i < 2; i++) {
                                     w[i] = __shfl_sync(~0u, k & 8 ? s[n][2 + i] : s[n][i], from);
-                                    see_k[i] = j >= see[n][i].x && j < see[n][i].y && !(gap >> t & 1);
+                                    see_k[i] = j >= see[n][i].x && j < see[n][i].y && !(gap >> t & 1) && !(S && j >= none && j < 0);
                                 }
 #pragma unroll
                                 for (int d = 0; d < 2 * DT; d++) {
@@ -533,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                 advance();
             }
         } else {
-        const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || (gaps >> 2 * stage & 3);
+        const bool edge = j0 < all_see.x || j0 + kSlice > all_see.y || (gaps >> 2 * stage & 3) || (S && j0 < 0 && j0 + kSlice > none);
         const uint32_t gap = gaps >> 2 * stage & 3;
         float s[NR][MT][4];  // scores, then weights: position 16 t + (lane >> 2) + 8 (i >> 1), row 8 n + 2 (lane & 3) + (i & 1)
         const bool some = ready();
@@ -572,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         x = score(x, mul, cap2);
                         if (edge) {
                             const int j = j0 + 16 * t + (lane >> 2) + 8 * (i >> 1);
-                            if (j < see[n][i & 1].x || j >= see[n][i & 1].y || (gap >> t & 1)) x = -INFINITY;
+                            if (j < see[n][i & 1].x || j >= see[n][i & 1].y || (gap >> t & 1) || (S && j >= none && j < 0)) x = -INFINITY;
                         }
                         top[n][i & 1] = fmaxf(top[n][i & 1], x);
                     }
@@ -619,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             uint32_t keep[MT][2];
             bool odd = false;
             if (edge) {
-                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y; };
+                auto seen = [&](int j) { return j >= any_see.x && j < any_see.y && !(S && j >= none && j < 0); };
 #pragma unroll
                 for (int t = 0; t < MT; t++)
 #pragma unroll
@@ -669,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         for (int i = 0; i < 2; i++) {
                             const float x = k & 16 ? (k & 8 ? s[n][1][2 + i] : s[n][1][i]) : (k & 8 ? s[n][0][2 + i] : s[n][0][i]);
                             w[i] = __shfl_sync(~0u, x, from);
-                            see_k[i] = j0 + k >= see[n][i].x && j0 + k < see[n][i].y && !(gap >> (k >> 4) & 1);
+                            see_k[i] = j0 + k >= see[n][i].x && j0 + k < see[n][i].y && !(gap >> (k >> 4) & 1) && !(S && j0 + k >= none && j0 + k < 0);
                         }
 #pragma unroll
                         for (int d = 0; d < 2 * DT; d++) {
@@ -852,26 +866,26 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     if (__any_sync(~0u, range || line.bad) && lane == 0) atomicOr(a.err, kKvErrRange);
 }
 
-template <bool H, int D, int NR, bool Q>
+template <bool H, int D, int NR, bool Q, bool S>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(k_kv_decode<H, D, NR, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NR, Q>::kSmem);
+    return cudaFuncSetAttribute(k_kv_decode<H, D, NR, Q, S>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NR, Q>::kSmem);
 }
-template <bool H, int D, bool Q>
+template <bool H, int D, bool Q, bool S>
 cudaError_t prepare() {
-    cudaError_t e = prepare<H, D, 1, Q>();
-    if (e == cudaSuccess) e = prepare<H, D, 2, Q>();
-    if constexpr (Q)
-        if (e == cudaSuccess) e = prepare<H, D, 3, Q>();
+    cudaError_t e = prepare<H, D, 1, Q, S>();
+    if (e == cudaSuccess) e = prepare<H, D, 2, Q, S>();
+    if constexpr (Q && !S)
+        if (e == cudaSuccess) e = prepare<H, D, 3, Q, S>();
     return e;
 }
-template <bool Q>
+template <bool Q, bool S>
 cudaError_t prepare_all() {
-    for (cudaError_t e : {prepare<false, 64, Q>(), prepare<true, 64, Q>(), prepare<false, 128, Q>(), prepare<true, 128, Q>()})
+    for (cudaError_t e : {prepare<false, 64, Q, S>(), prepare<true, 64, Q, S>(), prepare<false, 128, Q, S>(), prepare<true, 128, Q, S>()})
         if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
 
-template <bool H, int D, int NR, bool Q>
+template <bool H, int D, int NR, bool Q, bool S>
 cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool early, int sms, cudaStream_t s) {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -883,19 +897,20 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool early, int sms,
     c.stream = s;
     c.attrs = at;
     c.numAttrs = early ? 1 : 0;
-    return cudaLaunchKernelEx(&c, k_kv_decode<H, D, NR, Q>, a, maps.k_slice, maps.v_slice);
+    return cudaLaunchKernelEx(&c, k_kv_decode<H, D, NR, Q, S>, a, maps.k_slice, maps.v_slice);
 }
-template <bool H, int D, bool Q>
+template <bool H, int D, bool Q, bool S>
 cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
-    if (rows <= 8) return launch<H, D, 1, Q>(a, maps, early, sms, s);
-    if constexpr (Q)
-        if (rows > 16) return launch<H, D, 3, Q>(a, maps, early, sms, s);
-    return launch<H, D, 2, Q>(a, maps, early, sms, s);
+    if (rows <= 8) return launch<H, D, 1, Q, S>(a, maps, early, sms, s);
+    if constexpr (Q && !S)
+        if (rows > 16) return launch<H, D, 3, Q, S>(a, maps, early, sms, s);
+    return launch<H, D, 2, Q, S>(a, maps, early, sms, s);
 }
-template <bool Q>
+template <bool Q, bool S>
 cudaError_t launch_any(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
-    if (a.half) return a.head_dim == 128 ? launch<true, 128, Q>(a, maps, rows, early, sms, s) : launch<true, 64, Q>(a, maps, rows, early, sms, s);
-    return a.head_dim == 128 ? launch<false, 128, Q>(a, maps, rows, early, sms, s) : launch<false, 64, Q>(a, maps, rows, early, sms, s);
+    if (a.half)
+        return a.head_dim == 128 ? launch<true, 128, Q, S>(a, maps, rows, early, sms, s) : launch<true, 64, Q, S>(a, maps, rows, early, sms, s);
+    return a.head_dim == 128 ? launch<false, 128, Q, S>(a, maps, rows, early, sms, s) : launch<false, 64, Q, S>(a, maps, rows, early, sms, s);
 }
 
 }  // namespace

@@ -3,10 +3,10 @@
 
 namespace kvdro {
 
-cudaError_t kv_decode8_prepare() { return prepare_all<true>(); }
+cudaError_t kv_decode8_prepare() { return prepare_all<true, false>(); }
 
 cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
-    return launch_any<true>(a, maps, rows, early, sms, s);
+    return launch_any<true, false>(a, maps, rows, early, sms, s);
 }
 
 }  // namespace kvdro

@@ -147,6 +147,7 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 // A tile that crosses from one stretch into the next is joined from its pieces.
 struct Request {
     int q0, n, rows, kv;  // first token, tokens, rows (tokens inside T times the group; 0: no positions, or not this launch's), positions
+    int pre, pad, prefix;  // positions of the prefix in front, padded to blocks, and which it is
 };
 
 struct Tile {
@@ -154,7 +155,9 @@ struct Tile {
 };
 
 // kHeads: a tile may be of 2^a.head_shift key heads, whose blocks then have that much fewer positions.
-template <int kRowsOf, int kKeysOf, int kAlign, int kOverOf, bool kHeads = false>
+// kPre: a's prefixes stand in front of their requests' own positions, at -pad .. -pad + pre - 1; what is between them and 0 is no
+// position.  Blocks, slices and pages begin at multiples of their sizes on both sides of 0.
+template <int kRowsOf, int kKeysOf, int kAlign, int kOverOf, bool kHeads = false, bool kPre = false>
 struct Line {
     static constexpr int kRows = kRowsOf, kKeys = kKeysOf, kOver = kOverOf;
     const AttendArgs& a;
@@ -171,6 +174,7 @@ struct Line {
     __device__ __forceinline__ int token(int row) const { return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift); }
     __device__ __forceinline__ Request request(int b) {
         Request r;
+        r.pre = r.pad = r.prefix = 0;
         int b0 = b, b1 = b + 1;
         if (a.share_off) {
             b0 = a.share_off[b];
@@ -195,12 +199,33 @@ struct Line {
             r.kv = 0;
         }
         r.rows = r.kv > 0 && r.n > a.min_q && r.n <= a.max_q ? max(0, min(q1, a.T) - r.q0) * a.group : 0;
+        if constexpr (kPre) {
+            int lo = 0, hi = a.pre_n;  // the first prefix whose requests end behind b
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (a.pre_off[mid + 1] > b) hi = mid;
+                else lo = mid + 1;
+            }
+            if (lo < a.pre_n && a.pre_off[lo] <= b) {
+                r.prefix = lo;
+                r.pre = prefix(lo);
+                r.pad = blocks(r.pre) * keys();
+            }
+        }
         return r;
+    }
+    // Positions of prefix g; 0, and bad, if its bounds or its length are out of range.
+    __device__ __forceinline__ int prefix(int g) {
+        const int b0 = a.pre_off[g], b1 = a.pre_off[g + 1], n = a.pre_len[g];
+        if (b0 >= 0 && b1 >= b0 && b1 <= a.B && n >= 0 && (int64_t)n <= ((int64_t)a.pre_pages << a.page_shift)) return n;
+        bad = true;
+        return 0;
     }
     // Visible positions [lo, hi) of token i of a request.
     __device__ __forceinline__ int2 seen(const Request& r, int i) const {
         const int p = r.kv - r.n + i;  // kv and n are below 2^31, not negative
         const int hi = a.causal ? min(max(p + 1, 0), r.kv) : r.kv;
+        if constexpr (kPre) return make_int2(-r.pad, hi);
         const int lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
         return make_int2(min(lo, hi), hi);
     }
@@ -461,6 +486,7 @@ template <int D, int kThreads, class L>
 __device__ __forceinline__ void clear_rest(L& line) {
     const AttendArgs& a = line.a;
     if (a.part == Part::kLeave) return clear_parts<kThreads>(line);
+    for (int g = blockIdx.x; g < a.pre_n; g += gridDim.x) line.prefix(g);  // what is out of range is reported
     auto clear = [&](int t0, int t1, int from, int step) {
         const int64_t vecs = (int64_t)(t1 - t0) * a.heads * (D / 8);
         for (int64_t i = (int64_t)from * kThreads + threadIdx.x; i < vecs; i += (int64_t)step * kThreads) {

@@ -1,0 +1,12 @@
+// The kernel for few rows, with prefixes in front of the requests' own tokens, on caches of 8 bits.
+#include "kv_decode.cuh"
+
+namespace kvdro {
+
+cudaError_t kv_direct8_prepare() { return prepare_all<true, true>(); }
+
+cudaError_t launch_kv_direct8(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s) {
+    return launch_any<true, true>(a, maps, rows, false, sms, s);
+}
+
+}  // namespace kvdro

@@ -99,9 +99,10 @@ class Case8(Case):
 
 class Shared:
     """Requests with prefixes: ``share`` bounds the requests of each of ``prefixes`` (lengths).  The prefixes are further rows of
-    the case's table, of no new tokens; ``check`` compares with each request's own case behind its prefix."""
+    the case's table, of no new tokens; ``check`` compares with each request's own case behind its prefix.  ``wide``: the prefixes' table has
+    room for so many pages that each prefix is read once for all of its requests, however few they are."""
 
-    def __init__(self, lens, share, prefixes, bits=16, **kw):
+    def __init__(self, lens, share, prefixes, bits=16, wide=False, **kw):
         self.base = (Case8 if bits == 8 else Case)(lens + [(0, n) for n in prefixes], **kw)
         c, B, G = self.base, len(lens), len(prefixes)
         self.c, self.lens, self.B, self.G, self.share = c, lens, B, G, share
@@ -110,6 +111,9 @@ class Shared:
         self.share_off, self.prefix_len = torch.tensor(share, **i32), torch.tensor(prefixes, **i32)
         self.q_off, self.kv_len = c.q_off[:B + 1].contiguous(), c.kv_len[:B].contiguous()
         self.table, self.prefix_table = c.table[:B].contiguous(), c.table[B:].contiguous()
+        if wide:
+            pages = (32 << 20) // (B * c.page * c.Hkv * c.D) + 1
+            self.prefix_table = torch.nn.functional.pad(self.prefix_table, (0, max(0, pages - self.prefix_table.shape[1])), value=-1)
 
     def whole(self):
         """The requests as ``Case.check`` takes them, their prefixes in front.  A (causal) token in front of position 0 sees its prefix

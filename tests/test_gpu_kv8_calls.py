@@ -20,11 +20,11 @@ def ctx():
 
 
 @pytest.mark.parametrize("skip", [0, 1, 2, 5])
-@pytest.mark.parametrize("kind", ["decode", "chunk", "both", "shared"])
+@pytest.mark.parametrize("kind", ["decode", "chunk", "both", "shared", "each"])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(monkeypatch, ctx, kind, skip):
     """Every CTA leaves one copy out, so nothing completes its barrier, and the bounded wait for it (1 ms under the hook) gives up."""
-    if kind == "shared":
-        case = Shared([(1, 9000)] * 40, [0, 40], [20000], bits=8, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=1)
+    if kind in ("shared", "each"):
+        case = Shared([(1, 9000)] * 40, [0, 40], [20000 if kind == "shared" else 3000], bits=8, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=1)
     else:
         case = Case8({"decode": [(1, 9000)] * 40, "chunk": [(300, 4000)] * 6, "both": [(1, 9000)] * 20 + [(300, 4000)] * 4}[kind], "bf16", 128,
                      8, 2, 16, seed=1)
@@ -40,7 +40,7 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(monkeypatch
         kvdro.kvdro_sync(broken)
     finally:
         kvdro.kvdro_destroy(broken)
-    if kind == "shared":
+    if kind in ("shared", "each"):
         case.check(*case.run(ctx))
     else:
         case.check(*case.run(ctx), only={0, len(case.lens) - 1})
@@ -136,11 +136,12 @@ def test_many_prefixes(ctx):
     share = np.sort(rng.integers(0, 501, 301)).tolist()
     prefixes = [int(x) for x in rng.integers(0, 90, 300)]
     for bits in (16, 8):
-        s = Shared(lens, share, prefixes, bits=bits, dtype="bf16", D=64, Hq=4, Hkv=2, page=16, seed=4)
-        out, lse = s.run(ctx)
-        whole = s.whole()
-        type(s.c).check(whole, out, lse, only=set(range(0, len(whole.lens), 17)))
-        kvdro.kvdro_sync(ctx)
+        for wide in (False, True):
+            s = Shared(lens, share, prefixes, bits=bits, wide=wide, dtype="bf16", D=64, Hq=4, Hkv=2, page=16, seed=4)
+            out, lse = s.run(ctx)
+            whole = s.whole()
+            type(s.c).check(whole, out, lse, only=set(range(0, len(whole.lens), 17)))
+            kvdro.kvdro_sync(ctx)
 
 
 def test_offsets_past_32_bits(ctx):

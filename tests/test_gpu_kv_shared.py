@@ -26,12 +26,13 @@ def ctx():
     kvdro.kvdro_destroy(c)
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("case", [ONE, FEW, MANY, GROUPS, NONE, CHUNKS], ids=["one", "few", "many", "groups", "none", "chunks"])
 @pytest.mark.parametrize("dtype,D,Hq,Hkv,page,layout", [("bf16", 128, 8, 2, 16, "dense"), ("fp16", 64, 14, 2, 32, "packed"),
                                                         ("bf16", 64, 4, 4, 128, "heads_first"), ("fp16", 128, 20, 1, 64, "dense")])
-def test_prefixes_and_own_tokens(ctx, bits, case, dtype, D, Hq, Hkv, page, layout):
-    s = Shared(*case, bits=bits, dtype=dtype, D=D, Hq=Hq, Hkv=Hkv, page=page, layout=layout, seed=D + Hq)
+def test_prefixes_and_own_tokens(ctx, wide, bits, case, dtype, D, Hq, Hkv, page, layout):
+    s = Shared(*case, bits=bits, wide=wide, dtype=dtype, D=D, Hq=Hq, Hkv=Hkv, page=page, layout=layout, seed=D + Hq)
     a, b = s.run(ctx), s.run(ctx)
     kvdro.kvdro_sync(ctx)
     s.check(*a)
@@ -40,12 +41,13 @@ def test_prefixes_and_own_tokens(ctx, bits, case, dtype, D, Hq, Hkv, page, layou
 
 @pytest.mark.parametrize("opt", [dict(causal=False), dict(softcap=30.0), dict(softcap=0.5), dict(scale=0.3), dict(scale=-0.1), dict(scale=0.0)],
                          ids=lambda o: "-".join(f"{k}{v}" for k, v in o.items()))
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
-def test_masks_caps_and_scales(ctx, bits, opt):
+def test_masks_caps_and_scales(ctx, wide, bits, opt):
     for case in (ONE, GROUPS, CHUNKS):
         if opt.get("causal") is False:  # whole() has no rows in front of position 0
             case = ([(min(q, kv), kv) for q, kv in case[0]], *case[1:])
-        s = Shared(*case, bits=bits, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=11)
+        s = Shared(*case, bits=bits, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=11)
         s.check(*s.run(ctx, **opt), **opt)
         kvdro.kvdro_sync(ctx)
 
@@ -65,41 +67,73 @@ def test_long_prefixes_are_split_and_joined(ctx, bits):
 @pytest.mark.parametrize("side", ["prefix", "own"])
 def test_one_side_has_all_the_weight(ctx, bits, side):
     """Scores hundreds apart between the prefix and the request's own tokens."""
-    s = Shared([(1, 100), (1, 40), (50, 60)], [0, 3], [300], bits=bits, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=5)
-    for b in range(4):
-        if (b == 3) == (side == "prefix"):
-            s.c.keys[b] = (s.c.keys[b] * 60).to(s.c.dt)
-            s.c.set(b, s.c.keys[b], s.c.values[b].to(s.c.dt))
+    for wide in (False, True):
+        for q in (1, 50):
+            s = Shared([(1, 100), (1, 40), (q, 60)], [0, 3], [300], bits=bits, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=5)
+            for b in range(4):
+                if (b == 3) == (side == "prefix"):
+                    s.c.keys[b] = (s.c.keys[b] * 60).to(s.c.dt)
+                    s.c.set(b, s.c.keys[b], s.c.values[b].to(s.c.dt))
+            s.check(*s.run(ctx))
+            kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_whatever_max_q_says(ctx, wide):
+    for bits in (16, 8):
+        s = Shared(*GROUPS, bits=bits, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
+        for max_q in (0, 1, 3, 130, 5000):
+            s.check(*s.run(ctx, max_q=max_q))
+            kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 128), (64, 32)])
+def test_prefixes_that_end_anywhere(ctx, bits, D, page):
+    """Around the ends of pages, slices and blocks, where each request reads its own; pages behind the end are none, and hold NaN."""
+    lengths = [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 0]
+    lens = [(1 + i % 2, 1 + 37 * i % 300) for i in range(2 * len(lengths) + 2)]
+    s = Shared(lens, list(range(0, 2 * len(lengths) + 1, 2)), lengths, bits=bits, dtype="fp16", D=D, Hq=8, Hkv=2, page=page, seed=12)
     s.check(*s.run(ctx))
     kvdro.kvdro_sync(ctx)
 
 
-def test_whatever_max_q_says(ctx):
-    s = Shared(*GROUPS, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
-    for max_q in (0, 1, 130, 5000):
-        s.check(*s.run(ctx, max_q=max_q))
+@pytest.mark.parametrize("bits", [16, 8])
+def test_values_of_nan_in_own_tokens_that_some_rows_see(ctx, bits):
+    """A row that does not see them is as if they were not there, its prefix beside them."""
+    make = lambda wide: Shared([(4, 200), (1, 9)], [0, 2], [77], bits=bits, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=13)  # noqa: E731
+    for wide in (False, True):
+        s, clean = make(wide), make(wide)
+        v = s.c.values[0].to(s.c.dt)
+        v[199, :, ::7] = float("nan")
+        s.c.set(0, s.c.keys[0].to(s.c.dt), v)
+        (out, lse), (want, wz) = s.run(ctx), clean.run(ctx)
         kvdro.kvdro_sync(ctx)
+        assert torch.isnan(out[3][:, ::7]).all() and torch.isfinite(out[:3]).all() and torch.isfinite(out[4]).all()
+        out[3], lse[3] = want[3], wz[3]
+        clean.check(out, lse)
 
 
 def test_nan_in_the_scratch_does_not_matter(ctx):
     for case in (GROUPS, NONE, ONE):
-        s = Shared(*case, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=7)
+        s = Shared(*case, wide=True, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=7)
         work = torch.full((kvdro.kvdro_kv_shared_bytes(s.T, 8, 128) // 4,), float("nan"), dtype=torch.float32, device="cuda")
         s.check(*s.run(ctx, work=work))
         kvdro.kvdro_sync(ctx)
 
 
-def test_bounds_out_of_range_are_reported(ctx):
+@pytest.mark.parametrize("wide", [False, True])
+def test_bounds_out_of_range_are_reported(ctx, wide):
     i32 = dict(dtype=torch.int32, device="cuda")
     for share, lengths in (([0, 5, 3, 4], [300] * 3), ([-1, 2, 3, 4], [300] * 3), ([0, 1, 2, 9], [300] * 3), ([0, 1, 2, 4], [300, -7, 300]),
-                           ([0, 1, 2, 4], [300, 10 ** 6, 300])):
-        s = Shared(ONE[0], [0, 1, 2, 4], [300] * 3, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
+                           ([0, 1, 2, 4], [300, 10 ** 9, 300])):
+        s = Shared(ONE[0], [0, 1, 2, 4], [300] * 3, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
         s.share_off, s.prefix_len = torch.tensor(share, **i32), torch.tensor(lengths, **i32)
         s.run(ctx)
         with pytest.raises(kvdro.KvdroError) as e:
             kvdro.kvdro_sync(ctx)
         assert e.value.status == kvdro.KVDRO_ERANGE
-    s = Shared(*ONE, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
+    s = Shared(*ONE, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=6)
     s.prefix_table[0, 3] = -1
     out, _ = s.run(ctx)
     with pytest.raises(kvdro.KvdroError) as e:
@@ -108,9 +142,10 @@ def test_bounds_out_of_range_are_reported(ctx):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-def test_captured_and_replayed(ctx, bits):
+@pytest.mark.parametrize("case,wide", [(GROUPS, True), (ONE, True), (ONE, False)], ids=["groups", "once", "each"])
+def test_captured_and_replayed(ctx, bits, case, wide):
     """New queries and lengths in the same arrays; a workspace of its own for the graph."""
-    s = Shared(*GROUPS, bits=bits, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=8)
+    s = Shared(*case, bits=bits, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=8)
     s.run(ctx)  # loads the kernels
     cache, work = s.open(ctx), torch.empty(kvdro.kvdro_kv_shared_bytes(s.T, 8, 128), dtype=torch.uint8, device="cuda")
     graph = torch.cuda.CUDAGraph()
