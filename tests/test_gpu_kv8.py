@@ -194,12 +194,13 @@ def test_tokens_of_very_different_sizes(ctx, q, dtype, spread):
     check(ctx, case)
 
 
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 16), ("fp16", 64, 64), ("fp16", 128, 32), ("bf16", 64, 16)])
 @pytest.mark.parametrize("where", ["future", "window"])
 @pytest.mark.parametrize("q", [1, 2, 5, 40, 300])
-def test_what_a_row_does_not_see_does_not_matter(ctx, where, q):
+def test_what_a_row_does_not_see_does_not_matter(ctx, where, q, dtype, D, page):
     """Keys and values of NaN at a position that some rows of a request see and others do not."""
     kv, opt = 700, dict(window=200) if where == "window" else {}
-    make = lambda: Case8([(q, kv), (1, 90)], "bf16", 128, 8, 2, 16, seed=q)  # noqa: E731
+    make = lambda: Case8([(q, kv), (1, 90)], dtype, D, 8, 2, page, seed=q)  # noqa: E731
     case, clean = make(), make()
     k, v = case.keys[0].to(case.dt), case.values[0].to(case.dt)
     at = kv - 1 if where == "future" else kv - q - 199 - 1 + (1 if q > 1 else 0)
@@ -213,7 +214,7 @@ def test_what_a_row_does_not_see_does_not_matter(ctx, where, q):
     assert torch.isfinite(out[~sees]).all()
     clean.check(torch.where(sees[:, None, None], want, out), torch.where(sees[:, None], wz, lse), **opt)
     assert torch.isnan(out[sees][..., ::7]).all()
-    rest = torch.ones(128, dtype=torch.bool)
+    rest = torch.ones(D, dtype=torch.bool)
     rest[::7] = False
     assert torch.isfinite(out[sees][..., rest]).all()
 
