@@ -118,7 +118,7 @@ cudaError_t kv_decode_prepare();
 cudaError_t kv_decode8_prepare();
 cudaError_t kv_direct_prepare();
 cudaError_t kv_direct8_prepare();
-// The same with a's prefixes in front of the requests' own tokens, up to sixteen rows.
+// The same with a's prefixes in front of the requests' own tokens.
 cudaError_t launch_kv_direct(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
 cudaError_t launch_kv_direct8(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
 cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);

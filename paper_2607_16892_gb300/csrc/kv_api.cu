@@ -31,10 +31,13 @@ constexpr int64_t kFewRows = 16, kFewRows8 = 24;
 // costs 2 us (five prefixes behind 84 rows each: 62.8 us, 60.5 without it) to 9 (behind 378: 136 and 127).
 constexpr int64_t kManyRows = 64;
 
-// Elements of keys that a call's requests read of their prefixes, had these all the pages of their table rows, up to which each of few
-// rows reads its own, out of L2, in one launch.  Single tokens with 200 of their own, 8 key heads of 128, one by one and once for all: 6 behind 2048
-// 16.7 and 23.9 us (8 bits: 17.1 and 27.2); 16 behind 2048, this many, 22.9 and 24.6 (23.3 and 27.6); 32 behind 2048 31.3 and 26.2.
-constexpr int64_t kDirectElements = 32 << 20;
+// Elements of keys that a call's requests read of their prefixes, had these all the pages of their table rows, times the groups of eight
+// rows that share a key head: up to this, and that many rows, each request reads its own prefix, out of L2, in one launch.  8 key
+// heads of 128, 200 own tokens, one by one and once for all: 4 rows, 6 requests behind 2048 (12 M) 16.7 and 23.9 us (8 bits: 17.1 and 27.2), 6 behind
+// 8192 (48 M) 27.0 and 29.0 (28.4 and 33.2), 16 behind 4096 (64 M) 29.2 and 26.5 (33.3 and 29.2); 12 rows, 6 behind 2048 (24 M) 23.0 and 29.3 (22.9
+// and 32.2), 16 behind 2048 (64 M) 33.3 and 29.3 (33.2 and 32.0); 32 rows, 6 behind 2048 (48 M) 31.1 and 40.5 (37.3 and 44.7), 4 behind 8192 (128 M) 46.5
+// and 45.2 (57.8 and 49.8).
+constexpr int64_t kDirectElements = 48 << 20, kDirectRows = 32;
 
 int log2_of(int32_t v) {
     int s = 0;
@@ -610,7 +613,8 @@ int kvdro_kv_attend_shared(kvdro_kv* kv, int32_t B, int32_t T, int32_t n_heads, 
     if (int rc = turn.begin(ctx, s)) return rc;
     const int64_t most = most_tokens(max_q, B, T);
     const int64_t each = (int64_t)prefix_pages * kv->page_size;  // positions, below 2^31
-    if (most * a.group <= kFewRows && each <= kDirectElements && B * each * (kv->heads * kv->head_dim) <= kDirectElements) {
+    if (most * a.group <= kDirectRows && each <= kDirectElements &&
+        B * each * (kv->heads * kv->head_dim) * ((most * a.group + 7) / 8) <= kDirectElements) {
         a.pre_off = share_off;
         a.pre_len = prefix_len;
         a.pre_table = prefix_table;

@@ -874,7 +874,7 @@ template <bool H, int D, bool Q, bool S>
 cudaError_t prepare() {
     cudaError_t e = prepare<H, D, 1, Q, S>();
     if (e == cudaSuccess) e = prepare<H, D, 2, Q, S>();
-    if constexpr (Q && !S)
+    if constexpr (Q)
         if (e == cudaSuccess) e = prepare<H, D, 3, Q, S>();
     return e;
 }
@@ -902,7 +902,7 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool early, int sms,
 template <bool H, int D, bool Q, bool S>
 cudaError_t launch(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s) {
     if (rows <= 8) return launch<H, D, 1, Q, S>(a, maps, early, sms, s);
-    if constexpr (Q && !S)
+    if constexpr (Q)
         if (rows > 16) return launch<H, D, 3, Q, S>(a, maps, early, sms, s);
     return launch<H, D, 2, Q, S>(a, maps, early, sms, s);
 }

@@ -112,7 +112,7 @@ class Shared:
         self.q_off, self.kv_len = c.q_off[:B + 1].contiguous(), c.kv_len[:B].contiguous()
         self.table, self.prefix_table = c.table[:B].contiguous(), c.table[B:].contiguous()
         if wide:
-            pages = (32 << 20) // (B * c.page * c.Hkv * c.D) + 1
+            pages = (48 << 20) // (B * c.page * c.Hkv * c.D) + 1
             self.prefix_table = torch.nn.functional.pad(self.prefix_table, (0, max(0, pages - self.prefix_table.shape[1])), value=-1)
 
     def whole(self):
