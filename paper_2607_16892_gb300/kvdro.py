@@ -16,6 +16,7 @@ go to torch's current stream then.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 import weakref
@@ -402,6 +403,12 @@ _kv_lock = threading.RLock()
 _I2, _I3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
+@functools.lru_cache(maxsize=256)
+def _two(s0: int, s1: int):
+    """Two strides as the library takes them, made once for each pair (a step's calls have the same ones)."""
+    return _I2(s0, s1)
+
+
 _lib_kv = _i32 = _f32 = None  # the loaded library and torch's dtypes
 _current_stream = None  # torch's current stream of a device, as a number (its public form takes a microsecond)
 
@@ -429,7 +436,7 @@ def _heads(cache: KvdroKv, name: str, a: Any, T=None, heads=None):
                 s0, s1, s2 = a.stride()
                 if s2 == 1:
                     # a dimension of one element has no stride of its own: any that the library takes will do
-                    return a.data_ptr(), _I2(s0 if t > 1 else 8, s1 if h > 1 else 8), t, h
+                    return a.data_ptr(), _two(s0 if t > 1 else 8, s1 if h > 1 else 8), t, h
     except (AttributeError, ValueError):
         pass
     if not getattr(a, "is_cuda", False):
