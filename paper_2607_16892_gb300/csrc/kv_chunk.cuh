@@ -716,6 +716,9 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                                 if (nones >> (16 * i >> a.page_shift) & 1) skip |= 1u << i;
                         }
                         if (lane == 0) sh.skip[note & (kNotes - 1)] = skip;
+                        // 8 bits: pages that are none, or no row's business.  Their codes come as zeros, and so must their scales: those of any
+                        // page may be bytes that nobody wrote, and 0 times the infinity of 255 is NaN, in all columns of every row of the tile.
+                        const uint32_t empty_pages = Q ? __ballot_sync(~0u, lane < n && page >= a.n_pages) : 0u;
                         __syncwarp();
                         for (int v = 0; v < 2; v++) {
                             if (turns >= (uint32_t)kRing) wait(empty[stage], round ^ 1, sh);
@@ -723,14 +726,24 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                             if (!ok) break;
                             const uint32_t bar = smem_u32(&full[stage]);
                             const bool skip_it = a.skip == note;  // a test's wait that runs out
-                            if (lane == 0 && !skip_it) mbar_expect(bar, Q ? Sh::kCodes + kKeys : kTile);
+                            if (Q && empty_pages) {
+                                if (empty_pages >> lane & 1) {
+                                    for (int i = 0; i < 1 << a.page_shift; i += 16)
+                                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(scale_at + stage * kKeys + (lane << a.page_shift) + i),
+                                                     "r"(0)
+                                                     : "memory");
+                                    fence_proxy_async();  // before the copy that comes to this stage next
+                                }
+                                __syncwarp();
+                            }
+                            if (lane == 0 && !skip_it) mbar_expect(bar, Q ? Sh::kCodes + kKeys - (__popc(empty_pages) << a.page_shift) : kTile);
                             __syncwarp();
                             if (lane < n && !skip_it) {
-                                if constexpr (Q) {  // (scales of any page, if it is none)
+                                if constexpr (Q) {
                                     load_box(raw_at + stage * Sh::kCodes + (lane << a.page_shift) * D, v ? &vmap : &kmap, 0, 0, w.at.h, page, bar);
-                                    const int64_t from = page < a.n_pages ? page : 0;
-                                    load_bytes(scale_at + stage * kKeys + (lane << a.page_shift),
-                                               (v ? a.v_exp : a.k_exp) + ((from * a.kv_heads + w.at.h) << a.page_shift), 1 << a.page_shift, bar);
+                                    if (page < a.n_pages)
+                                        load_bytes(scale_at + stage * kKeys + (lane << a.page_shift),
+                                                   (v ? a.v_exp : a.k_exp) + (((int64_t)page * a.kv_heads + w.at.h) << a.page_shift), 1 << a.page_shift, bar);
                                 } else {
                                     const uint32_t to = kv_at + stage * kTile + (lane << a.page_shift) * 128;
 #pragma unroll
