@@ -19,7 +19,9 @@
 //
 // Caches of 8 bits (Q): codes become FP16, exactly, two to an instruction, as they leave shared memory, whatever the type of the
 // queries; BF16 queries become FP16 times a power of two per row.  A key's scale multiplies its scores.  A value's scale goes
-// into its weight, 2^(s + E - m_o), so O has a maximum of its own, that of s + E: nothing is lost whatever the scales' range.
+// into its weight for O, 2^(s - m + E - c), beside 2^(s - m) in the sum: c, a whole number, follows the largest s - m + E as m follows the
+// largest s, so that tokens' sizes may differ by any factor.  As weights are FP16, held 2^7 above 1 at the largest, what is below 2^-32 of a
+// row's largest weight times 2^E is lost, also in columns where that token holds zeros.
 // V is transposed in pairs of columns, as 16-bit elements, and a byte permutation per register parts them.
 // Half the bytes leave half the time for as many positions, and what bounds such a kernel first is its own code: unrolled over 32
 // positions it took 1050 instructions a slice (70 us for the batch below), over 64 1700 and as long, warps waiting for instructions
@@ -44,6 +46,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps, kMostRows = 24;
 constexpr int kMostCtas = 4;  // per SM
 constexpr int kOver = 2;      // a tile's fixed cost, in blocks (0 / 1 / 2: window case 41.3 / 40.3 / 39.6 us)
 constexpr int kAtOnce = 8;    // pieces read at a time
+constexpr float kTop = kRaise + kLift<true>;  // 8 bits: weights are 2^15 at most, which FP16 holds
 
 template <int D, int NR, bool Q>
 struct Ring {  // a stage: K or V of a slice; 8 bits: both
@@ -118,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     constexpr int kStages = Ring<D, NR, Q>::kStages, kStage = Ring<D, NR, Q>::kBytes, KS = D / 16, DT = D / 16, MT = kSlice / 16;
     constexpr int kRows = 8 * NR;
     using DecodeLine = Line<kRows, kKeys, kSlice, kOver, Q && NR == 1, S>;
-    constexpr bool F16 = H || Q;  // the type of the products
+    constexpr bool kLifted = H && !Q;  // weights are 2^(s - m + kLift); 8 bits: 2^(s - m), of an m that lies below by that much
     // Where column c of row r of the sums stands in shared memory, without bank conflicts.
     auto sum_at = [](int r, int c) { return Q ? r * D + (c ^ (r >> 1 & 3) << 3) : r * (D + 4) + c; };
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
@@ -276,8 +279,8 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     uint32_t qf[NR][KS][2];
     float o[NR][DT][4];  // columns 16 d + (lane >> 2) and 8 more (8 bits: 16 d + 2 (lane >> 2) and 1 more), of the rows
     float m[NR][2], l[NR][2];  // of rows 8 n + 2 (lane & 3) + i
-    float mo[NR][2], qmul[NR][2];  // 8 bits: what O refers to, and what turns products into scores
-    float up[NR][2], upo[NR][2];   // 8 bits: m and mo are raised above this
+    float qmul[NR][2];          // 8 bits: what turns products into scores
+    float c[NR][2], up[NR][2];  // 8 bits: O refers to 2^(m + c), c a whole number; m is raised where s - m passes `up`
     int2 see[NR][2];
     int2 all_see, any_see;  // positions that every row of the tile sees, and that some row does
     int none = 0;           // S: from here to 0 there are no positions
@@ -359,8 +362,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     see[n][i] = line.seen(at.r, line.token(first + min(8 * n + 2 * (lane & 3) + i, rows - 1)));
-                    m[n][i] = mo[n][i] = Q ? 0.f : -INFINITY;
-                    up[n][i] = upo[n][i] = -INFINITY;
+                    m[n][i] = Q ? 0.f : -INFINITY;
+                    c[n][i] = 0.f;
+                    up[n][i] = -INFINITY;  // nothing seen so far
                     l[n][i] = 0.f;
                 }
 #pragma unroll
@@ -425,16 +429,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         ks[i] = scale_of(load_u8(ke + 16 * t + 8 * i));
                         vs[i] = (float)((int)load_u8(ve + 16 * t + 8 * i) - 127);
                     }
-                    float top[NR][2], topo[NR][2];
-#pragma unroll
-                    for (int n = 0; n < NR; n++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++) s[n][i] *= ks[i >> 1];
+                    // Exponents of the weights in l, d = s - m, and of those in O, e = d + (E - c), whose factor is a power of two: whatever FP32
+                    // made of s, both come from the same d, so that O / l is a mean.
+                    float e[NR][4];
                     bool raise = false;
 #pragma unroll
                     for (int n = 0; n < NR; n++) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) s[n][i] = score(s[n][i], qmul[n][i & 1], cap2);
+                        for (int i = 0; i < 4; i++) s[n][i] = score(s[n][i] * ks[i >> 1], qmul[n][i & 1], cap2);
                         if (edge) {
                             const int j = j0 + 16 * t + (lane >> 2);
 #pragma unroll
@@ -444,33 +446,42 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                                     s[n][i] = -INFINITY;
                         }
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            top[n][i] = fmaxf(s[n][i], s[n][i + 2]);
-                            topo[n][i] = fmaxf(s[n][i] + vs[0], s[n][i + 2] + vs[1]);
-                            raise |= top[n][i] > up[n][i] || topo[n][i] > upo[n][i];
+                        for (int i = 0; i < 4; i++) {
+                            s[n][i] -= m[n][i & 1];
+                            e[n][i] = s[n][i] + (vs[i >> 1] - c[n][i & 1]);
                         }
+#pragma unroll
+                        for (int i = 0; i < 2; i++) raise |= fmaxf(s[n][i], s[n][i + 2]) > up[n][i] || fmaxf(e[n][i], e[n][i + 2]) > kTop;
                     }
-                    if (__any_sync(~0u, raise)) {
+                    if (__any_sync(~0u, raise)) {  // m by whatever brings the largest d to 7, c what brings the largest e there
 #pragma unroll
                         for (int n = 0; n < NR; n++)
 #pragma unroll
                             for (int i = 0; i < 2; i++) {
-                                float to = top[n][i], too = topo[n][i];
+                                float top = fmaxf(s[n][i], s[n][i + 2]), tope = fmaxf(e[n][i], e[n][i + 2]);
 #pragma unroll
                                 for (int x = 4; x < 32; x <<= 1) {
-                                    to = fmaxf(to, __shfl_xor_sync(~0u, to, x));
-                                    too = fmaxf(too, __shfl_xor_sync(~0u, too, x));
+                                    top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+                                    tope = fmaxf(tope, __shfl_xor_sync(~0u, tope, x));
                                 }
-                                // Nothing seen so far: 0 stands for the maximum, and sums are 0.  (As raises(), by the maximum itself.)
-                                if (up[n][i] != -INFINITY) to = fmaxf(to, m[n][i]);
-                                if (upo[n][i] != -INFINITY) too = fmaxf(too, mo[n][i]);
-                                up[n][i] = to + (fabsf(to) > 0x1p19f ? 0.f : kRaise);
-                                upo[n][i] = too + (fabsf(too) > 0x1p19f ? 0.f : kRaise);
-                                if (to == -INFINITY) to = too = 0.f;
-                                l[n][i] *= exp2_fast(fminf(m[n][i] - to, 0.f));
-                                const float keep = exp2_fast(fminf(mo[n][i] - too, 0.f));
+                                const bool first = up[n][i] == -INFINITY, some = !first || top != -INFINITY;
+                                float by = top - kLift<true>;
+                                if (!first) by = fmaxf(by, 0.f);
+                                const float to = some ? m[n][i] + by : 0.f;
+                                by = to - m[n][i];  // as it was rounded
+                                float by_e = rintf(tope - by - kLift<true>);
+                                if (!first) by_e = fmaxf(by_e, ceilf(-by));  // m + c never falls
+                                if (!(fabsf(by_e) < INFINITY)) by_e = 0.f;   // nothing seen, or a row that is NaN
+                                l[n][i] *= exp2_fast(fminf(-by, 0.f));
+                                const float keep = exp2_fast(fminf(-(by + by_e), 0.f));
                                 m[n][i] = to;
-                                mo[n][i] = too;
+                                c[n][i] += by_e;
+                                if (some) up[n][i] = kTop;
+#pragma unroll
+                                for (int k = 0; k < 4; k += 2) {
+                                    s[n][i + k] -= by;
+                                    e[n][i + k] = s[n][i + k] + (vs[k >> 1] - c[n][i]);
+                                }
 #pragma unroll
                                 for (int d = 0; d < DT; d++) {
                                     o[n][d][i] *= keep;
@@ -483,13 +494,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     for (int n = 0; n < NR; n++) {
 #pragma unroll
                         for (int i = 0; i < 2; i++) {
-                            const float shift = m[n][i] - kLift<true>, shifto = mo[n][i] - kLift<true>;
-                            l[n][i] += exp2_fast(s[n][i] - shift) + exp2_fast(s[n][i + 2] - shift);
-                            s[n][i] = exp2_fast(s[n][i] + vs[0] - shifto);
-                            s[n][i + 2] = exp2_fast(s[n][i + 2] + vs[1] - shifto);
+                            l[n][i] += exp2_fast(s[n][i]) + exp2_fast(s[n][i + 2]);
+                            e[n][i] = exp2_fast(e[n][i]);
+                            e[n][i + 2] = exp2_fast(e[n][i + 2]);
                         }
-                        pf[n][0] = transpose8(pack2<true>(s[n][0], s[n][1]));
-                        pf[n][1] = transpose8(pack2<true>(s[n][2], s[n][3]));
+                        pf[n][0] = transpose8(pack2<true>(e[n][0], e[n][1]));
+                        pf[n][1] = transpose8(pack2<true>(e[n][2], e[n][3]));
                     }
                     if (!odd) {
                         uint32_t keep[2] = {~0u, ~0u};  // values of positions that no row sees are taken as zero, whatever is stored there
@@ -524,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                                 bool see_k[2];
 #pragma unroll
                                 for (int i = 0; i < 2; i++) {
-                                    w[i] = __shfl_sync(~0u, k & 8 ? s[n][2 + i] : s[n][i], from);
+                                    w[i] = __shfl_sync(~0u, k & 8 ? e[n][2 + i] : e[n][i], from);
                                     see_k[i] = j >= see[n][i].x && j < see[n][i].y && !(gap >> t & 1) && !(S && j >= none && j < 0);
                                 }
 #pragma unroll
@@ -713,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             for (int n = 0; n < NR; n++)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    if (Q && up[n][i] == -INFINITY) m[n][i] = mo[n][i] = -INFINITY;
+                    if (Q && up[n][i] == -INFINITY) m[n][i] = -INFINITY;
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(~0u, l[n][i], x);
                     if (lane < 4) {
@@ -735,11 +745,11 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                 const int64_t row = t * a.heads + h;
                 if (a.part == Part::kLeave) {
                     for (int i = 0; i < N; i += 2) *reinterpret_cast<float2*>(a.sums + row * D + c + i) = make_float2(x[i], x[i + 1]);
-                    if (c == 0) leave_max<F16>(a, row, to, sum);
+                    if (c == 0) leave_max<kLifted>(a, row, to, sum);
                     return;
                 }
                 if (a.part == Part::kJoin) {
-                    const float2 by = join_max<F16>(a, row, to, sum);
+                    const float2 by = join_max<kLifted>(a, row, to, sum);
                     join_sums<D, N>(a, row, c, by, x);
                 }
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -748,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                 uint16_t* const to_out = a.out + t * a.out_tok + h * a.out_head + c;
                 if constexpr (N == 4) *reinterpret_cast<uint2*>(to_out) = make_uint2(y[0], y[1]);
                 else *reinterpret_cast<uint32_t*>(to_out) = y[0];
-                if (a.lse && c == 0) a.lse[row] = log_sum<F16>(to, sum);
+                if (a.lse && c == 0) a.lse[row] = log_sum<kLifted>(to, sum);
             };
             constexpr int kQuads = D / 4;
             // Each warp's sums go over its own last stage, whose next copy waits for that; eight rows at a time.
@@ -761,7 +771,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     const int r = 2 * (lane & 3) + i;
                     float to = s_m[my_head * of_head][8 * n + r];
                     for (int w = 1; w < of_head; w++) to = fmaxf(to, s_m[my_head * of_head + w][8 * n + r]);
-                    const float f = exp2_fast((Q ? mo[n][i] : m[n][i]) - (to == -INFINITY ? 0.f : to));
+                    const float f = exp2_fast(m[n][i] - (to == -INFINITY ? 0.f : to) + (Q ? c[n][i] : 0.f));
 #pragma unroll
                     for (int d = 0; d < DT; d++) {
                         if constexpr (Q) {

@@ -1,6 +1,7 @@
-"""Caches of 8 bits at the ends of their ranges."""
+"""Caches of 8 bits at the ends of their ranges: pages that are none, values and keys near the type's largest, scores so large that FP32 rounds them."""
 
 import copy
+import math
 
 import pytest
 
@@ -8,7 +9,8 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2607_16892_gb300 import kvdro  # noqa: E402
-from tests.kv8_support import Case8, Shared  # noqa: E402
+from tests.kv8_support import F64, Case8, Shared  # noqa: E402
+from tests.kv_support import UNIT  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -77,3 +79,58 @@ def test_a_page_of_a_prefix_that_is_none_is_left_out(ctx, lens, wide, dtype, D, 
     for x in (s.c.keys, s.c.values):
         x[s.B] = torch.cat([x[s.B][:3 * page], x[s.B][4 * page:]])
     s.check(out, lse)
+
+
+@pytest.mark.parametrize("q", [1, 3, 6, 40])
+@pytest.mark.parametrize("n", [1, 40, 700])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64), ("fp16", 128)])
+def test_large_scores_leave_a_mean_a_mean(ctx, q, n, dtype, D):
+    """All keys are the same one, so that the scores are equal whatever FP32 makes of them, and the result is the mean of the values, which
+    differ in size.  Off by u for its own rounding, u for its weights' (FP16 ones of at least 2^-7: normal numbers) and 2^-18 for exponentials
+    and sums: no part of a score."""
+    case = Case8([(q, n)], dtype, D, 8, 2, 16, seed=n, spread=6.0)
+    k = torch.zeros((n, 2, D), device="cuda", dtype=case.dt)
+    k[..., 0] = 1.0
+    case.set(0, k, case.values[0].to(case.dt))
+    case.q.zero_()
+    case.q[..., 0] = 1.3671875
+    u, v = UNIT[case.dt], case.values[0].repeat_interleave(4, 1)
+    ref, size = v.mean(0), v.abs().mean(0)
+    tol = u * ref.abs() + (u + 2.0 ** -18) * size + (2.0 ** -25 if dtype == "fp16" else 0.0)
+    for x in range(0, 27):
+        # in units of log2 just below 2^x too, where a score and a value's exponent together may need a bit more
+        for scale in (2.0 ** x, -2.0 ** x, 2.0 ** x * 0.9999 / 1.3671875 * math.log(2)):
+            out, lse = case.run(ctx, causal=False, scale=scale)
+            assert torch.isfinite(lse).all()
+            worst = ((out.to(F64) - ref).abs() / tol).max()
+            assert worst <= 1, (scale, float(worst))
+    kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("q", [1, 3, 6, 40])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("B", [1, 300])
+def test_scores_so_large_that_their_spacing_matters(ctx, q, dtype, D, B):
+    """Scores of 2^16 to 2^27 that climb or fall in small steps, over values of sizes of 2^-6 to 2^6: whatever FP32 makes of them, a result is a
+    mean of values."""
+    kv = 2000
+    case = Case8([(q, kv)], dtype, D, 4, 1, 16, seed=1, spread=6.0)
+    v = case.values[0].to(case.dt)
+    case.table, case.kv_len, case.q = case.table.repeat(B, 1), case.kv_len.repeat(B), case.q.repeat(B, 1, 1)
+    case.lens, case.T = case.lens * B, B * q
+    case.q_off = torch.arange(B + 1, dtype=torch.int32, device="cuda") * q
+    held = case.values[0].abs().amax(0).clamp(min=0) * 1.01
+    codes = torch.arange(0x7f, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).float()
+    climb = codes[torch.arange(kv, device="cuda") * 127 // kv]
+    for e in range(16, 27):
+        for step, keys in ((0.05, climb), (0.4, climb), (0.05, climb.flip(0))):
+            k = torch.zeros((kv, 1, D), device="cuda")
+            k[..., 0], k[..., 1] = 448.0, keys[:, None]
+            case.set(0, k.to(case.dt), v)
+            case.q.zero_()
+            case.q[..., 0], case.q[..., 1] = 1.0, step * 2.0 ** (8 - e)
+            for scale in (2.0 ** (e - 8), -2.0 ** (e - 8)):
+                out, lse = case.run(ctx, scale=scale, max_q=q)
+                assert torch.isfinite(lse).all() and torch.isfinite(out).all(), (e, step, scale)
+                assert (out.to(F64).abs() <= held).all(), (e, step, scale)
+    kvdro.kvdro_sync(ctx)
