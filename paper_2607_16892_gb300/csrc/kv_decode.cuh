@@ -112,6 +112,14 @@ __device__ __forceinline__ uint32_t load_u8(uint32_t at) {
     return x;
 }
 
+// 8 bits: rows are left in units of 2^k, which brings their sum of weights into [1/2, 1): sums of weights times values are then no larger than
+// the values.  k for a sum that refers to m, or 0 where m + k is rounded.
+__device__ __forceinline__ float unit_of(float m, float sum) {
+    const float k = (float)((int)(__float_as_uint(sum) >> 23) - 126);
+    return sum > 0.f && sum < INFINITY && (m + k) - m == k ? k : 0.f;
+}
+__device__ __forceinline__ float power_of(float k) { return __uint_as_float((uint32_t)(127 + (int)k) << 23); }  // 2^k, -126 to 127
+
 // NR: groups of eight rows of a tile.
 template <bool H, int D, int NR, bool Q, bool S>
 __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
@@ -127,6 +135,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
     __shared__ alignas(8) uint64_t s_bar[kWarps][kStages];
     __shared__ Stretch<kThreads> s_part;
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+    __shared__ float2 s_row[kWarps][Q ? kRows : 1];  // 8 bits: of the warp's head, a row's maximum and sum over all of the head's warps
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(s_raw), ring = ((raw + 1023) & ~1023u) + warp * kStages * kStage;
@@ -749,7 +758,12 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                     return;
                 }
                 if (a.part == Part::kJoin) {
-                    const float2 by = join_max<kLifted>(a, row, to, sum);
+                    float2 by = join_max<kLifted>(a, row, to, sum);
+                    if constexpr (Q) {  // of two sums below 1, the half
+                        by = make_float2(0.5f * by.x, 0.5f * by.y);
+                        sum *= 0.5f;
+                        to += 1.f;
+                    }
                     join_sums<D, N>(a, row, c, by, x);
                 }
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -763,15 +777,59 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
             constexpr int kQuads = D / 4;
             // Each warp's sums go over its own last stage, whose next copy waits for that; eight rows at a time.
             float* const mine_o = reinterpret_cast<float*>(ring_ptr + stage * kStage);
+            float by[NR][2];  // 8 bits: from what this warp's O refers to, to the row's unit
+            if constexpr (Q) {
+                bool far = false;
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const int r = 8 * n + 2 * (lane & 3) + i;
+                        float mw[kWarps], lw[kWarps], to = -INFINITY, sum = 0.f;
+#pragma unroll
+                        for (int w = 0; w < kWarps; w++) {
+                            mw[w] = w < of_head ? s_m[my_head * of_head + w][r] : -INFINITY;
+                            lw[w] = w < of_head ? s_l[my_head * of_head + w][r] : 0.f;
+                            to = fmaxf(to, mw[w]);
+                        }
+                        const float shift = to == -INFINITY ? 0.f : to;
+#pragma unroll
+                        for (int w = 0; w < kWarps; w++) sum += lw[w] * exp2_fast(mw[w] - shift);
+                        const float k = unit_of(to, sum);
+                        if (lane < 4) s_row[warp][r] = make_float2(to + k, sum * power_of(-k));
+                        by[n][i] = m[n][i] - shift + (c[n][i] - k);  // up to 127
+                        far |= by[n][i] < -100.f && m[n][i] > -INFINITY;
+                    }
+                far = __any_sync(~0u, far);
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        if (far) {  // two steps, for 2^by may be far below FP32's numbers
+                            const float g = exp2_fast(fminf(by[n][i] + 100.f, 0.f));
+#pragma unroll
+                            for (int d = 0; d < DT; d++) {
+                                o[n][d][i] *= g;
+                                o[n][d][i + 2] *= g;
+                            }
+                        }
+                        by[n][i] = exp2_fast(fmaxf(by[n][i], -100.f));
+                    }
+            }
 #pragma unroll
             for (int n = 0; n < NR; n++) {
-                if (n > 0) __syncthreads();
+                if (n > 0) __syncthreads();  // (the sums of the eight rows before have been read)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     const int r = 2 * (lane & 3) + i;
-                    float to = s_m[my_head * of_head][8 * n + r];
-                    for (int w = 1; w < of_head; w++) to = fmaxf(to, s_m[my_head * of_head + w][8 * n + r]);
-                    const float f = exp2_fast(m[n][i] - (to == -INFINITY ? 0.f : to) + (Q ? c[n][i] : 0.f));
+                    float f;
+                    if constexpr (Q) {
+                        f = by[n][i];
+                    } else {
+                        float to = s_m[my_head * of_head][8 * n + r];
+                        for (int w = 1; w < of_head; w++) to = fmaxf(to, s_m[my_head * of_head + w][8 * n + r]);
+                        f = exp2_fast(m[n][i] - (to == -INFINITY ? 0.f : to));
+                    }
 #pragma unroll
                     for (int d = 0; d < DT; d++) {
                         if constexpr (Q) {
@@ -785,8 +843,14 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                 __syncthreads();
                 for (int i = tid; i < (min(8, rows - 8 * n) << hs) * kQuads; i += kThreads) {
                     const int all = i / kQuads, r8 = all >> hs, of = all - (r8 << hs), c = 4 * (i % kQuads), r = 8 * n + r8, w0 = of * of_head, w1 = w0 + of_head;
-                    float to = s_m[w0][r], sum = 0.f;
-                    for (int w = w0 + 1; w < w1; w++) to = fmaxf(to, s_m[w][r]);
+                    float to, sum = 0.f;
+                    if constexpr (Q) {
+                        to = s_row[w0][r].x;
+                        sum = s_row[w0][r].y;
+                    } else {
+                        to = s_m[w0][r];
+                        for (int w = w0 + 1; w < w1; w++) to = fmaxf(to, s_m[w][r]);
+                    }
                     float x[4] = {};
                     for (int w = w0; w < w1; w++) {
                         const float4 y = *reinterpret_cast<const float4*>(ring_ptr + (w - warp) * kStages * kStage + stage * kStage + 4 * sum_at(r8, c));
@@ -794,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         x[1] += y.y;
                         x[2] += y.z;
                         x[3] += y.w;
-                        sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
+                        if constexpr (!Q) sum += s_l[w][r] * exp2_fast(s_m[w][r] - (to == -INFINITY ? 0.f : to));
                     }
                     if (whole) {
                         row_out(of, r, c, x, to, sum);
@@ -834,11 +898,19 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                             float up = ml.x;
                             for (int o = 16; o; o >>= 1) up = fmaxf(up, __shfl_xor_sync(~0u, up, o));
                             up = fmaxf(up, to);
-                            const float shift = up == -INFINITY ? 0.f : up, keep = exp2_fast(to - shift), f = exp2_fast(ml.x - shift);
+                            const float shift = up == -INFINITY ? 0.f : up;
+                            float keep = exp2_fast(to - shift), f = exp2_fast(ml.x - shift);
                             to = up;
                             float l = ml.y * f;
                             for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
                             sum = sum * keep + l;
+                            if constexpr (Q) {
+                                const float k = unit_of(to, sum), by = power_of(-k);
+                                sum *= by;
+                                keep *= by;
+                                f *= by;
+                                to += k;
+                            }
                             for (int i = 0; i < V; i++) x[i] *= keep;
                             for (int k0 = 0; k0 < n; k0 += kAtOnce) {
                                 float y[kAtOnce][V];

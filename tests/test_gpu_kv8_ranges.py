@@ -81,6 +81,48 @@ def test_a_page_of_a_prefix_that_is_none_is_left_out(ctx, lens, wide, dtype, D, 
     s.check(out, lse)
 
 
+def large_values(case, e):
+    """The values of every request within 1.7 * 2^e, whatever is asked of the scale: 448 * 2^119 = 1.75 * 2^127."""
+    g = torch.Generator(device="cuda").manual_seed(e + 200)
+    for b, (_, kv) in enumerate(case.lens):
+        v = (2 * torch.rand((kv, case.Hkv, case.D), generator=g, device="cuda", dtype=F64) - 1) * 1.7 * 2.0 ** e
+        case.set(b, case.keys[b].to(case.dt), v.to(case.dt))
+
+
+@pytest.mark.parametrize("q", [1, 3, 6])
+@pytest.mark.parametrize("n", [1, 2, 40, 3000])
+@pytest.mark.parametrize("e", [-118, 113, 121, 125, 127])
+def test_few_rows_over_values_near_the_largest(ctx, q, n, e):
+    """BF16: a mean of values is no larger than they are, however many, one request alone (pieces joined) or many; and the smallest."""
+    for B, D in ((1, 128), (200, 64)):
+        case = Case8([(q, n)] * B, "bf16", D, 8, 2, 16, seed=n)
+        large_values(case, e)
+        out, lse = case.run(ctx, causal=False)
+        kvdro.kvdro_sync(ctx)
+        case.check(out, lse, causal=False, only={0, B - 1})
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("e", [-118, 113, 121, 125, 127])
+def test_prefixes_of_values_near_the_largest(ctx, wide, e):
+    for n in (1, 3000):
+        s = Shared([(1, 1), (1, 300), (2, 40)], [0, 3], [n], bits=8, wide=wide, dtype="bf16", D=128, Hq=8, Hkv=2, page=16, seed=3)
+        large_values(s.c, e)
+        out, lse = s.run(ctx)
+        kvdro.kvdro_sync(ctx)
+        s.check(out, lse)
+
+
+@pytest.mark.parametrize("q,n,e", [(40, 1, 127), (300, 1, 121), (40, 3000, 106)])
+def test_chunks_over_large_values(ctx, q, n, e):
+    """Their sums are not divided before the end: n weights of up to 2^8 times values of up to 2^(e + 1) have to stay below 2^128."""
+    case = Case8([(q, n)], "bf16", 128, 8, 2, 16, seed=n)
+    large_values(case, e)
+    out, lse = case.run(ctx, causal=False)
+    kvdro.kvdro_sync(ctx)
+    case.check(out, lse, causal=False)
+
+
 @pytest.mark.parametrize("q", [1, 3, 6, 40])
 @pytest.mark.parametrize("n", [1, 40, 700])
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64), ("fp16", 128)])
