@@ -432,7 +432,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                             }
                         }
                     }
-                    float ks[2], vs[2];  // scales of the keys, exponents of the values'
+                    // Scales of the keys, exponents of the values'.  A key's scale meets its query's first: one of 2^119 times a sum of codes, 2^17 at
+                    // most, would pass FP32 before a query of 2^-110 brings it back.
+                    float ks[2], vs[2];
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         ks[i] = scale_of(load_u8(ke + 16 * t + 8 * i));
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
 #pragma unroll
                     for (int n = 0; n < NR; n++) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) s[n][i] = score(s[n][i] * ks[i >> 1], qmul[n][i & 1], cap2);
+                        for (int i = 0; i < 4; i++) s[n][i] = score(s[n][i], ks[i >> 1] * qmul[n][i & 1], cap2);
                         if (edge) {
                             const int j = j0 + 16 * t + (lane >> 2);
 #pragma unroll

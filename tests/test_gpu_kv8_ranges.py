@@ -176,3 +176,19 @@ def test_scores_so_large_that_their_spacing_matters(ctx, q, dtype, D, B):
                 assert torch.isfinite(lse).all() and torch.isfinite(out).all(), (e, step, scale)
                 assert (out.to(F64).abs() <= held).all(), (e, step, scale)
     kvdro.kvdro_sync(ctx)
+
+
+@pytest.mark.parametrize("q", [1, 3, 6, 40])
+@pytest.mark.parametrize("D", [64, 128])
+def test_keys_near_the_largest_and_small_queries(ctx, q, D):
+    """Scores of ordinary size from keys of 2^125 and queries of 2^-110, and from small keys and large queries; a query of zeros beside them."""
+    for up, down in ((125, -110), (-120, 110)):
+        case = Case8([(q, 300), (1, 40)], "bf16", D, 8, 2, 16, seed=q)
+        for b in range(2):
+            case.set(b, (case.keys[b].clamp(-3, 3) * 2.0 ** up).to(case.dt), case.values[b].to(case.dt))
+        case.q = (case.q.to(F64).clamp(-3, 3) * 2.0 ** down).to(case.dt)
+        case.q[0, ::3] = 0
+        scale = 2.0 ** (-up - down - 3)
+        out, lse = case.run(ctx, scale=scale)
+        kvdro.kvdro_sync(ctx)
+        case.check(out, lse, scale=scale)
