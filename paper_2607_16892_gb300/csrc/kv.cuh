@@ -124,6 +124,7 @@ cudaError_t launch_kv_direct8(const AttendArgs& a, const KvMaps& maps, int rows,
 cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
+bool kv_join_few(int64_t tiles, int sms);  // whether the launch that joins few tiles takes so many
 cudaError_t kv_chunk_prepare();
 cudaError_t kv_chunk8_prepare();
 cudaError_t launch_kv_chunk8(const AttendArgs& a, const KvMaps& maps, bool after_few, int sms, cudaStream_t s);

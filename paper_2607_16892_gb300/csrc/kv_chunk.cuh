@@ -1142,7 +1142,7 @@ cudaError_t launch(const AttendArgs& a, const KvMaps& maps, bool after_few, int 
     c.dynamicSmemBytes = 0;
     c.numAttrs = 1;
     const int64_t tiles = ((int64_t)a.T * a.group / kRows + a.B) * a.kv_heads;  // at most
-    if (tiles <= kFewTiles && sms <= kJoinMost) {
+    if (kv_join_few(tiles, sms)) {
         c.gridDim = dim3(sms * kJoinCtas);
         return cudaLaunchKernelEx(&c, k_kv_join_few<H, D>, a, sms);
     }
