@@ -815,7 +815,8 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                                             const int at = 2 * c + (swap ? !k : k);
                                             asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(kv_at + stage * kTile + (at >> 3) * (kKeys * 128) +
                                                                                                       r * 128 + (((at & 7) ^ (r & 7)) << 4)),
-                                                         "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w));
+                                                         "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w)
+                                                         : "memory");  // read again below, where some row does not see the block
                                         }
                                     }
                                 }
