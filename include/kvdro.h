@@ -250,7 +250,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
  * elements, the codes are x_d / 2^E rounded to nearest, ties to even, so that every element is within 2^-4 of itself or 2^(E-10).
  * Non-finite elements become NaN.  With FP16 rows E = 8 stops at 240 * 2^8 = 61440, for 256 * 2^8 is no FP16 number.
  *   dtype       the type of the rows that calls on the handle take and give (append, read, q, out): KVDRO_BF16 or
- *               KVDRO_FP16.  Values beyond FP16's range (written as BF16) are infinities to a handle of KVDRO_FP16.
+ *               KVDRO_FP16.  To a handle of KVDRO_FP16 elements beyond FP16's range (written as BF16) are infinities in kvdro_kv_read and
+ *               where many new rows share a key head; attention of few (at most 24) multiplies codes and takes them as they are.
  *   k, v, k_exp, v_exp  device memory, 16-byte aligned.  The rest as in kvdro_kv_open.
  */
 int kvdro_kv_open8(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, int32_t page_size, int32_t n_kv_heads,

@@ -192,3 +192,34 @@ def test_keys_near_the_largest_and_small_queries(ctx, q, D):
         out, lse = case.run(ctx, scale=scale)
         kvdro.kvdro_sync(ctx)
         case.check(out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_beyond_fp16_in_attention(ctx, D):
+    """A cache that was written as BF16 and is opened as FP16.  Few rows multiply codes, which are no larger than 448, whatever the scale: values
+    and keys beyond FP16 count as they are.  Chunks widen them to FP16, as reads do: infinities."""
+    for q in (1, 3, 6, 40):
+        case = Case8([(q, 100), (1, 50)], "bf16", D, 8, 2, 16, seed=q)
+        k, v = case.keys[0].to(case.dt), case.values[0].to(case.dt)
+        v[5, :, 3] = 3.0e5  # every row sees it, at a weight of about 1 / 100: a result that FP16 holds
+        case.set(0, k, v)
+        case.dt, case.q = torch.float16, case.q.to(torch.float16) * 0.25
+        out, lse = case.run(ctx)
+        kvdro.kvdro_sync(ctx)
+        if q < 40:
+            case.check(out, lse)
+        else:
+            assert torch.isinf(out[:q, :, 3]).all() and torch.isfinite(out[:q, :, 4:]).all()
+        k[5, :, 7], v[5, :, 3] = -2.0 ** 17, 1.0
+        case.dt = torch.bfloat16
+        case.set(0, k, v)
+        case.dt = torch.float16
+        case.q[..., 7] = 2.0 ** -14
+        out, lse = case.run(ctx)
+        kvdro.kvdro_sync(ctx)
+        if q < 40:
+            case.check(out, lse)
+        else:  # a score of -infinity
+            case.keys[0], case.values[0] = (torch.cat([x[0][:5], x[0][6:]]) for x in (case.keys, case.values))
+            case.lens[0] = (q, 99)
+            case.check(out, lse)
