@@ -716,9 +716,6 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                                 if (nones >> (16 * i >> a.page_shift) & 1) skip |= 1u << i;
                         }
                         if (lane == 0) sh.skip[note & (kNotes - 1)] = skip;
-                        // 8 bits: pages that are none, or no row's business.  Their codes come as zeros, and so must their scales: those of any
-                        // page may be bytes that nobody wrote, and 0 times the infinity of 255 is NaN, in all columns of every row of the tile.
-                        const uint32_t empty_pages = Q ? __ballot_sync(~0u, lane < n && page >= a.n_pages) : 0u;
                         __syncwarp();
                         for (int v = 0; v < 2; v++) {
                             if (turns >= (uint32_t)kRing) wait(empty[stage], round ^ 1, sh);
@@ -726,24 +723,14 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                             if (!ok) break;
                             const uint32_t bar = smem_u32(&full[stage]);
                             const bool skip_it = a.skip == note;  // a test's wait that runs out
-                            if (Q && empty_pages) {
-                                if (empty_pages >> lane & 1) {
-                                    for (int i = 0; i < 1 << a.page_shift; i += 16)
-                                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(scale_at + stage * kKeys + (lane << a.page_shift) + i),
-                                                     "r"(0)
-                                                     : "memory");
-                                    fence_proxy_async();  // before the copy that comes to this stage next
-                                }
-                                __syncwarp();
-                            }
-                            if (lane == 0 && !skip_it) mbar_expect(bar, Q ? Sh::kCodes + kKeys - (__popc(empty_pages) << a.page_shift) : kTile);
+                            if (lane == 0 && !skip_it) mbar_expect(bar, Q ? Sh::kCodes + kKeys : kTile);
                             __syncwarp();
                             if (lane < n && !skip_it) {
-                                if constexpr (Q) {
+                                if constexpr (Q) {  // (scales of any page, if it is none)
                                     load_box(raw_at + stage * Sh::kCodes + (lane << a.page_shift) * D, v ? &vmap : &kmap, 0, 0, w.at.h, page, bar);
-                                    if (page < a.n_pages)
-                                        load_bytes(scale_at + stage * kKeys + (lane << a.page_shift),
-                                                   (v ? a.v_exp : a.k_exp) + (((int64_t)page * a.kv_heads + w.at.h) << a.page_shift), 1 << a.page_shift, bar);
+                                    const int64_t from = page < a.n_pages ? page : 0;
+                                    load_bytes(scale_at + stage * kKeys + (lane << a.page_shift),
+                                               (v ? a.v_exp : a.k_exp) + ((from * a.kv_heads + w.at.h) << a.page_shift), 1 << a.page_shift, bar);
                                 } else {
                                     const uint32_t to = kv_at + stage * kTile + (lane << a.page_shift) * 128;
 #pragma unroll
@@ -775,7 +762,7 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                 constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes, kRowsOf = kKeys / 4;  // lanes of a row; rows at a time, and of a warp
                 const int c = lane % kLanes;
                 const bool swap = D == 128 && c >= kLanes / 2;
-                int raw = 0;
+                int raw = 0, note = 0;  // note: blocks of the stretch before this piece
                 uint32_t raw_round = 0, turns = 0;
                 while (w.more) {
                     const int2 all = w.all_see();
@@ -787,6 +774,14 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                             if (turns++ >= (uint32_t)kStages) wait(sh.kv_empty[stage], round ^ 1, sh);
                             wait(sh.raw_full[raw], raw_round, sh);
                             __syncwarp();
+                            // Codes of pages that are none came as zeros, with scales of some page, which may be bytes that nobody wrote: 0 times
+                            // the infinity of 255 is NaN.
+                            const uint32_t skip = sh.skip[(note + blk - w.p0) & (kNotes - 1)];
+                            if (skip) {
+                                const int r = part * kRowsOf + lane;
+                                if (skip >> (r / 16) & 1) asm volatile("st.shared.u8 [%0], %1;" ::"r"(scale_at + raw * kKeys + r), "r"(0) : "memory");
+                                __syncwarp();
+                            }
                             // Four rows of a lane at once, so that their loads overlap; what is rare is kept out of this loop, for the
                             // instruction cache.
                             auto tile = [&](auto in_half) {
@@ -867,6 +862,7 @@ __global__ void __launch_bounds__(kThreadsOf<Q>, 1)
                             }
                         }
                     }
+                    note += w.p1 - w.p0;
                     w.next();
                 }
             } else {
