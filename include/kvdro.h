@@ -248,7 +248,8 @@ int kvdro_kv_open(kvdro_ctx* ctx, kvdro_kv** out, int dtype, int32_t n_pages, in
  * an element stands for its code times 2^(byte - 127).  Bytes are 1 to 254; 0 stands for zeros.
  * kvdro_kv_append quantises as it writes: byte - 127 is the least E >= -126 with max |x_d| <= 448 * 2^E over the head's finite
  * elements, the codes are x_d / 2^E rounded to nearest, ties to even, so that every element is within 2^-4 of itself or 2^(E-10).
- * Non-finite elements become NaN.  With FP16 rows E = 8 stops at 240 * 2^8 = 61440, for 256 * 2^8 is no FP16 number.
+ * Non-finite elements become NaN.  With FP16 rows E = 8 stops at 240 * 2^8 = 61440, for 256 * 2^8 is no FP16 number.  BF16 rows have no such
+ * stop: an element of 1.9375 * 2^127 or more becomes 2^128, which is an infinity as BF16.
  *   dtype       the type of the rows that calls on the handle take and give (append, read, q, out): KVDRO_BF16 or
  *               KVDRO_FP16.  To a handle of KVDRO_FP16 elements beyond FP16's range (written as BF16) are infinities in kvdro_kv_read and
  *               where many new rows share a key head; attention of few (at most 24) multiplies codes and takes them as they are.
@@ -319,8 +320,13 @@ int kvdro_kv_read(kvdro_kv* kv, int32_t B, int32_t T, const int32_t* q_off, cons
  *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q . k_j),   f(x) = x, or softcap tanh(x / softcap)
  * over the positions j < kv_len[b] with j <= p (causal) and j > p - window (window > 0).  A token that sees
  * no position gets out = 0 and lse = -infinity.  What is stored at unseen positions does not
- * matter, NaN included, nor do the table's entries of pages that no token of the request sees (behind a window, say).  Products are of the cache's dtype with FP32 sums; the softmax is FP32, its
- * weights are rounded to the cache's dtype for the product with v.
+ * matter, NaN included, nor do the table's entries of pages that no token of the request sees (behind a window, say).
+ * Products are of the cache's dtype with FP32 sums (scores below 2^120: a query's largest element times a key's times the scale); the softmax is
+ * FP32, its weights are rounded to the cache's dtype for the product with v.  That product's sums are FP32 of weights of up to 2^8 and divided at
+ * the end, so that values above 2^120 / (positions seen) may pass FP32 in them.
+ * Over 8 bits few tokens (up to 24 rows that share a key head) are multiplied as FP16: codes as they are, BF16 queries off by 2^-25 of their row's
+ * largest element at most, and weights times a power of two, w_j 2^(E_j), of which what is below 2^-32 of a row's largest is lost.  Their sums are no
+ * larger than the values.
  *   B          requests, 1 <= B <= 16384;  T: tokens, T >= 0; tokens beyond T are left out, and T tokens of out and lse
  *              are written (zeros and -infinity for tokens of no request).
  *   n_heads    a multiple of n_kv_heads, at most 4096; T * n_heads <= 2^30.

@@ -113,16 +113,16 @@ struct AttendArgs {
 size_t kv_decode_piece_bytes(int sms);
 int kv_decode_ctas(int sms);
 cudaError_t kv_decode_prepare();
-// `rows`: that share a key head, at most (more are right, but slow).  `early`: may start while the launch before it, whose sums it
-// joins, ends.
 cudaError_t kv_decode8_prepare();
 cudaError_t kv_direct_prepare();
 cudaError_t kv_direct8_prepare();
+// `rows`: that share a key head, at most (more are right, but slow).  `early`: may start while the launch before it, whose sums it
+// joins, ends.
+cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
+cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 // The same with a's prefixes in front of the requests' own tokens.
 cudaError_t launch_kv_direct(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
 cudaError_t launch_kv_direct8(const AttendArgs& a, const KvMaps& maps, int rows, int sms, cudaStream_t s);
-cudaError_t launch_kv_decode8(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
-cudaError_t launch_kv_decode(const AttendArgs& a, const KvMaps& maps, int rows, bool early, int sms, cudaStream_t s);
 size_t kv_chunk_piece_bytes(int sms);
 bool kv_join_few(int64_t tiles, int sms);  // whether the launch that joins few tiles takes so many
 cudaError_t kv_chunk_prepare();

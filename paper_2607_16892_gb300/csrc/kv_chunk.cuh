@@ -996,8 +996,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_kv_join(const AttendArgs a) {
 // reads.
 constexpr int kJoinCtas = 3, kJoinPieces = 64;  // per SM; pieces at a time
 constexpr int kJoinMost = 1024;                 // CTAs of the launch before, at most
-// Up to this many tiles.  64 requests behind a prefix of 32768, 8 tiles of 19 pieces: 85 us in all, 93 with the other; 512 tokens over
-// 4099, 64 tiles of three: 47.4 us in all, 45.1 with the other.
+// Up to this many tiles.  64 requests behind a prefix of 32768, 8 tiles of 19 pieces: 85 us in all, 93 with the other; one tile of 63 pieces
+// 20.7 and 41.0; 8 tiles of 32 blocks 20.5 and 22.6.  Near the line the two are alike: 28 tiles 26.7 and 26.7, 34 28.9 and 28.7 (8 bits 32.8 and
+// 31.5); beyond it, 512 tokens over 4099, 64 tiles of three: 47.4 us in all, 45.1 with the other.
 constexpr int64_t kFewTiles = 38;
 
 template <bool H, int D, int N>  // N: 16-byte vectors of a row and thread

@@ -335,8 +335,9 @@ __global__ void __launch_bounds__(kThreads, Ring<D, NR, Q>::kCtas)
                         }
                     }
                     if constexpr (Q && !H) {
-                        // BF16 to FP16 at a row's largest in [1, 2): exact down to 2^-17 of that, off by 2^-25 of it below (less than the
-                        // FP32 sum's rounding).  A NaN stays one, an infinity too.
+                        // BF16 to FP16 at a row's largest in [1, 2): exact down to 2^-17 of that, off by 2^-25 of it below.  Where a key's
+                        // elements are of one size that is less than the FP32 sum's rounding; a key with one large element, on a small one of
+                        // the query, has a score that is off by 2^-25 of the largest of each.  A NaN stays one, an infinity too.
                         float top = 0.f;
 #pragma unroll
                         for (int k = 0; k < KS; k++)

@@ -1,4 +1,4 @@
-// Pages for requests (kvdro_kv_plan) and the write into them (kvdro_kv_append).
+// Pages for requests (kvdro_kv_plan), the write into them (kvdro_kv_append, 16 and 8 bits) and the way back (kvdro_kv_read).
 #include "kv_device.cuh"
 
 #include <type_traits>
@@ -361,8 +361,8 @@ __device__ __forceinline__ uint4 quantise(const uint4 (&x)[2], unsigned mask, in
 
 // As the copy above, a row dealt to lanes of sixteen elements each.  Bound by the bytes: 65539 tokens of 8 heads of 128 in FP16, 396 MB
 // read and written, 67.5 us = 5.9 TB/s.  On the way there: eight elements to a lane and addresses by products, 182 instructions for
-// every eight elements, 115 us; addresses by steps 92; sixteen elements 87; 128 threads 76; ten CTAs per SM (48 registers) 67.5,
-// eight 73.6, twelve 70.9; two or four heads of a lane at once 84 and 98.
+// every eight elements, 115 us; addresses by steps 92; sixteen elements 87; 128 threads 76; ten CTAs per SM (48 registers,
+// and 16 bytes spilled in BF16, 20 in FP16) 67.5, eight 73.6, twelve 70.9; two or four heads of a lane at once 84 and 98.
 constexpr int kAppend8Deep = 1, kAppend8Threads = 128, kAppend8Ctas = 10;
 
 template <bool H>
