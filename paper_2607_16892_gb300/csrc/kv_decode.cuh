@@ -27,8 +27,8 @@
 // positions it took 1050 instructions a slice (70 us for the batch below), over 64 1700 and as long, warps waiting for instructions
 // more often than for data; the loop over 16 positions is rolled, 460 instructions with their share of a slice's, and the batch takes 61.  Copies without any
 // products take 57: rows of 128 bytes are the least that DRAM gives, and rows of 64 are read in pairs of heads.
-// Measured (8 bits): 64 requests of lognormal lengths up to 8192, 8 key heads of 128, 281 MB, 61 to 64 us from one GPU to the next = 4.6 to 4.4
-// TB/s; 4 requests of 131071, 16 heads of 64, 1090 MB, 183 to 205 us = 6.0 to 5.3 TB/s; one request of 1000, 12.8 us, all latency.
+// Measured (8 bits): 64 requests of lognormal lengths up to 8192, 8 key heads of 128, 281 MB, 60 to 64 us from one GPU to the next = 4.7 to 4.4
+// TB/s; 4 requests of 131071, 16 heads of 64, 1090 MB, 180 to 205 us = 6.1 to 5.3 TB/s; one request of 1000, 12.3 us, all latency.
 //
 // With prefixes in front (S) a request's line of blocks begins with its prefix's, and pages are looked up in the one table or the other:
 // what it costs to read a short prefix once per request out of L2 is less than the launches that read it once for all.
